@@ -18,7 +18,6 @@ import torch
 own = False
 
 HEAD = 64
-TEXT = 448
 # what a drawn case has at most, as the largest listed ones: bytes of keys and values, scores, logits
 MOST_BYTES = 2.8e9
 MOST_SCORES = 128 * 20 * 65536
