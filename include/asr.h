@@ -402,6 +402,119 @@ asr_status asr_debug_set_self_kv(asr_ctx* ctx, int32_t slot, const float* src, i
 asr_status asr_logmel_noalloc(const float* const* pcm, const int64_t* n_samples, int32_t n,
                               int32_t n_mels, float* out, void* stream);
 
+/* ---- operators of a decode step with several hypotheses per clip --------
+ * Stateless calls on device memory: every pointer below is a device pointer
+ * of the current device unless it says host, work is enqueued on `stream`
+ * (NULL = default stream) and the calls neither allocate nor synchronise, so
+ * they may be captured into graphs.  Scratch is the caller's: `ws` of at least
+ * the bytes that the _size call gives, 256-byte aligned.  It carries nothing
+ * from one call to the next; calls that may overlap need blocks of their own.
+ * Sizes and pointers are checked (EINVAL, ENOMEM for a small ws); what lies in
+ * device memory (lengths, slots, tokens) is kept in bounds by the kernels as
+ * stated. */
+
+/* Keys and values of a cache [slots][heads][positions][64], any strides
+ * (elements) with the 64 dims of a head contiguous: k and v 16-byte aligned,
+ * strides multiples of 16 bytes, pos_stride >= 64.  An entry (a group, or a
+ * row) uses keys [first, first + len) of its slot: slot NULL means slot =
+ * entry, first NULL 0, len NULL the most there may be; a negative first or
+ * length counts as 0, a range past the last position ends there, and a slot out
+ * of [0, slots) has no keys. */
+typedef struct {
+  const void* k;
+  const void* v;
+  int64_t slot_stride, head_stride, pos_stride;
+  int32_t slots, positions;
+  const int32_t* slot;
+  const int32_t* first;
+  const int32_t* len;
+} asr_keys;
+
+/* Attention of one new token per row over keys shared by the rows of a group
+ * (hypotheses of one clip: its audio, its prompt) and keys of the row's own
+ * behind them:
+ *   out[r][h] = softmax over all keys (scale q[r][h] . k) . v,
+ * query head h reading cache head h / (n_head / n_kv_head).  Shared keys are
+ * read once per group.  A row without any key gives zeros.  Sums are float32;
+ * a row's bits depend neither on the other rows nor on its place (with
+ * part_keys given; 0 lets the library split by the size of the call).
+ *   Group g holds the rows row_of[i], group_start[g] <= i < group_start[g+1]
+ * (row_of NULL: row i), at most max_group of them, each row in one group; group
+ * starts do not fall.  Rows in no group are left as they were, and so are
+ * entries of row_of outside [0, rows).
+ *   q: float32 [rows][n_head * 64], rows q_ld elements apart; out in the
+ * cache's type, rows out_ld apart (both 16-byte aligned, q_ld and out_ld
+ * multiples of 4).  max_prefix and max_own bound the lengths (longer ones are
+ * cut).  prefix is indexed by group, own by row; own.k may be NULL with
+ * max_own = 0, prefix.k with max_prefix = 0. */
+typedef struct {
+  int32_t dtype;       /* asr_dtype of the caches and of out */
+  int32_t n_head, n_kv_head;
+  int32_t rows, groups, max_group;
+  int32_t max_prefix, max_own;
+  int32_t part_keys;   /* keys per part of the work: 0, or a multiple of 128 up to 8192 */
+  float scale;
+  const float* q;
+  int64_t q_ld;
+  void* out;
+  int64_t out_ld;
+  const int32_t* group_start;   /* [groups + 1] */
+  const int32_t* row_of;        /* [rows] or NULL */
+  asr_keys prefix, own;
+} asr_attention;
+asr_status asr_attend_shared_size(const asr_attention* a, size_t* bytes);
+asr_status asr_attend_shared(const asr_attention* a, void* ws, size_t ws_bytes, void* stream);
+
+/* Rules on the logits of a step, and the k best tokens under them.  Row r
+ * follows rule set s = set[r] (set NULL: s = r; outside [0, sets): no rules).
+ * For every token v, in float32, each operation rounded by itself:
+ *   l = logits[r][v];
+ *   v in the history of s:               l = l > 0 ? l / repetition : l * repetition;
+ *   c > 0 times in it behind the prompt: l = (l - frequency * c) - presence;
+ *   l = l + (sum of v's biases in list order);
+ *   v not allowed by the mask:           l = -inf, whatever it was;
+ *   z = l / temperature  (a temperature that is not above 0 counts as 1).
+ * History of s: history[s * history_ld + j], j < history_len[s], of which the
+ * first prompt_len[s] (NULL: 0) are the prompt; biases alike; tokens outside
+ * [0, vocab) are passed over, lengths are cut to the row.  mask: bit v % 32 of
+ * word v / 32 of row mask_of[s] (NULL: s) set = allowed; a row outside
+ * [0, masks) allows every token.  NULL lists, masks and parameters do nothing.
+ *   out (may be NULL): z, float32; it may be the logits themselves (float32,
+ * out_ld = ld).  k in [0, 16] best tokens per row, larger z first, the lower
+ * token of equal ones, a NaN before everything: token and logprob [rows][k],
+ * logprob = z - log sum_v e^z.  A token with z = -inf is never given: where the
+ * others run out, token = -1 and logprob = -inf (a row whose mask allows
+ * nothing has only these).
+ *   vocab at most 1048576, rows at most 65535. */
+typedef struct {
+  int32_t dtype;       /* asr_dtype of the logits */
+  int32_t rows, vocab, sets, masks, k;
+  const void* logits;
+  int64_t ld;
+  const int32_t* set;                 /* [rows] or NULL */
+  const int32_t* history;             /* [sets][history_ld] */
+  int64_t history_ld;
+  const int32_t* history_len;         /* [sets] */
+  const int32_t* prompt_len;          /* [sets] or NULL */
+  const float* repetition;            /* [sets] or NULL, each */
+  const float* frequency;
+  const float* presence;
+  const int32_t* bias_token;          /* [sets][bias_ld] */
+  const float* bias_value;
+  int64_t bias_ld;
+  const int32_t* bias_len;            /* [sets] */
+  const uint32_t* mask;               /* [masks][mask_ld] words */
+  int64_t mask_ld;
+  const int32_t* mask_of;             /* [sets] or NULL */
+  const float* temperature;           /* [sets] or NULL */
+  float* out;
+  int64_t out_ld;
+  int32_t* token;                     /* [rows][k] */
+  float* logprob;                     /* [rows][k] */
+} asr_rules;
+asr_status asr_logit_rules_size(const asr_rules* r, size_t* bytes);
+asr_status asr_logit_rules(const asr_rules* r, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

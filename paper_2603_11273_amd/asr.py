@@ -36,6 +36,7 @@ EXPORTED = [
     "asr_debug_set_self_kv", "asr_logmel_noalloc", "asr_serve_config", "asr_serve_step",
     "asr_serve_plan",
     "asr_serve_tokens", "asr_serve_simulate", "asr_serve_stats",
+    "asr_attend_shared_size", "asr_attend_shared", "asr_logit_rules_size", "asr_logit_rules",
 ]
 
 
@@ -75,6 +76,33 @@ class ServeOut(C.Structure):
 
 class SimCost(C.Structure):
     _fields_ = [("prefill_us", C.c_int64), ("step_us", C.c_int64), ("row_us", C.c_int64)]
+
+
+class Keys(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("slot_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("pos_stride", C.c_int64), ("slots", C.c_int32),
+                ("positions", C.c_int32), ("slot", C.c_void_p), ("first", C.c_void_p),
+                ("len", C.c_void_p)]
+
+
+class Attention(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in (
+        "dtype", "n_head", "n_kv_head", "rows", "groups", "max_group", "max_prefix", "max_own",
+        "part_keys")] + [
+        ("scale", C.c_float), ("q", C.c_void_p), ("q_ld", C.c_int64), ("out", C.c_void_p),
+        ("out_ld", C.c_int64), ("group_start", C.c_void_p), ("row_of", C.c_void_p),
+        ("prefix", Keys), ("own", Keys)]
+
+
+class Rules(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "rows", "vocab", "sets", "masks", "k")] + [
+        ("logits", C.c_void_p), ("ld", C.c_int64), ("set", C.c_void_p), ("history", C.c_void_p),
+        ("history_ld", C.c_int64), ("history_len", C.c_void_p), ("prompt_len", C.c_void_p),
+        ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p),
+        ("bias_token", C.c_void_p), ("bias_value", C.c_void_p), ("bias_ld", C.c_int64),
+        ("bias_len", C.c_void_p), ("mask", C.c_void_p), ("mask_ld", C.c_int64),
+        ("mask_of", C.c_void_p), ("temperature", C.c_void_p), ("out", C.c_void_p),
+        ("out_ld", C.c_int64), ("token", C.c_void_p), ("logprob", C.c_void_p)]
 
 
 class AsrError(RuntimeError):
@@ -133,6 +161,10 @@ def _load():
         "asr_serve_stats": [vp, P(i64)],
         "asr_serve_simulate": [vp, P(SimCost), i64, i32, P(i64), P(i64), P(i64), P(i32),
                                P(i32), P(i64), i64, P(i64)],
+        "asr_attend_shared_size": [P(Attention), P(C.c_size_t)],
+        "asr_attend_shared": [P(Attention), vp, C.c_size_t, vp],
+        "asr_logit_rules_size": [P(Rules), P(C.c_size_t)],
+        "asr_logit_rules": [P(Rules), vp, C.c_size_t, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -186,6 +218,163 @@ def logmel_noalloc(clips, n_mels, out, stream=None):
     st = (stream or torch.cuda.current_stream()).cuda_stream
     _check(lib.asr_logmel_noalloc(ptrs, ns.ctypes.data_as(C.POINTER(C.c_int64)), n, n_mels,
                                   _ptr(out), st))
+
+
+class _Operator:
+    """What the plans of the stateless operators share: the tensors they keep, their scratch and
+    the call.  Tensors are taken as they lie (no copies) and must stay where they are; what is in
+    them may change between calls."""
+
+    def __init__(self, device, workspace, size, run, args):
+        self._dev, self._run, self._args = device, run, args
+        self._ref = C.byref(args)
+        n = C.c_size_t()
+        _check(size(self._ref, C.byref(n)))
+        self.workspace_bytes = n.value
+        self._ws = workspace
+        if workspace is None:
+            import torch
+            self._ws = torch.empty(max(n.value, 1), dtype=torch.uint8, device=device)
+        self._ws_ptr, self._ws_bytes = self._ws.data_ptr(), self._ws.numel()
+
+    def _need(self, t, name, dtype, shape, device, ld=False):
+        """A tensor's checks (contiguous; with ld, rows that are); its address."""
+        if t is None:
+            return None
+        if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+            raise TypeError(f"{name} must be {dtype} of shape {tuple(shape)} on {device}")
+        if not (t.is_contiguous() or (ld and t.stride(-1) == 1)):
+            raise TypeError(f"{name} must be contiguous")
+        return t.data_ptr()
+
+    def _launch(self, stream):
+        import torch
+        if torch.cuda.current_device() == self._dev.index:
+            st = stream or torch.cuda.current_stream(self._dev)
+            _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st.cuda_stream))
+            return
+        with torch.cuda.device(self._dev):
+            st = stream or torch.cuda.current_stream(self._dev)
+            _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st.cuda_stream))
+
+
+class SharedAttention(_Operator):
+    """asr_attend_shared as a plan: caches, groups and lengths once, then plan(q, out) per step.
+
+    prefix_k, prefix_v, own_k, own_v: [slots][kv heads][positions][64] views of a cache (float32
+    or bfloat16, the dims of a head contiguous, k and v with the same strides).  Group g holds rows
+    row_of[group_start[g] : group_start[g + 1]] (row_of None: the rows themselves), at most
+    max_group of them.  The int32 device tensors group_start [groups + 1], row_of [rows],
+    prefix_slot / prefix_first / prefix_len [groups] and own_slot / own_first / own_len [rows] are
+    read at every call.  max_prefix, max_own bound the lengths (default: the positions).
+    plan(q, out): q float32 [rows][n_head * 64], out [rows][n_head * 64] in the cache's type, on
+    `stream` (default: torch's current stream).  Plans whose calls may overlap need a
+    workspace each (default: one of the plan's own)."""
+
+    def __init__(self, prefix_k=None, prefix_v=None, own_k=None, own_v=None, *, n_head, rows,
+                 groups, max_group, group_start, row_of=None, prefix_slot=None, prefix_first=None,
+                 prefix_len=None, max_prefix=None, own_slot=None, own_first=None, own_len=None,
+                 max_own=None, scale=0.125, part_keys=0, workspace=None):
+        import torch
+        some = prefix_k if prefix_k is not None else own_k
+        if some is None or some.dtype not in (torch.float32, torch.bfloat16) or not some.is_cuda:
+            raise TypeError("caches must be float32 or bfloat16 device tensors")
+        dev, i32 = some.device, torch.int32
+        self._dtype = some.dtype
+
+        def keys(k, v, slot, first, length, entries, name):
+            if k is None:
+                return Keys()
+            if v is None or k.dim() != 4 or k.shape != v.shape or k.shape[3] != 64 or k.shape[1] != some.shape[1]:
+                raise TypeError(f"{name}: k and v must be [slots][kv heads][positions][64]")
+            if any(t.device != dev or t.dtype != some.dtype for t in (k, v)):
+                raise TypeError(f"{name}: k and v must be {some.dtype} on {dev}")
+            if k.stride() != v.stride() or k.stride(3) != 1:
+                raise TypeError(f"{name}: k and v must have the same strides, dims contiguous")
+            idx = [self._need(t, f"{name}_{n}", i32, (entries,), dev)
+                   for t, n in ((slot, "slot"), (first, "first"), (length, "len"))]
+            return Keys(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                        k.shape[0], k.shape[2], *idx)
+
+        self._keep = (prefix_k, prefix_v, own_k, own_v, group_start, row_of, prefix_slot,
+                      prefix_first, prefix_len, own_slot, own_first, own_len)
+        most = [0 if k is None else k.shape[2] if m is None else m
+                for k, m in ((prefix_k, max_prefix), (own_k, max_own))]
+        args = Attention(
+            BF16 if some.dtype == torch.bfloat16 else F32, n_head, some.shape[1], rows, groups,
+            max_group, most[0], most[1], part_keys, scale, None, 0, None, 0,
+            self._need(group_start, "group_start", i32, (groups + 1,), dev),
+            self._need(row_of, "row_of", i32, (rows,), dev),
+            keys(prefix_k, prefix_v, prefix_slot, prefix_first, prefix_len, groups, "prefix"),
+            keys(own_k, own_v, own_slot, own_first, own_len, rows, "own"))
+        self._shape = (rows, n_head * 64)
+        super().__init__(dev, workspace, lib.asr_attend_shared_size, lib.asr_attend_shared, args)
+
+    def __call__(self, q, out, stream=None):
+        import torch
+        a = self._args
+        a.q = self._need(q, "q", torch.float32, self._shape, self._dev, ld=True)
+        a.out = self._need(out, "out", self._dtype, self._shape, self._dev, ld=True)
+        a.q_ld, a.out_ld = q.stride(0), out.stride(0)
+        self._launch(stream)
+        return out
+
+
+class LogitRules(_Operator):
+    """asr_logit_rules as a plan: rule sets once, then plan(logits, ...) per step.
+
+    Row r follows rule set set[r] (None: r).  Device tensors, read at every call: set int32 [rows];
+    history int32 [sets][n] with history_len and prompt_len int32 [sets]; repetition, frequency,
+    presence, temperature float32 [sets]; bias_token int32 and bias_value float32 [sets][n] with
+    bias_len int32 [sets]; mask int32 [masks][words] (bit v % 32 of word v / 32 set = allowed) with
+    mask_of int32 [sets].  plan(logits, out, token, logprob): logits [rows][vocab] of `dtype`
+    (float32 or bfloat16), out float32 [rows][vocab] or None (may be the logits themselves), token
+    int32 and logprob float32 [rows][k]."""
+
+    def __init__(self, rows, vocab, dtype, *, k=0, sets=None, set=None, history=None,
+                 history_len=None, prompt_len=None, repetition=None, frequency=None,
+                 presence=None, bias_token=None, bias_value=None, bias_len=None, mask=None,
+                 mask_of=None, temperature=None, device=None, workspace=None):
+        import torch
+        i32, f32 = torch.int32, torch.float32
+        if dtype not in (f32, torch.bfloat16):
+            raise TypeError("logits must be float32 or bfloat16")
+        given = [t for t in (set, history, repetition, frequency, presence, bias_token, mask,
+                             temperature) if t is not None]
+        dev = torch.device(device if device is not None else
+                           given[0].device if given else torch.cuda.current_device())
+        if dev.index is None:
+            dev = torch.device(dev.type, torch.cuda.current_device())
+        n = rows if sets is None else sets
+        need = self._need
+        self._keep = (set, history, history_len, prompt_len, repetition, frequency, presence,
+                      bias_token, bias_value, bias_len, mask, mask_of, temperature)
+        hist_n = 0 if history is None else history.shape[-1]
+        bias_n = 0 if bias_token is None else bias_token.shape[-1]
+        masks, words = (0, 0) if mask is None else mask.shape
+        one = lambda t, name, kind: need(t, name, kind, (n,), dev)  # noqa: E731
+        args = Rules(
+            BF16 if dtype == torch.bfloat16 else F32, rows, vocab, n, masks, k, None, 0,
+            need(set, "set", i32, (rows,), dev), need(history, "history", i32, (n, hist_n), dev),
+            hist_n, one(history_len, "history_len", i32), one(prompt_len, "prompt_len", i32),
+            one(repetition, "repetition", f32), one(frequency, "frequency", f32),
+            one(presence, "presence", f32), need(bias_token, "bias_token", i32, (n, bias_n), dev),
+            need(bias_value, "bias_value", f32, (n, bias_n), dev), bias_n,
+            one(bias_len, "bias_len", i32), need(mask, "mask", i32, (masks, words), dev), words,
+            one(mask_of, "mask_of", i32), one(temperature, "temperature", f32), None, 0, None, None)
+        self._dtype, self._shape, self._best = dtype, (rows, vocab), (rows, k)
+        super().__init__(dev, workspace, lib.asr_logit_rules_size, lib.asr_logit_rules, args)
+
+    def __call__(self, logits, out=None, token=None, logprob=None, stream=None):
+        import torch
+        a = self._args
+        a.logits = self._need(logits, "logits", self._dtype, self._shape, self._dev, ld=True)
+        a.ld = logits.stride(0)
+        a.out = self._need(out, "out", torch.float32, self._shape, self._dev, ld=True)
+        a.out_ld = 0 if out is None else out.stride(0)
+        a.token = self._need(token, "token", torch.int32, self._best, self._dev)
+        a.logprob = self._need(logprob, "logprob", torch.float32, self._best, self._dev)
+        self._launch(stream)
 
 
 def model_cfg(shape, max_slots=8, max_prefill=1, max_decode=8, max_queue=4096) -> ModelCfg:

@@ -166,6 +166,62 @@ template <typename T>
 void embed(const T* tok_emb, const float* pos_emb, const int32_t* tokens, const int32_t* pos,
            int D, int d, float* h, hipStream_t s);
 
+// Decode attention of rows that share keys (asr_attend_shared): the shared keys
+// of a group and each row's own, in parts of at most prefix_part and own_part
+// keys; np and no parts at most (np + no > 1: a record of each in `rec`,
+// 66 floats per row, head and part).
+struct ShareKeys {
+  const void *k, *v;
+  int64_t slot_stride, head_stride, pos_stride;   // elements
+  const int32_t *slot, *first, *len;              // per group or row, or NULL
+  int32_t slots, positions, most;
+};
+struct ShareLaunch {
+  const float* q;
+  int64_t q_ld;
+  void* out;
+  int64_t out_ld;
+  float qmul;                                     // scale * log2(e)
+  const int32_t *group_start, *row_of;
+  int32_t rows, groups, max_group, n_head, n_kv;
+  ShareKeys prefix, own;
+  int32_t np, no, prefix_part, own_part;
+  float* rec;
+};
+hipError_t attend_shared(const ShareLaunch& a, bool bf16, hipStream_t s);
+// 16-column query tiles that a block holds, of `cols` queries of a group and cache head
+int share_query_tiles(int cols);
+
+// Rules on logits and the k best tokens (asr_logit_rules).
+constexpr int kRulesChunk = 4096, kRulesMaxK = 16, kRulesMaxVocab = 1 << 20;
+struct RulesLaunch {
+  const void* logits;
+  int64_t ld;
+  int32_t rows, vocab, sets;
+  const int32_t* set;
+  const int32_t* history;
+  int64_t history_ld;
+  const int32_t *history_len, *prompt_len;
+  const float *repetition, *frequency, *presence;
+  const int32_t* bias_token;
+  const float* bias_value;
+  int64_t bias_ld;
+  const int32_t* bias_len;
+  const uint32_t* mask;
+  int64_t mask_ld;
+  int32_t masks;
+  const int32_t* mask_of;
+  const float* temperature;
+  float* out;
+  int64_t out_ld;
+  int32_t k;
+  int32_t* token;
+  float* logprob;
+  float* ws;                                      // rules_ws_bytes
+};
+size_t rules_ws_bytes(int rows, int vocab, int k);
+void logit_rules(const RulesLaunch& a, bool bf16, hipStream_t s);
+
 // Log-mel front-end.  pcm_ptrs[i] is a device pointer to clip i's samples.
 struct MelTables {
   const float* window;     // [400] periodic Hann

@@ -12,19 +12,22 @@
 
 #include "../../include/asr.h"
 #include "asr_kernels.h"
+#include "errors.h"
 #include "queue.h"
 #include "serve.h"
 
 using namespace asr;
 
 namespace {
-
 thread_local std::string g_err;
+}  // namespace
 
-asr_status fail(asr_status s, const std::string& msg) {
+asr_status asr::fail(asr_status s, const std::string& msg) {
   g_err = msg;
   return s;
 }
+
+namespace {
 
 #define HIPCHK(x)                                                                   \
   do {                                                                              \
