@@ -250,4 +250,21 @@ __device__ __forceinline__ float from_ordered_u32(uint32_t k) {
   return __uint_as_float(u);
 }
 
+// Maximum over the wave, without LDS round trips.
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#define ASR_DPP_MAX(ctrl) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, (ctrl), 0xF, 0xF, true))
+  ASR_DPP_MAX(0xB1);
+  ASR_DPP_MAX(0x4E);
+  ASR_DPP_MAX(0x141);
+  ASR_DPP_MAX(0x140);
+#undef ASR_DPP_MAX
+  const auto p16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(p16[0], p16[1]);
+  const auto p32 = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(p32[0], p32[1]);
+}
+__device__ __forceinline__ float wave_max_lanes(float v) {
+  return from_ordered_u32(wave_max_u32(ordered_u32(v)));
+}
+
 }  // namespace asr

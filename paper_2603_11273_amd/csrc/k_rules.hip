@@ -59,22 +59,6 @@ __device__ __forceinline__ uint32_t rank_of(float z) {
   return z == -INFINITY ? 0u : ordered_u32(z + 0.f);
 }
 
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#define ASR_DPP_MAX(ctrl) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, (ctrl), 0xF, 0xF, true))
-  ASR_DPP_MAX(0xB1);
-  ASR_DPP_MAX(0x4E);
-  ASR_DPP_MAX(0x141);
-  ASR_DPP_MAX(0x140);
-#undef ASR_DPP_MAX
-  const auto p16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = max(p16[0], p16[1]);
-  const auto p32 = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return max(p32[0], p32[1]);
-}
-__device__ __forceinline__ float wave_max_lanes(float v) {
-  // (as the maximum of ordered integers; -inf where there is nothing)
-  return from_ordered_u32(wave_max_u32(ordered_u32(v)));
-}
 // The largest of the lanes' (rank, token) pairs; its lane, or -1 where all ranks are 0.
 __device__ __forceinline__ int best_lane(uint32_t rank, int token) {
   const uint32_t top = wave_max_u32(rank);

@@ -31,10 +31,22 @@ constexpr int SH_NW = 4;                 // waves of a block
 constexpr int SH_OLD = 68;               // floats a query's row takes in LDS: 16 lanes, 64 banks
 constexpr float kRaise = 8.f;            // the reference follows the maximum from 2^8 on
 
+// Loads of keys and values pass the caches as data that is read once: 8 x 16
+// rows on 65536 shared keys 515 -> 486 us, 24 x 5 on 1500 54 -> 49.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <typename V>
+__device__ __forceinline__ V load16(const char* p) {
+  return __builtin_bit_cast(V, __builtin_nontemporal_load((const u32x4*)p));
+}
+__device__ __forceinline__ uint2 load8(const char* p) {
+  return __builtin_bit_cast(uint2, __builtin_nontemporal_load((const u32x2*)p));
+}
+
 struct ShareArgs {
   ShareLaunch c;
   int per, tiles, own_tiles;
-  int64_t prefix_blocks;
+  uint32_t prefix_units, prefix_blocks;
 };
 
 // The keys of one tile in a lane's registers, and the two products with them.
@@ -73,17 +85,19 @@ struct KeyTile<bf16_t> {
   };
   // keys of the lane's scores: first + i
   static __device__ __forceinline__ int first_key(int g) { return 8 * g; }
-  // tile at key t0 of n (past the end: the last key again, masked later)
-  __device__ __forceinline__ void load(const char* kb, const char* vb, uint32_t pos_bytes, int t0, int n, int m, int g) {
+  // tile at kb, vb, of which n keys are left (past the end: the last key again, masked later)
+  __device__ __forceinline__ void load_keys(const char* kb, uint32_t pos_bytes, int n, int m, int g) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t off = (uint32_t)min(t0 + (m >> 2) * 8 + (m & 3) + 4 * h, n - 1) * pos_bytes + 16 * g;
-      k[h][0] = *(const uint4*)(kb + off);
-      k[h][1] = *(const uint4*)(kb + off + 64);
+      const uint32_t off = (uint32_t)min((m >> 2) * 8 + (m & 3) + 4 * h, n - 1) * pos_bytes + 16 * g;
+      k[h][0] = load16<uint4>(kb + off);
+      k[h][1] = load16<uint4>(kb + off + 64);
     }
+  }
+  __device__ __forceinline__ void load_values(const char* vb, uint32_t pos_bytes, int n, int m, int g) {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      v[j] = *(const uint2*)(vb + (uint32_t)min(t0 + 8 * g + j, n - 1) * pos_bytes + 8 * m);
+      v[j] = load8(vb + (uint32_t)min(8 * g + j, n - 1) * pos_bytes + 8 * m);
   }
   __device__ __forceinline__ void drop_values(int key0, int n) {
 #pragma unroll
@@ -149,7 +163,7 @@ struct KeyTile<float> {
     __device__ __forceinline__ void set(const float* p, int g, float mul) {
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const float4 a = *(const float4*)(p + 16 * g + 4 * s);
+        const float4 a = *(const float4*)(p + 16 * s + 4 * g);
         x[4 * s] = a.x * mul;
         x[4 * s + 1] = a.y * mul;
         x[4 * s + 2] = a.z * mul;
@@ -162,13 +176,16 @@ struct KeyTile<float> {
     }
   };
   static __device__ __forceinline__ int first_key(int g) { return 4 * g; }
-  __device__ __forceinline__ void load(const char* kb, const char* vb, uint32_t pos_bytes, int t0, int n, int m, int g) {
-    const uint32_t off = (uint32_t)min(t0 + m, n - 1) * pos_bytes + 64 * g;
+  __device__ __forceinline__ void load_keys(const char* kb, uint32_t pos_bytes, int n, int m, int g) {
+    // (four lanes read 64 bytes of a key at once; the query's dims lie alike)
+    const uint32_t off = (uint32_t)min(m, n - 1) * pos_bytes + 16 * g;
 #pragma unroll
-    for (int s = 0; s < 4; ++s) k[s] = *(const float4*)(kb + off + 16 * s);
+    for (int s = 0; s < 4; ++s) k[s] = load16<float4>(kb + off + 64 * s);
+  }
+  __device__ __forceinline__ void load_values(const char* vb, uint32_t pos_bytes, int n, int m, int g) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      v[j] = *(const float4*)(vb + (uint32_t)min(t0 + 4 * g + j, n - 1) * pos_bytes + 16 * m);
+      v[j] = load16<float4>(vb + (uint32_t)min(4 * g + j, n - 1) * pos_bytes + 16 * m);
   }
   __device__ __forceinline__ void drop_values(int key0, int n) {
 #pragma unroll
@@ -252,8 +269,14 @@ __device__ __forceinline__ void attend_part(const ShareArgs& a, const ShareKeys&
   const char *kb = (const char*)((const T*)c.k + at), *vb = (const char*)((const T*)c.v + at);
   const uint32_t pos_bytes = (uint32_t)c.pos_stride * sizeof(T);
   constexpr int STEP = SH_NW * Tile::KEYS;
-  Tile buf[2];
-  if (wave * Tile::KEYS < n) buf[0].load(kb, vb, pos_bytes, wave * Tile::KEYS, n, m, g);
+  const int64_t step_bytes = (int64_t)STEP * pos_bytes;
+  kb += (int64_t)(wave * Tile::KEYS) * pos_bytes;
+  vb += (int64_t)(wave * Tile::KEYS) * pos_bytes;
+  Tile tile;
+  if (wave * Tile::KEYS < n) {
+    tile.load_keys(kb, pos_bytes, n - wave * Tile::KEYS, m, g);
+    tile.load_values(vb, pos_bytes, n - wave * Tile::KEYS, m, g);
+  }
 
   typename Tile::Query q[QT];
 #pragma unroll
@@ -276,24 +299,32 @@ __device__ __forceinline__ void attend_part(const ShareArgs& a, const ShareKeys&
     for (int i = 0; i < 4; ++i) o[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  auto compute = [&](Tile& tile, int t0) {
+  // The next tile's keys are under way as soon as this one's have given their
+  // scores, its values as soon as this one's are fragments: one set of registers
+  // each, hence more waves, and the loads never stop.
+  for (int t0 = wave * Tile::KEYS; t0 < n; t0 += STEP) {
     const int key0 = t0 + Tile::first_key(g);
-    const bool tail = t0 + Tile::KEYS > n;             // wave-uniform
+    const bool tail = t0 + Tile::KEYS > n, more = t0 + STEP < n;   // wave-uniform
+    float s[QT][Tile::NS];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) tile.scores(q[t], s[t]);
+    kb += step_bytes;
+    vb += step_bytes;
+    if (more) tile.load_keys(kb, pos_bytes, n - t0 - STEP, m, g);
     if (tail) tile.drop_values(key0, n);
     typename Tile::Frag f[4];
     tile.fragments(f);
+    if (more) tile.load_values(vb, pos_bytes, n - t0 - STEP, m, g);
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      float s[Tile::NS];
-      tile.scores(q[t], s);
       if (tail) {
 #pragma unroll
         for (int i = 0; i < Tile::NS; ++i)
-          if (key0 + i >= n) s[i] = -INFINITY;
+          if (key0 + i >= n) s[t][i] = -INFINITY;
       }
-      float top = s[0];
+      float top = s[t][0];
 #pragma unroll
-      for (int i = 1; i < Tile::NS; ++i) top = fmaxf(top, s[i]);
+      for (int i = 1; i < Tile::NS; ++i) top = fmaxf(top, s[t][i]);
       // the reference of the exponents is a query's own matter: another query
       // of the tile that raises its own leaves this one's factor at exactly 1
       if (__any(top > mx[t] + kRaise)) {
@@ -309,18 +340,10 @@ __device__ __forceinline__ void attend_part(const ShareArgs& a, const ShareKeys&
       float p[Tile::NS];
 #pragma unroll
       for (int i = 0; i < Tile::NS; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(s[i] - ref);
+        p[i] = __builtin_amdgcn_exp2f(s[t][i] - ref);
         l[t] += p[i];
       }
       Tile::accumulate(f, p, o[t]);
-    }
-  };
-  for (int t0 = wave * Tile::KEYS; t0 < n; t0 += 2 * STEP) {
-    if (t0 + STEP < n) buf[1].load(kb, vb, pos_bytes, t0 + STEP, n, m, g);
-    compute(buf[0], t0);
-    if (t0 + STEP < n) {
-      if (t0 + 2 * STEP < n) buf[0].load(kb, vb, pos_bytes, t0 + 2 * STEP, n, m, g);
-      compute(buf[1], t0 + STEP);
     }
   }
 
@@ -381,33 +404,34 @@ __device__ __forceinline__ void attend_part(const ShareArgs& a, const ShareKeys&
 // to the XCDs in turn, so the query tiles of one part lie 8 blocks apart: they
 // read the same keys through one L2.
 template <typename T, int QT>
-__global__ __launch_bounds__(SH_NW * 64) void k_attend_shared(ShareArgs a) {
+__global__ __launch_bounds__(SH_NW * 64) __attribute__((amdgpu_waves_per_eu(QT == 1 ? 4 : QT == 2 ? 3 : 2)))   // share_blocks_per_cu
+void k_attend_shared(ShareArgs a) {
   extern __shared__ __attribute__((aligned(16))) float share_lds[];
-  int64_t b = blockIdx.x;
-  if (b < a.prefix_blocks) {
-    const int tile = (int)((b >> 3) % a.tiles);
-    int64_t u = (b >> 3) / a.tiles * 8 + (b & 7);
-    if (u >= (int64_t)a.c.groups * a.c.np * a.c.n_kv) return;
+  uint32_t u = blockIdx.x;
+  if (u < a.prefix_blocks) {
+    const int tile = (int)((u >> 3) % a.tiles);
+    u = (u >> 3) / a.tiles * 8 + (u & 7);
+    if (u >= a.prefix_units) return;
     const int head = (int)(u % a.c.n_kv);
     u /= a.c.n_kv;
     const int part = (int)(u % a.c.np), grp = (int)(u / a.c.np);
-    const int start = a.c.group_start[grp];
-    const int count = min(min(a.c.group_start[grp + 1], a.c.rows) - start, a.c.max_group);
-    if (start < 0 || tile * 16 * QT >= count * a.per) return;
+    // (all of the block's numbers in one go: memory answers late once it is busy)
     const Range r = key_range(a.c.prefix, grp);
+    const int start = a.c.group_start[grp], end = a.c.group_start[grp + 1];
+    const int count = min(min(end, a.c.rows) - start, a.c.max_group);
+    if (start < 0 || tile * 16 * QT >= count * a.per) return;
     const int k0 = part * a.c.prefix_part, k1 = min(k0 + a.c.prefix_part, r.n);
     if (k0 >= k1 && a.c.np + a.c.no > 1) return;
     attend_part<T, QT>(a, a.c.prefix, r, min(k0, k1), k1, head, start, count, tile * 16 * QT, part, share_lds);
   } else {
-    b -= a.prefix_blocks;
-    const int head = (int)(b % a.c.n_kv);
-    b /= a.c.n_kv;
-    const int tile = (int)(b % a.own_tiles);
-    b /= a.own_tiles;
-    const int part = (int)(b % a.c.no), i = (int)(b / a.c.no);
-    if (i < a.c.group_start[0] || i >= a.c.group_start[a.c.groups]) return;
-    const int row = a.c.row_of ? a.c.row_of[i] : i;
-    if (row < 0 || row >= a.c.rows) return;
+    u -= a.prefix_blocks;
+    const int head = (int)(u % a.c.n_kv);
+    u /= a.c.n_kv;
+    const int tile = (int)(u % a.own_tiles);
+    u /= a.own_tiles;
+    const int part = (int)(u % a.c.no), i = (int)(u / a.c.no);
+    const int row = a.c.row_of ? a.c.row_of[i] : i, first = a.c.group_start[0], end = a.c.group_start[a.c.groups];
+    if (i < first || i >= end || row < 0 || row >= a.c.rows) return;
     const Range r = key_range(a.c.own, row);
     const int k0 = part * a.c.own_part, k1 = min(k0 + a.c.own_part, r.n);
     if (k0 >= k1 && a.c.np + a.c.no > 1) return;
@@ -416,44 +440,54 @@ __global__ __launch_bounds__(SH_NW * 64) void k_attend_shared(ShareArgs a) {
 }
 
 // out of a row and head from its parts' records; one wave each, lane = dim.  A
-// row's group is the last one that starts at or before its place.
+// row's group is the last one that starts at or before its place.  The kernel is
+// a chain of loads, so the records are loaded before it is known which of them
+// there are (those that no block wrote count as nothing), SH_JOIN at a time.
+constexpr int SH_JOIN = 16;
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_join(ShareArgs a) {
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const uint32_t w = blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (w >= (int64_t)a.c.rows * a.c.n_head) return;
+  if (w >= (uint32_t)a.c.rows * a.c.n_head) return;
   const int i = (int)(w / a.c.n_head), h = (int)(w % a.c.n_head);
+  const int parts = a.c.np + a.c.no;
+  const float* val = a.c.rec + (int64_t)w * parts * kHeadDim + lane;
+  const float2* ml = (const float2*)(a.c.rec + (int64_t)a.c.rows * a.c.n_head * parts * kHeadDim) + (int64_t)w * parts;
+  float v[SH_JOIN];
+  float2 rec = {-INFINITY, 0.f};
+  auto load = [&](int p0) {
+    rec = p0 + lane < parts && lane < SH_JOIN ? ml[p0 + lane] : float2{-INFINITY, 0.f};
+#pragma unroll
+    for (int p = 0; p < SH_JOIN; ++p) v[p] = p0 + p < parts ? val[(int64_t)(p0 + p) * kHeadDim] : 0.f;
+  };
+  load(0);
+  const int row = a.c.row_of ? a.c.row_of[i] : i;
   int grp = -1;
   for (int g0 = 0; g0 < a.c.groups; g0 += 64)
     grp += __popcll(__ballot(g0 + lane < a.c.groups && a.c.group_start[min(g0 + lane, a.c.groups - 1)] <= i));
   if (grp < 0 || i >= a.c.group_start[a.c.groups] || i - a.c.group_start[grp] >= a.c.max_group) return;
-  const int row = a.c.row_of ? a.c.row_of[i] : i;
   if (row < 0 || row >= a.c.rows) return;
   const int np = a.c.np > 0 ? (key_range(a.c.prefix, grp).n + a.c.prefix_part - 1) / a.c.prefix_part : 0;
   const int no = a.c.no > 0 ? (key_range(a.c.own, row).n + a.c.own_part - 1) / a.c.own_part : 0;
-  const int parts = a.c.np + a.c.no, n = np + no;
-  const float* val = a.c.rec + w * parts * kHeadDim + lane;
-  const float2* ml = (const float2*)(a.c.rec + (int64_t)a.c.rows * a.c.n_head * parts * kHeadDim) + w * parts;
-  auto slot_of = [&](int p) { return p < np ? p : a.c.np + p - np; };
-  float M = -INFINITY;
-  for (int p0 = 0; p0 < n; p0 += 64)
-    if (p0 + lane < n) M = fmaxf(M, ml[slot_of(p0 + lane)].x);
-  M = wave_max(M);
-  float L = 0.f, acc = 0.f;
-  for (int p0 = 0; p0 < n; p0 += 64) {
-    float fac = 0.f, lw = 0.f;
-    if (p0 + lane < n) {
-      const float2 x = ml[slot_of(p0 + lane)];
-      fac = x.x == M ? 1.f : __builtin_amdgcn_exp2f(x.x - M);
-      lw = fac * x.y;
-    }
-    L += wave_sum_lanes(lw);
-    const int here = min(64, n - p0);
-#pragma unroll 4
-    for (int p = 0; p < here; ++p)
-      acc += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fac), p)) * val[(int64_t)slot_of(p0 + p) * kHeadDim];
+  float M = -INFINITY, L = 0.f, acc = 0.f;
+  for (int p0 = 0; p0 < parts; p0 += SH_JOIN) {
+    const int p = p0 + lane;
+    const bool there = lane < SH_JOIN && (p < a.c.np ? p < np : p - a.c.np < no);
+    const uint64_t some = __ballot(there);
+    if (!some) continue;
+    if (p0 > 0) load(p0);
+    const float m = there ? rec.x : -INFINITY;
+    const float top = fmaxf(M, wave_max_lanes(m));
+    const float keep = M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
+    const float fac = !there ? 0.f : m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+    M = top;
+    L = L * keep + wave_sum_lanes(there ? fac * rec.y : 0.f);
+    acc *= keep;
+#pragma unroll
+    for (int j = 0; j < SH_JOIN; ++j)
+      if (some >> j & 1) acc += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fac), j)) * v[j];
   }
-  St<T>::st((T*)a.c.out, (int64_t)row * a.c.out_ld + h * kHeadDim + lane, n > 0 ? acc / L : 0.f);
+  St<T>::st((T*)a.c.out, (int64_t)row * a.c.out_ld + h * kHeadDim + lane, np + no > 0 ? acc / L : 0.f);
 }
 
 template <typename T, int QT>
@@ -477,9 +511,9 @@ hipError_t attend(const ShareLaunch& c, hipStream_t s) {
   const int qt = share_query_tiles(cols);
   a.tiles = (cols + 16 * qt - 1) / (16 * qt);
   a.own_tiles = (a.per + 15) / 16;
-  const int64_t units = ((int64_t)c.groups * c.np * c.n_kv + 7) / 8 * 8;
-  a.prefix_blocks = units * a.tiles;
-  const int64_t blocks = a.prefix_blocks + (int64_t)c.rows * c.no * a.own_tiles * c.n_kv;
+  a.prefix_units = (uint32_t)((int64_t)c.groups * c.np * c.n_kv);
+  a.prefix_blocks = (a.prefix_units + 7) / 8 * 8 * a.tiles;
+  const int64_t blocks = a.prefix_blocks + (int64_t)c.rows * c.no * a.own_tiles * c.n_kv;   // (below 2^31: the caller)
   if (blocks > 0) {
     const hipError_t e = qt == 1 ? launch<T, 1>(a, blocks, s) : qt == 2 ? launch<T, 2>(a, blocks, s) : launch<T, 4>(a, blocks, s);
     if (e != hipSuccess) return e;
@@ -492,6 +526,7 @@ hipError_t attend(const ShareLaunch& c, hipStream_t s) {
 }  // namespace
 
 int share_query_tiles(int cols) { return cols <= 16 ? 1 : cols <= 32 ? 2 : 4; }
+int share_blocks_per_cu(int query_tiles) { return query_tiles == 1 ? 4 : query_tiles == 2 ? 3 : 2; }
 
 hipError_t attend_shared(const ShareLaunch& c, bool bf16, hipStream_t s) {
   return bf16 ? attend<bf16_t>(c, s) : attend<float>(c, s);

@@ -43,7 +43,7 @@ asr_status check_keys(const asr_keys& c, int32_t most, int es, const char* name)
   const int64_t unit = 16 / es;
   if (c.slot_stride < 0 || c.head_stride < 0 || c.slot_stride % unit || c.head_stride % unit || c.pos_stride % unit)
     return fail(ASR_EINVAL, n + ": strides must be multiples of 16 bytes");
-  // (a part of 8192 keys is addressed with 32 bits)
+  // (a tile of 32 keys is addressed with 32 bits)
   if (c.pos_stride < kHeadDim || c.pos_stride * es > 262144)
     return fail(ASR_EINVAL, n + ": pos_stride out of [64 elements, 262144 bytes]");
   return ASR_OK;
