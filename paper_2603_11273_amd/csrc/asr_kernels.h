@@ -191,8 +191,6 @@ struct ShareLaunch {
 hipError_t attend_shared(const ShareLaunch& a, bool bf16, hipStream_t s);
 // 16-column query tiles that a block holds, of `cols` queries of a group and cache head
 int share_query_tiles(int cols);
-// blocks that a CU holds with so many (registers)
-int share_blocks_per_cu(int query_tiles);
 
 // Rules on logits and the k best tokens (asr_logit_rules).
 constexpr int kRulesChunk = 4096, kRulesMaxK = 16, kRulesMaxVocab = 1 << 20;

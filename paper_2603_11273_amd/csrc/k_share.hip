@@ -404,7 +404,7 @@ __device__ __forceinline__ void attend_part(const ShareArgs& a, const ShareKeys&
 // to the XCDs in turn, so the query tiles of one part lie 8 blocks apart: they
 // read the same keys through one L2.
 template <typename T, int QT>
-__global__ __launch_bounds__(SH_NW * 64) __attribute__((amdgpu_waves_per_eu(QT == 1 ? 4 : QT == 2 ? 3 : 2)))   // share_blocks_per_cu
+__global__ __launch_bounds__(SH_NW * 64) __attribute__((amdgpu_waves_per_eu(QT == 1 ? 4 : QT == 2 ? 3 : 2)))
 void k_attend_shared(ShareArgs a) {
   extern __shared__ __attribute__((aligned(16))) float share_lds[];
   uint32_t u = blockIdx.x;
@@ -526,7 +526,6 @@ hipError_t attend(const ShareLaunch& c, hipStream_t s) {
 }  // namespace
 
 int share_query_tiles(int cols) { return cols <= 16 ? 1 : cols <= 32 ? 2 : 4; }
-int share_blocks_per_cu(int query_tiles) { return query_tiles == 1 ? 4 : query_tiles == 2 ? 3 : 2; }
 
 hipError_t attend_shared(const ShareLaunch& c, bool bf16, hipStream_t s) {
   return bf16 ? attend<bf16_t>(c, s) : attend<float>(c, s);

@@ -49,22 +49,47 @@ asr_status check_keys(const asr_keys& c, int32_t most, int es, const char* name)
   return ASR_OK;
 }
 
+int cu_count() {
+  static const int n = [] {
+    int dev = 0, v = 0;
+    if (hipGetDevice(&dev) != hipSuccess ||
+        hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v <= 0) {
+      (void)hipGetLastError();
+      v = 256;                                         // (sizes asked for without a GPU)
+    }
+    return v;
+  }();
+  return n;
+}
+
 ShareKeys keys_of(const asr_keys& c, int32_t most) {
   return {c.k, c.v, c.slot_stride, c.head_stride, c.pos_stride, c.slot, c.first, c.len, c.slots, c.positions, most};
 }
 
 int parts_of(int keys, int part) { return (int)(((int64_t)keys + part - 1) / part); }
 
-// Keys per part: enough blocks to keep every CU reading (see k_share.hip), no part below
-// 128 keys (one tile of each wave), and none so short that the records of its
-// queries (264 bytes each, written and read) come near the bytes of its keys.
-int part_keys(int64_t heads_and_entries, int keys, int cols) {
-  constexpr int64_t kBlocks = 2048;
-  const int64_t parts = std::max<int64_t>(1, kBlocks / std::max<int64_t>(1, heads_and_entries));
-  int64_t n = (keys + parts - 1) / parts;
-  n = std::max<int64_t>(n, 8 * std::min(cols, 64));
-  n = std::min<int64_t>((std::max<int64_t>(n, 1) + 127) / 128 * 128, 2048);
-  return (int)n;
+// Keys per part, `keys` at most for each of `units` (a group's queries and a cache
+// head, or a row and one).  One block per CU reads nearly as fast as several, so
+// with P parts a unit the work takes ceil(units P / CUs) turns of keys / P keys
+// and what a part costs besides (its first loads, its records), `fixed` keys'
+// worth; only the largest P of 1, 2, .. turns come into question.  Measured
+// (bf16, 20 heads, us): 8 groups of 16 rows on 65536 keys in parts of 2048 /
+// 4096 / 8192 / 16384 487 / 446 / 426 / 455, the rule's 8192; 64 rows on 30011
+// in 1024 / 1536 / 2560 / 4096 64 / 59 / 52 / 60, the rule's 2560; 24 x 5 on 1500
+// in 512 / 768 / 1536 51 / 50 / 49, the rule's one part.  Lengths that may differ
+// need more parts, as the longest unit would be last: 16 groups on 515 to 8191
+// keys in 768 / 1408 / 2048 / 4096 43 / 45 / 50 / 51, hence three turns at least.
+int part_keys(int64_t units, int64_t keys, bool ragged, int fixed, int step) {
+  if (keys <= step) return step;
+  const int64_t cus = cu_count();
+  int64_t best = step, best_cost = INT64_MAX;
+  for (int64_t turns = ragged ? 3 : 1; turns <= 8; ++turns) {
+    const int64_t p = std::max<int64_t>(1, cus * turns / units);
+    const int64_t n = ((keys + p - 1) / p + step - 1) / step * step;
+    const int64_t cost = (units * ((keys + n - 1) / n) + cus - 1) / cus * (n + fixed);
+    if (cost < best_cost) best = n, best_cost = cost;
+  }
+  return (int)best;
 }
 
 asr_status plan_attention(const asr_attention* a, ShareLaunch* s, size_t* bytes) {
@@ -98,14 +123,22 @@ asr_status plan_attention(const asr_attention* a, ShareLaunch* s, size_t* bytes)
   s->own = keys_of(a->own, a->max_own);
   const int64_t per = a->n_head / a->n_kv_head, cols = a->max_group * per;
   if (cols > INT32_MAX) return fail(ASR_EINVAL, "too many queries in a group");
-  s->prefix_part = a->part_keys ? a->part_keys : part_keys((int64_t)a->groups * a->n_kv_head, a->max_prefix, (int)std::min<int64_t>(cols, 64));
-  s->own_part = a->part_keys ? a->part_keys : part_keys((int64_t)a->rows * a->n_kv_head, a->max_own, (int)std::min<int64_t>(per, 64));
+  if (a->max_prefix > (1 << 30) || a->max_own > (1 << 30)) return fail(ASR_EINVAL, "more than 2^30 keys");
+  const int64_t tile = 16 * share_query_tiles((int)cols), tiles = (cols + tile - 1) / tile, own_tiles = (per + 15) / 16;
+  const int64_t units = (int64_t)a->groups * a->n_kv_head * tiles, own_units = (int64_t)a->rows * a->n_kv_head * own_tiles;
+  if (a->part_keys) {
+    s->prefix_part = s->own_part = a->part_keys;
+  } else {
+    // (float32: half as many keys in the same bytes, a tile of each wave in half as many)
+    const int step = 256 / es;
+    const auto fixed = [&](int64_t queries) { return (int)(200 + 10 * std::min<int64_t>(queries, 64)) * 2 / es; };
+    s->prefix_part = part_keys(std::max<int64_t>(units, 1), a->max_prefix, a->groups > 1 && a->prefix.len, fixed(cols), step);
+    s->own_part = part_keys(std::max<int64_t>(own_units, 1), a->max_own, a->rows > 1 && a->own.len, fixed(per), step);
+  }
   s->np = parts_of(a->max_prefix, s->prefix_part);
   s->no = parts_of(a->max_own, s->own_part);
-  const int64_t tile = 16 * share_query_tiles((int)cols), tiles = (cols + tile - 1) / tile;
-  const double blocks = ((double)a->groups * s->np * a->n_kv_head + 8) * tiles +
-                        (double)a->rows * s->no * a->n_kv_head * ((per + 15) / 16);
-  if (blocks > 2147483647.0 || (double)a->rows * a->n_head > 4e9) return fail(ASR_EINVAL, "too much work for one call");
+  const double blocks = ((double)units * s->np + 8.0 * tiles) + (double)own_units * s->no;
+  if (blocks > 2147483647.0 || (double)a->rows * a->n_head > 2e9) return fail(ASR_EINVAL, "too much work for one call");
   const int64_t parts = s->np + s->no;
   *bytes = parts > 1 ? (size_t)a->rows * a->n_head * parts * (kHeadDim + 2) * 4 : 0;
   return ASR_OK;
