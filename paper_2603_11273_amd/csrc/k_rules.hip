@@ -2,14 +2,15 @@
 // repeated tokens, biases, masks of allowed tokens and a temperature, and the
 // log-probabilities of the best tokens under what remains.
 //
-// One pass over the logits.  A block takes 4096 tokens of a row, 16 a thread, in
-// registers.  What is sparse -- the row's history, its biases -- is scattered into
-// an LDS table of the block's tokens (every block of a row reads the whole
-// lists, a few KB) and read back by the threads that own the tokens, so nothing
-// of the vocabulary's size is cleared, written or read besides the logits
-// themselves.  The block leaves its maximum, its sum of exponentials and its k
-// best tokens; a second, short kernel joins a row's blocks.  HBM bounds a batch
-// of rows, two launches a single one.
+// One pass over the logits.  256 threads take 4096 tokens of a row, 16 a thread,
+// in registers.  What is sparse -- the row's history, its biases -- is scattered
+// into an LDS table of the block's tokens (every block of a row reads the whole
+// lists) and read back by the threads that own the tokens, so nothing of the
+// vocabulary's size is cleared, written or read besides the logits themselves.
+// The 256 threads leave their maximum, their sum of exponentials and their k best
+// tokens; a second, short kernel joins a row's.  HBM bounds a batch of rows, two
+// launches a single one; long histories would be read once for 4096 tokens, so
+// with those a block is 1024 threads with the same work each.
 #include "asr_device.h"
 
 // Every operation below is rounded by itself, as the definition has it: two
@@ -21,6 +22,7 @@ namespace {
 
 constexpr int RU_NT = 256, RU_E = 16, RU_CHUNK = RU_NT * RU_E;
 static_assert(RU_CHUNK == kRulesChunk, "workspace");
+constexpr int kLongHistory = 4096;
 constexpr uint32_t kSeen = 0x80000000u;     // in the history; below it the count behind the prompt
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
@@ -71,17 +73,36 @@ __device__ __forceinline__ int best_lane(uint32_t rank, int token) {
   return __ffsll((unsigned long long)who) - 1;
 }
 
-template <typename T>
-__global__ __launch_bounds__(RU_NT) void k_rules(RulesLaunch a) {
-  constexpr int VEC = Logits<T>::VEC, NV = RU_E / VEC;
-  __shared__ __attribute__((aligned(16))) uint32_t count[RU_CHUNK];
-  __shared__ __attribute__((aligned(16))) float bias[RU_CHUNK];
-  __shared__ uint2 best[4][kRulesMaxK];
-  __shared__ float wave_ms[4][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int chunk = blockIdx.x, row = blockIdx.y, v0 = chunk * RU_CHUNK;
+// The better of two results comes first.
+__device__ __forceinline__ bool better(uint2 a, uint2 b) { return a.x > b.x || (a.x == b.x && a.y < b.y); }
+
+// A rank such that at least k of the lanes' largest ranks lie at or above it (1
+// where there are not so many above 0): the wave's k best do too, and few others.
+__device__ __forceinline__ uint32_t rank_floor(uint32_t largest, int k) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t x = t | 1u << bit;
+    if (__popcll(__ballot(largest >= x)) >= k) t = x;
+  }
+  return t ? t : 1u;
+}
+
+constexpr int RU_CAND = 64;        // candidates of a wave
+
+template <typename T, int SUBS>
+__global__ __launch_bounds__(SUBS * RU_NT) void k_rules(RulesLaunch a, int chunks) {
+  constexpr int VEC = Logits<T>::VEC, NV = RU_E / VEC, NT = SUBS * RU_NT, TOKENS = SUBS * RU_CHUNK;
+  extern __shared__ __attribute__((aligned(16))) uint32_t table[];   // [TOKENS] where there are lists
+  __shared__ uint2 cand[SUBS * 4][RU_CAND];
+  __shared__ int cand_n[SUBS * 4];
+  __shared__ float wave_ms[SUBS * 4][2];
+  const int tid = threadIdx.x % RU_NT, sub = threadIdx.x / RU_NT, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blockIdx.y, b0 = blockIdx.x * TOKENS, v0 = b0 + sub * RU_CHUNK;
   const int V = a.vocab;
   const T* src = (const T*)a.logits + (int64_t)row * a.ld + v0;
+  uint32_t* own = table + sub * RU_CHUNK;
 
   float z[RU_E];
 #pragma unroll
@@ -95,92 +116,111 @@ __global__ __launch_bounds__(RU_NT) void k_rules(RulesLaunch a) {
     }
   }
 
+  // everything about the set at once (a chain of loads is what a single row waits for)
   int set = a.set ? a.set[row] : row;
   const bool ruled = set >= 0 && set < a.sets;
   if (!ruled) set = 0;
-  const int hist_n = ruled && a.history ? (int)min((int64_t)max(a.history_len[set], 0), a.history_ld) : 0;
-  const int bias_n = ruled && a.bias_token ? (int)min((int64_t)max(a.bias_len[set], 0), a.bias_ld) : 0;
-  const int mask_row = ruled && a.mask ? (a.mask_of ? a.mask_of[set] : set) : -1;
-  if (hist_n > 0 || bias_n > 0) {                      // block-uniform
+  const bool some = ruled && a.sets > 0;
+  const int hist_len = some && a.history ? a.history_len[set] : 0;
+  const int prompt = some && a.history && a.prompt_len ? a.prompt_len[set] : 0;
+  const int bias_len = some && a.bias_token ? a.bias_len[set] : 0;
+  const int mask_row = some && a.mask ? (a.mask_of ? a.mask_of[set] : set) : -1;
+  const float rep = some && a.repetition ? a.repetition[set] : 1.f;
+  const float freq = some && a.frequency ? a.frequency[set] : 0.f;
+  const float pres = some && a.presence ? a.presence[set] : 0.f;
+  const float temp = some && a.temperature ? a.temperature[set] : 1.f;
+  const int hist_n = (int)min((int64_t)max(hist_len, 0), a.history_ld);
+  const int bias_n = (int)min((int64_t)max(bias_len, 0), a.bias_ld);
+  const bool masked = mask_row >= 0 && mask_row < a.masks;
+  uint32_t words[NV];
+  if (masked) {
 #pragma unroll
-    for (int i = 0; i < RU_E / 4; ++i) {
-      *(uint4*)(count + (i * RU_NT + tid) * 4) = uint4{0u, 0u, 0u, 0u};
-      *(float4*)(bias + (i * RU_NT + tid) * 4) = float4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < NV; ++i) {
+      const int v = v0 + (i * RU_NT + tid) * VEC;      // VEC tokens lie in one word
+      words[i] = v < V ? a.mask[(int64_t)mask_row * a.mask_ld + (v >> 5)] >> (v & 31) : 0u;
     }
+  }
+  if (hist_n > 0) {                                    // block-uniform
+#pragma unroll
+    for (int i = 0; i < RU_E / 4; ++i) *(uint4*)(table + (i * NT + (int)threadIdx.x) * 4) = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
     const int32_t* hist = a.history + (int64_t)set * a.history_ld;
-    const int prompt = a.prompt_len ? a.prompt_len[set] : 0;
-    for (int j0 = tid; j0 < hist_n; j0 += 8 * RU_NT) {
+    for (int j0 = threadIdx.x; j0 < hist_n; j0 += 8 * NT) {
       int tok[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) tok[i] = j0 + i * RU_NT < hist_n ? hist[j0 + i * RU_NT] : -1;
+      for (int i = 0; i < 8; ++i) tok[i] = j0 + i * NT < hist_n ? hist[j0 + i * NT] : -1;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t u = (uint32_t)tok[i] - (uint32_t)v0;
-        if (tok[i] < 0 || u >= RU_CHUNK) continue;
-        if (j0 + i * RU_NT < prompt)
-          atomicOr(&count[u], kSeen);
+        const uint32_t u = (uint32_t)tok[i] - (uint32_t)b0;
+        if (tok[i] < 0 || u >= TOKENS) continue;
+        if (j0 + i * NT < prompt)
+          atomicOr(&table[u], kSeen);
         else
-          atomicAdd(&count[u], 1u);
+          atomicAdd(&table[u], 1u);
       }
     }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RU_E / 4; ++i) {
+      const int u = i * 4 / VEC * RU_NT * VEC + tid * VEC + i * 4 % VEC;
+      const uint4 c4 = *(const uint4*)(own + u);
+      const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (!c[j]) continue;
+        float x = z[4 * i + j];
+        x = x > 0.f ? x / rep : x * rep;
+        const uint32_t times = c[j] & ~kSeen;
+        if (times) x = (x - freq * (float)times) - pres;
+        z[4 * i + j] = x;
+      }
+    }
+  }
+  if (bias_n > 0) {
     // the biases in the order of their list, so that a token given twice has
-    // one sum: a wave takes the tokens that are its number modulo 4, one after
-    // the other
+    // one sum: of 64 entries, those that are a wave's in turn
+    float* sums = (float*)table;
+    if (hist_n > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RU_E / 4; ++i) *(float4*)(sums + (i * NT + (int)threadIdx.x) * 4) = float4{0.f, 0.f, 0.f, 0.f};
+    __syncthreads();
     const int32_t* bt = a.bias_token + (int64_t)set * a.bias_ld;
     const float* bv = a.bias_value + (int64_t)set * a.bias_ld;
     for (int j0 = 0; j0 < bias_n; j0 += 64) {
       const bool in = j0 + lane < bias_n;
       const int tok = in ? bt[j0 + lane] : -1;
       const float val = in ? bv[j0 + lane] : 0.f;
-      const uint32_t u = (uint32_t)tok - (uint32_t)v0;
-      uint64_t hit = __ballot(tok >= 0 && u < RU_CHUNK && (tok & 3) == wave);
+      const uint32_t u = (uint32_t)tok - (uint32_t)b0;
+      uint64_t hit = __ballot(tok >= 0 && u < TOKENS && (tok & (SUBS * 4 - 1)) == wave);
       while (hit) {
         const int l = __ffsll((unsigned long long)hit) - 1;
         hit &= hit - 1;
         const uint32_t ul = __builtin_amdgcn_readlane(u, l);
         const float vl = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(val), l));
-        if (lane == 0) bias[ul] += vl;
+        if (lane == 0) sums[ul] += vl;
       }
     }
     __syncthreads();
-    const float rep = a.repetition ? a.repetition[set] : 1.f;
-    const float freq = a.frequency ? a.frequency[set] : 0.f;
-    const float pres = a.presence ? a.presence[set] : 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const int u = (i * RU_NT + tid) * VEC + j;
-        const uint32_t c = count[u];
-        float x = z[i * VEC + j];
-        if (c) {
-          x = x > 0.f ? x / rep : x * rep;
-          const uint32_t times = c & ~kSeen;
-          if (times) x = (x - freq * (float)times) - pres;
-        }
-        if (bias_n > 0) x = x + bias[u];
-        z[i * VEC + j] = x;
-      }
+    for (int i = 0; i < RU_E / 4; ++i) {
+      const int u = i * 4 / VEC * RU_NT * VEC + tid * VEC + i * 4 % VEC;
+      const float4 x = *(const float4*)((const float*)own + u);
+      z[4 * i] = z[4 * i] + x.x;
+      z[4 * i + 1] = z[4 * i + 1] + x.y;
+      z[4 * i + 2] = z[4 * i + 2] + x.z;
+      z[4 * i + 3] = z[4 * i + 3] + x.w;
     }
   }
-  if (mask_row >= 0 && mask_row < a.masks) {
-    const uint32_t* words = a.mask + (int64_t)mask_row * a.mask_ld;
+  if (masked) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int v = v0 + (i * RU_NT + tid) * VEC;      // VEC tokens lie in one word
-      const uint32_t w = v < V ? words[v >> 5] >> (v & 31) : 0u;
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < VEC; ++j)
-        if (!(w >> j & 1)) z[i * VEC + j] = -INFINITY;
-    }
+        if (!(words[i] >> j & 1)) z[i * VEC + j] = -INFINITY;
   }
-  if (ruled && a.temperature) {
-    const float t = a.temperature[set];
-    if (t > 0.f && t != 1.f) {
+  if (temp > 0.f && temp != 1.f) {
 #pragma unroll
-      for (int i = 0; i < RU_E; ++i) z[i] = z[i] / t;
-    }
+    for (int i = 0; i < RU_E; ++i) z[i] = z[i] / temp;
   }
   if (a.out) {
     float* dst = a.out + (int64_t)row * a.out_ld + v0;
@@ -222,69 +262,80 @@ __global__ __launch_bounds__(RU_NT) void k_rules(RulesLaunch a) {
     wave_ms[wave][1] = sum;
   }
 
-  // the wave's k best: each lane offers the best that it has not yet given
-  uint32_t given = 0;
-  uint32_t rank = 0;
-  int token = 0;
-  auto offer = [&]() {
-    rank = 0;
-    token = 0;
+  // the wave's candidates, its k best among them
+  uint32_t rank[RU_E], largest = 0;
 #pragma unroll
-    for (int i = 0; i < RU_E; ++i) {
-      const uint32_t r = given >> i & 1 ? 0u : rank_of(z[i]);
-      if (r > rank) {
-        rank = r;
-        token = i;
+  for (int i = 0; i < RU_E; ++i) {
+    rank[i] = rank_of(z[i]);
+    largest = max(largest, rank[i]);
+  }
+  const auto token_of = [&](int i) { return v0 + ((i / VEC) * RU_NT + tid) * VEC + i % VEC; };
+  const uint32_t least = a.k == 1 ? max(wave_max_u32(largest), 1u) : rank_floor(largest, a.k);
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < RU_E; ++i) {
+    const uint64_t in = __ballot(rank[i] >= least);
+    if (!in) continue;
+    const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0));
+    if (rank[i] >= least && at < RU_CAND) cand[wave][at] = uint2{rank[i], (uint32_t)token_of(i)};
+    n += __popcll(in);
+  }
+  if (n > RU_CAND) {
+    // many equal ones: k rounds, each lane offering the best that it has not yet given
+    uint32_t given = 0;
+    for (n = 0; n < a.k; ++n) {
+      uint32_t r = 0;
+      int tok = 0;
+#pragma unroll
+      for (int i = 0; i < RU_E; ++i)
+        if (!(given >> i & 1) && rank[i] > r) {
+          r = rank[i];
+          tok = i;
+        }
+      const int l = best_lane(r, token_of(tok));
+      if (l < 0) break;
+      if (lane == l) {
+        cand[wave][n] = uint2{r, (uint32_t)token_of(tok)};
+        given |= 1u << tok;
       }
     }
-    token = v0 + ((token / VEC) * RU_NT + tid) * VEC + token % VEC;
-  };
-  offer();
-  for (int i = 0; i < a.k; ++i) {
-    const int l = best_lane(rank, token);
-    if (l < 0) {
-      if (lane == 0) best[wave][i] = uint2{0u, 0u};
-      continue;
-    }
-    if (lane == l) {
-      best[wave][i] = uint2{rank, (uint32_t)token};
-      const int u = token - v0;
-      given |= 1u << (u / (RU_NT * VEC) * VEC + u % VEC);
-      offer();
-    }
   }
+  if (lane == 0) cand_n[wave] = n;
   __syncthreads();
-  if (wave != 0) return;
-  // the block's: a token's place is the number of better ones
-  uint2* keys = (uint2*)(a.ws + (int64_t)a.rows * gridDim.x * 2) + ((int64_t)row * gridDim.x + chunk) * a.k;
-  const int n = 4 * a.k;
-  uint2 mine = {0u, 0u};
-  if (lane < n) mine = best[lane / a.k][lane % a.k];
+  if (v0 >= V) return;
+  // the 256 threads': a candidate's place is the number of better ones
+  const int chunk = blockIdx.x * SUBS + sub, w0 = wave & ~3;
+  uint2* keys = (uint2*)(a.ws + (int64_t)a.rows * chunks * 2) + ((int64_t)row * chunks + chunk) * a.k;
+  const uint2 mine = lane < n ? cand[wave][lane] : uint2{0u, 0u};
   int place = 0, have = 0;
-  for (int i = 0; i < n; ++i) {
-    const uint32_t r = __builtin_amdgcn_readlane(mine.x, i), t = __builtin_amdgcn_readlane(mine.y, i);
-    place += r > mine.x || (r == mine.x && t < mine.y);
-    have += r != 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int m = __builtin_amdgcn_readfirstlane(cand_n[w0 + w]);
+    have += m;
+    for (int i = 0; i < m; ++i) place += better(cand[w0 + w][i], mine);
   }
-  if (mine.x != 0 && place < a.k) keys[place] = mine;
-  if (lane >= have && lane < a.k) keys[lane] = uint2{0u, 0u};
-  if (lane == 0) {
-    float M = wave_ms[0][0], S = 0.f;
+  if (lane < n && place < a.k) keys[place] = mine;
+  if (wave == w0) {
+    if (lane >= have && lane < a.k) keys[lane] = uint2{0u, 0u};
+    if (lane == 0) {
+      float M = wave_ms[w0][0], S = 0.f;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) M = fmaxf(M, wave_ms[w][0]);
+      for (int w = 1; w < 4; ++w) M = fmaxf(M, wave_ms[w0 + w][0]);
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
-      S += wave_ms[w][0] == M ? wave_ms[w][1]
-                              : wave_ms[w][1] * __builtin_amdgcn_exp2f((wave_ms[w][0] - M) * 1.4426950408889634f);
-    *((float2*)a.ws + (int64_t)row * gridDim.x + chunk) = float2{M, S};
+      for (int w = 0; w < 4; ++w)
+        S += wave_ms[w0 + w][0] == M
+                 ? wave_ms[w0 + w][1]
+                 : wave_ms[w0 + w][1] * __builtin_amdgcn_exp2f((wave_ms[w0 + w][0] - M) * 1.4426950408889634f);
+      *((float2*)a.ws + (int64_t)row * chunks + chunk) = float2{M, S};
+    }
   }
 }
 
-// A row's blocks joined, one wave a row: lane l goes down the sorted lists of
-// blocks l, l + 64, ...
+// A row's blocks joined, one wave a row, in the same way: a floor under the k
+// best, the few above it, the place of each.
 __global__ __launch_bounds__(64) void k_rules_join(RulesLaunch a, int chunks) {
   constexpr int LISTS = kRulesMaxVocab / RU_CHUNK / 64;
-  extern __shared__ uint2 rules_lds[];
+  extern __shared__ uint2 rules_lds[];                 // the lists, then RU_CAND candidates
   const int row = blockIdx.x, lane = threadIdx.x, n = chunks * a.k;
   const uint2* keys = (const uint2*)(a.ws + (int64_t)a.rows * chunks * 2) + (int64_t)row * n;
   const float2* ms = (const float2*)a.ws + (int64_t)row * chunks;
@@ -297,7 +348,17 @@ __global__ __launch_bounds__(64) void k_rules_join(RulesLaunch a, int chunks) {
     s[i] = x.y;
     M = fmaxf(M, x.x);
   }
-  for (int i = lane; i < n; i += 64) rules_lds[i] = keys[i];
+  uint32_t largest = 0;
+  for (int i0 = 0; i0 < n; i0 += 4 * 64) {
+    uint2 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = i0 + 64 * i + lane < n ? keys[i0 + 64 * i + lane] : uint2{0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      largest = max(largest, x[i].x);
+      if (i0 + 64 * i + lane < n) rules_lds[i0 + 64 * i + lane] = x[i];
+    }
+  }
   M = wave_max_lanes(M);
   float S = 0.f;
 #pragma unroll
@@ -305,42 +366,70 @@ __global__ __launch_bounds__(64) void k_rules_join(RulesLaunch a, int chunks) {
     S += m[i] == M ? s[i] : s[i] * __builtin_amdgcn_exp2f((m[i] - M) * 1.4426950408889634f);
   const float log_sum = logf(wave_sum_lanes(S));
   __syncthreads();
+  auto put = [&](int place, uint2 x) {
+    const float z = x.x == 0xffffffffu ? NAN : from_ordered_u32(x.x);
+    a.token[(int64_t)row * a.k + place] = x.x ? (int)x.y : -1;
+    a.logprob[(int64_t)row * a.k + place] = x.x ? (z - M) - log_sum : -INFINITY;
+  };
+  uint2* cand = rules_lds + n;
+  const uint32_t least = rank_floor(largest, a.k);
+  int have = 0;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const uint2 x = i0 + lane < n ? rules_lds[i0 + lane] : uint2{0u, 0u};
+    const uint64_t in = __ballot(x.x >= least);
+    const int at = have + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0));
+    if (x.x >= least && at < RU_CAND) cand[at] = x;
+    have += __popcll(in);
+  }
+  __syncthreads();
+  if (have <= RU_CAND) {
+    const uint2 mine = lane < have ? cand[lane] : uint2{0u, 0u};
+    int place = 0;
+    for (int i = 0; i < have; ++i) place += better(cand[i], mine);
+    if (lane < have && place < a.k) put(place, mine);
+    if (lane >= have && lane < a.k) put(lane, uint2{0u, 0u});
+    return;
+  }
+  // many equal ones: lane l goes down the sorted lists of blocks l, l + 64, ...
   int at[LISTS];
 #pragma unroll
   for (int i = 0; i < LISTS; ++i) at[i] = 0;
-  uint32_t rank = 0;
-  int token = 0, from = 0;
-  auto offer = [&]() {
-    rank = 0;
+  for (int i = 0; i < a.k; ++i) {
+    uint2 x = {0u, 0u};
+    int from = 0;
 #pragma unroll
-    for (int i = 0; i < LISTS; ++i) {
-      const int c = lane + 64 * i;
-      if (c >= chunks || at[i] >= a.k) continue;
-      const uint2 x = rules_lds[c * a.k + at[i]];
-      if (x.x > rank) {                                // (equal: the lower chunk has the lower tokens)
-        rank = x.x;
-        token = (int)x.y;
-        from = i;
+    for (int j = 0; j < LISTS; ++j) {
+      const int c = lane + 64 * j;
+      if (c >= chunks || at[j] >= a.k) continue;
+      const uint2 y = rules_lds[c * a.k + at[j]];
+      if (y.x > x.x) {                                 // (equal: the lower chunk has the lower tokens)
+        x = y;
+        from = j;
       }
     }
-  };
-  offer();
-  for (int i = 0; i < a.k; ++i) {
-    const int l = best_lane(rank, token);
+    const int l = best_lane(x.x, (int)x.y);
     if (l < 0) {
-      if (lane == 0) {
-        a.token[(int64_t)row * a.k + i] = -1;
-        a.logprob[(int64_t)row * a.k + i] = -INFINITY;
-      }
+      if (lane == 0) put(i, uint2{0u, 0u});
     } else if (lane == l) {
-      const float z = rank == 0xffffffffu ? NAN : from_ordered_u32(rank);
-      a.token[(int64_t)row * a.k + i] = token;
-      a.logprob[(int64_t)row * a.k + i] = (z - M) - log_sum;
+      put(i, x);
 #pragma unroll
       for (int j = 0; j < LISTS; ++j) at[j] += j == from;
-      offer();
     }
   }
+}
+
+template <typename T>
+void rules(const RulesLaunch& a, hipStream_t s) {
+  const int chunks = (a.vocab + RU_CHUNK - 1) / RU_CHUNK;
+  const bool lists = a.history || a.bias_token;
+  if (a.history_ld >= kLongHistory) {
+    constexpr int SUBS = 4;
+    static_assert(SUBS * RU_CHUNK * 4 <= 65536, "dynamic LDS without asking");
+    k_rules<T, SUBS><<<dim3((chunks + SUBS - 1) / SUBS, a.rows), SUBS * RU_NT, lists ? SUBS * RU_CHUNK * 4 : 0, s>>>(a, chunks);
+  } else {
+    k_rules<T, 1><<<dim3(chunks, a.rows), RU_NT, lists ? RU_CHUNK * 4 : 0, s>>>(a, chunks);
+  }
+  if (a.k > 0) k_rules_join<<<a.rows, 64, ((size_t)chunks * a.k + RU_CAND) * sizeof(uint2), s>>>(a, chunks);
 }
 
 }  // namespace
@@ -352,12 +441,10 @@ size_t rules_ws_bytes(int rows, int vocab, int k) {
 
 void logit_rules(const RulesLaunch& a, bool bf16, hipStream_t s) {
   if (a.rows <= 0) return;
-  const int chunks = (a.vocab + RU_CHUNK - 1) / RU_CHUNK;
   if (bf16)
-    k_rules<bf16_t><<<dim3(chunks, a.rows), RU_NT, 0, s>>>(a);
+    rules<bf16_t>(a, s);
   else
-    k_rules<float><<<dim3(chunks, a.rows), RU_NT, 0, s>>>(a);
-  if (a.k > 0) k_rules_join<<<a.rows, 64, (size_t)chunks * a.k * sizeof(uint2), s>>>(a, chunks);
+    rules<float>(a, s);
 }
 
 }  // namespace asr
