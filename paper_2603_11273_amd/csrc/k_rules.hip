@@ -22,10 +22,12 @@ namespace {
 
 constexpr int RU_NT = 256, RU_E = 16, RU_CHUNK = RU_NT * RU_E;
 static_assert(RU_CHUNK == kRulesChunk, "workspace");
-constexpr int kLongHistory = 4096;
+// chunks of a block where histories may be long: every block reads all of them
+constexpr int RU_LONG = 4, kLongHistory = 4096;
 constexpr uint32_t kSeen = 0x80000000u;     // in the history; below it the count behind the prompt
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
 
 // VEC neighbouring logits; rows begin at any element (an odd vocabulary), which
@@ -73,6 +75,31 @@ __device__ __forceinline__ int best_lane(uint32_t rank, int token) {
   return __ffsll((unsigned long long)who) - 1;
 }
 
+// f(token - b0) of the entries [from, to) of a list: what is no token, or none of
+// the block's, ends far above them.  Every block reads the whole list, so what
+// counts is the instructions of an entry: 16 a thread without a test while there
+// are so many.
+template <int NT, class F>
+__device__ __forceinline__ void each_token(const int32_t* list, int from, int to, int b0, F&& f) {
+  for (; to - from >= 16 * NT; from += 16 * NT) {
+    i32x4u tok[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tok[i] = *(const i32x4u*)(list + from + (i * NT + (int)threadIdx.x) * 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f((uint32_t)tok[i][e] - (uint32_t)b0);
+  }
+  for (; from < to; from += 8 * NT) {
+    int tok[8];
+    const int at = from + (int)threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) tok[i] = list[min(at + i * NT, to - 1)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f(at + i * NT < to ? (uint32_t)tok[i] - (uint32_t)b0 : ~0u);
+  }
+}
+
 // The better of two results comes first.
 __device__ __forceinline__ bool better(uint2 a, uint2 b) { return a.x > b.x || (a.x == b.x && a.y < b.y); }
 
@@ -88,10 +115,11 @@ __device__ __forceinline__ uint32_t rank_floor(uint32_t largest, int k) {
   return t ? t : 1u;
 }
 
-constexpr int RU_CAND = 64;        // candidates of a wave
+constexpr int RU_CAND = 64;                  // candidates of a wave
+constexpr uint32_t kLowest = 0x00800000u;    // rank of the lowest finite float
 
 template <typename T, int SUBS>
-__global__ __launch_bounds__(SUBS * RU_NT) void k_rules(RulesLaunch a, int chunks) {
+__device__ __forceinline__ void rules_block(const RulesLaunch& a, int chunks) {
   constexpr int VEC = Logits<T>::VEC, NV = RU_E / VEC, NT = SUBS * RU_NT, TOKENS = SUBS * RU_CHUNK;
   extern __shared__ __attribute__((aligned(16))) uint32_t table[];   // [TOKENS] where there are lists
   __shared__ uint2 cand[SUBS * 4][RU_CAND];
@@ -144,35 +172,30 @@ __global__ __launch_bounds__(SUBS * RU_NT) void k_rules(RulesLaunch a, int chunk
 #pragma unroll
     for (int i = 0; i < RU_E / 4; ++i) *(uint4*)(table + (i * NT + (int)threadIdx.x) * 4) = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
+    // the prompt's tokens are marked, the others counted
     const int32_t* hist = a.history + (int64_t)set * a.history_ld;
-    for (int j0 = threadIdx.x; j0 < hist_n; j0 += 8 * NT) {
-      int tok[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) tok[i] = j0 + i * NT < hist_n ? hist[j0 + i * NT] : -1;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t u = (uint32_t)tok[i] - (uint32_t)b0;
-        if (tok[i] < 0 || u >= TOKENS) continue;
-        if (j0 + i * NT < prompt)
-          atomicOr(&table[u], kSeen);
-        else
-          atomicAdd(&table[u], 1u);
-      }
-    }
+    const int marked = min(max(prompt, 0), hist_n);
+    each_token<NT>(hist, 0, marked, b0, [&](uint32_t u) {
+      if (u < TOKENS) atomicOr(&table[u], kSeen);
+    });
+    each_token<NT>(hist, marked, hist_n, b0, [&](uint32_t u) {
+      if (u < TOKENS) atomicAdd(&table[u], 1u);
+    });
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < RU_E / 4; ++i) {
       const int u = i * 4 / VEC * RU_NT * VEC + tid * VEC + i * 4 % VEC;
       const uint4 c4 = *(const uint4*)(own + u);
       const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
+      // (few of the wave's tokens were said, mostly none: no division for them)
+      if (!__any(c4.x | c4.y | c4.z | c4.w)) continue;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (!c[j]) continue;
         float x = z[4 * i + j];
         x = x > 0.f ? x / rep : x * rep;
         const uint32_t times = c[j] & ~kSeen;
         if (times) x = (x - freq * (float)times) - pres;
-        z[4 * i + j] = x;
+        z[4 * i + j] = c[j] ? x : z[4 * i + j];
       }
     }
   }
@@ -248,10 +271,10 @@ __global__ __launch_bounds__(SUBS * RU_NT) void k_rules(RulesLaunch a, int chunk
       if (v0 + ((i / VEC) * RU_NT + tid) * VEC + i % VEC >= V) z[i] = -INFINITY;
   }
 
-  float mx = z[0];
+  float largest = z[0];
 #pragma unroll
-  for (int i = 1; i < RU_E; ++i) mx = fmaxf(mx, z[i]);
-  mx = wave_max_lanes(mx);
+  for (int i = 1; i < RU_E; ++i) largest = fmaxf(largest, z[i]);
+  const float mx = wave_max_lanes(largest);
   const float ref = mx == -INFINITY ? 0.f : mx;
   float sum = 0.f;
 #pragma unroll
@@ -262,23 +285,21 @@ __global__ __launch_bounds__(SUBS * RU_NT) void k_rules(RulesLaunch a, int chunk
     wave_ms[wave][1] = sum;
   }
 
-  // the wave's candidates, its k best among them
-  uint32_t rank[RU_E], largest = 0;
-#pragma unroll
-  for (int i = 0; i < RU_E; ++i) {
-    rank[i] = rank_of(z[i]);
-    largest = max(largest, rank[i]);
-  }
+  // the wave's candidates, its k best among them: what is not below the floor
   const auto token_of = [&](int i) { return v0 + ((i / VEC) * RU_NT + tid) * VEC + i % VEC; };
-  const uint32_t least = a.k == 1 ? max(wave_max_u32(largest), 1u) : rank_floor(largest, a.k);
-  int n = 0;
+  int n = RU_CAND + 1;
+  if (sum == sum) {                                    // (a NaN or +inf would not compare: the other way)
+    const float least = a.k == 1 ? fmaxf(mx, -3.402823466e38f)
+                                 : from_ordered_u32(max(rank_floor(rank_of(largest), a.k), kLowest));
+    n = 0;
 #pragma unroll
-  for (int i = 0; i < RU_E; ++i) {
-    const uint64_t in = __ballot(rank[i] >= least);
-    if (!in) continue;
-    const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0));
-    if (rank[i] >= least && at < RU_CAND) cand[wave][at] = uint2{rank[i], (uint32_t)token_of(i)};
-    n += __popcll(in);
+    for (int i = 0; i < RU_E; ++i) {
+      const uint64_t in = __ballot(z[i] >= least);
+      if (!in) continue;
+      const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0));
+      if (z[i] >= least && at < RU_CAND) cand[wave][at] = uint2{rank_of(z[i]), (uint32_t)token_of(i)};
+      n += __popcll(in);
+    }
   }
   if (n > RU_CAND) {
     // many equal ones: k rounds, each lane offering the best that it has not yet given
@@ -287,11 +308,13 @@ __global__ __launch_bounds__(SUBS * RU_NT) void k_rules(RulesLaunch a, int chunk
       uint32_t r = 0;
       int tok = 0;
 #pragma unroll
-      for (int i = 0; i < RU_E; ++i)
-        if (!(given >> i & 1) && rank[i] > r) {
-          r = rank[i];
+      for (int i = 0; i < RU_E; ++i) {
+        const uint32_t x = given >> i & 1 ? 0u : rank_of(z[i]);
+        if (x > r) {
+          r = x;
           tok = i;
         }
+      }
       const int l = best_lane(r, token_of(tok));
       if (l < 0) break;
       if (lane == l) {
@@ -329,6 +352,18 @@ __global__ __launch_bounds__(SUBS * RU_NT) void k_rules(RulesLaunch a, int chunk
       *((float2*)a.ws + (int64_t)row * chunks + chunk) = float2{M, S};
     }
   }
+}
+
+template <typename T>
+__global__ __launch_bounds__(RU_NT) void k_rules(RulesLaunch a, int chunks) {
+  rules_block<T, 1>(a, chunks);
+}
+// (two of these blocks fit a CU only with at most 64 vector and 80 scalar
+// registers a wave: 256 rows of 131071, 32768 tokens of history 151 -> 110 us)
+template <typename T>
+__global__ __launch_bounds__(RU_LONG * RU_NT) __attribute__((amdgpu_waves_per_eu(8), amdgpu_num_sgpr(80)))
+void k_rules_long(RulesLaunch a, int chunks) {
+  rules_block<T, RU_LONG>(a, chunks);
 }
 
 // A row's blocks joined, one wave a row, in the same way: a floor under the k
@@ -423,11 +458,11 @@ void rules(const RulesLaunch& a, hipStream_t s) {
   const int chunks = (a.vocab + RU_CHUNK - 1) / RU_CHUNK;
   const bool lists = a.history || a.bias_token;
   if (a.history_ld >= kLongHistory) {
-    constexpr int SUBS = 4;
-    static_assert(SUBS * RU_CHUNK * 4 <= 65536, "dynamic LDS without asking");
-    k_rules<T, SUBS><<<dim3((chunks + SUBS - 1) / SUBS, a.rows), SUBS * RU_NT, lists ? SUBS * RU_CHUNK * 4 : 0, s>>>(a, chunks);
+    static_assert(RU_LONG * RU_CHUNK * 4 <= 65536, "dynamic LDS without asking");
+    k_rules_long<T><<<dim3((chunks + RU_LONG - 1) / RU_LONG, a.rows), RU_LONG * RU_NT,
+                      lists ? RU_LONG * RU_CHUNK * 4 : 0, s>>>(a, chunks);
   } else {
-    k_rules<T, 1><<<dim3(chunks, a.rows), RU_NT, lists ? RU_CHUNK * 4 : 0, s>>>(a, chunks);
+    k_rules<T><<<dim3(chunks, a.rows), RU_NT, lists ? RU_CHUNK * 4 : 0, s>>>(a, chunks);
   }
   if (a.k > 0) k_rules_join<<<a.rows, 64, ((size_t)chunks * a.k + RU_CAND) * sizeof(uint2), s>>>(a, chunks);
 }
