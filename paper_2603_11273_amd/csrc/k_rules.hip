@@ -75,28 +75,51 @@ __device__ __forceinline__ int best_lane(uint32_t rank, int token) {
   return __ffsll((unsigned long long)who) - 1;
 }
 
-// f(token - b0) of the entries [from, to) of a list: what is no token, or none of
-// the block's, ends far above them.  Every block reads the whole list, so what
-// counts is the instructions of an entry: 16 a thread without a test while there
-// are so many.
-template <int NT, class F>
-__device__ __forceinline__ void each_token(const int32_t* list, int from, int to, int b0, F&& f) {
-  for (; to - from >= 16 * NT; from += 16 * NT) {
+// The history's n entries into the block's table: the first `marked` as seen, the
+// others counted.  Every block reads the whole list, so what counts is the
+// instructions of an entry: 16 a thread without a test while there are so many,
+// then four.  What is no token, or none of the block's, ends far above them.
+template <int NT, int TOKENS>
+__device__ __forceinline__ void count_tokens(const int32_t* list, int marked, int n, int b0, uint32_t* table) {
+  int from = 0;
+  for (; n - from >= 16 * NT; from += 16 * NT) {
     i32x4u tok[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) tok[i] = *(const i32x4u*)(list + from + (i * NT + (int)threadIdx.x) * 4);
+    auto each = [&](auto&& f) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f((uint32_t)tok[i][e] - (uint32_t)b0);
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t u = (uint32_t)tok[i][e] - (uint32_t)b0;
+          if (u < TOKENS) f(u, from + (i * NT + (int)threadIdx.x) * 4 + e);
+        }
+    };
+    if (from + 16 * NT <= marked)
+      each([&](uint32_t u, int) { atomicOr(&table[u], kSeen); });
+    else
+      each([&](uint32_t u, int j) {
+        if (j < marked)
+          atomicOr(&table[u], kSeen);
+        else
+          atomicAdd(&table[u], 1u);
+      });
   }
-  for (; from < to; from += 8 * NT) {
-    int tok[8];
+  for (; from < n; from += 4 * NT) {
+    int tok[4];
     const int at = from + (int)threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) tok[i] = list[min(at + i * NT, to - 1)];
+    for (int i = 0; i < 4; ++i) tok[i] = list[min(at + i * NT, n - 1)];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f(at + i * NT < to ? (uint32_t)tok[i] - (uint32_t)b0 : ~0u);
+    for (int i = 0; i < 4; ++i) {
+      const int j = at + i * NT;
+      const uint32_t u = (uint32_t)tok[i] - (uint32_t)b0;
+      if (j >= n || u >= TOKENS) continue;
+      if (j < marked)
+        atomicOr(&table[u], kSeen);
+      else
+        atomicAdd(&table[u], 1u);
+    }
   }
 }
 
@@ -172,15 +195,7 @@ __device__ __forceinline__ void rules_block(const RulesLaunch& a, int chunks) {
 #pragma unroll
     for (int i = 0; i < RU_E / 4; ++i) *(uint4*)(table + (i * NT + (int)threadIdx.x) * 4) = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
-    // the prompt's tokens are marked, the others counted
-    const int32_t* hist = a.history + (int64_t)set * a.history_ld;
-    const int marked = min(max(prompt, 0), hist_n);
-    each_token<NT>(hist, 0, marked, b0, [&](uint32_t u) {
-      if (u < TOKENS) atomicOr(&table[u], kSeen);
-    });
-    each_token<NT>(hist, marked, hist_n, b0, [&](uint32_t u) {
-      if (u < TOKENS) atomicAdd(&table[u], 1u);
-    });
+    count_tokens<NT, TOKENS>(a.history + (int64_t)set * a.history_ld, prompt, hist_n, b0, table);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < RU_E / 4; ++i) {
