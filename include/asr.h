@@ -369,7 +369,8 @@ asr_status asr_debug_set_encoder_out(asr_ctx* ctx, const int32_t* slots, const i
                                      const int32_t* steps_left, int32_t n, const float* E,
                                      int32_t on_device);
 /* Reads (which = 0: self cache [n_dec][2][H][448][64]; which = 1: cross cache
- * [n_dec][2][H][1500][64]) of one slot as float32. */
+ * [n_dec][2][H][1500][64]) of one slot as float32 (of a hypothesis: what it
+ * reads, shared positions included). */
 asr_status asr_debug_get_kv(asr_ctx* ctx, int32_t slot, int32_t which, float* out);
 /* Writes the self cache of an occupied slot from float32 [n_dec][2][H][448][64]
  * (host, or device when on_device) and sets its position to `length`
@@ -401,6 +402,70 @@ asr_status asr_debug_set_self_kv(asr_ctx* ctx, int32_t slot, const float* src, i
  * range), EDEVICE (HIP error). */
 asr_status asr_logmel_noalloc(const float* const* pcm, const int64_t* n_samples, int32_t n,
                               int32_t n_mels, float* out, void* stream);
+
+/* ---- hypotheses and rules --------------------------------------------------
+ * Beam search, best-of-n and temperature fallback decode one clip several
+ * times; grammars, suppressed tokens, hot words and penalties for repeated
+ * tokens say which tokens may come next.  Both need a second block of device
+ * memory, bound after asr_bind; contexts without one run as if this section
+ * did not exist.
+ *
+ * asr_hypotheses_size: bytes for up to max_bias biases per slot and a table of
+ * n_masks masks.  asr_bind_hypotheses hands the block over (256-byte aligned,
+ * the caller's until asr_destroy), clears every slot's rules and the tokens
+ * known of the slots; ESTATE before asr_bind or while a slot is a hypothesis.
+ * A later asr_bind forgets it. */
+asr_status asr_hypotheses_size(const asr_ctx* ctx, int32_t max_bias, int32_t n_masks, size_t* bytes);
+asr_status asr_bind_hypotheses(asr_ctx* ctx, int32_t max_bias, int32_t n_masks, void* dev_block,
+                               size_t bytes);
+
+/* Makes the free slot dst a hypothesis of the sequence in src: the same
+ * position, steps left, request id, tokens and rules.  The audio's cross cache
+ * and the self cache up to the position of the family's first fork stay where
+ * they are and are shared: a step reads them once for all of a family's rows
+ * (asr_attend_shared).  What src has decoded since is copied.  Slots of a
+ * family decode, fork and are released in any order; a slot whose caches others
+ * read stays taken after its release until they are released too
+ * (asr_slot_info shows it free, prefill passes it over).  Its caches cannot be
+ * overwritten meanwhile (asr_debug_set_*: EINVAL).
+ * Errors: ESTATE (no hypotheses block, continuous batching), EINVAL (src not
+ * occupied, dst out of range or the same), EFULL (dst taken). */
+asr_status asr_fork_slot(asr_ctx* ctx, int32_t src, int32_t dst);
+
+/* Rules of one slot, as asr_logit_rules has them.  History: the tokens decoded
+ * in the slot, the step's input token included, the first n_prompt of them as
+ * the prompt (tokens behind a cache set by asr_debug_set_self_kv are unknown and
+ * not counted).  repetition > 0 (1: off), frequency and presence 0: off,
+ * temperature > 0, mask: a row of the mask table, -1: none; bias_token and
+ * bias_value are host arrays of n_bias <= max_bias entries. */
+typedef struct {
+  float repetition, frequency, presence, temperature;
+  int32_t n_prompt;
+  int32_t mask;
+  int32_t n_bias;
+  const int32_t* bias_token;
+  const float* bias_value;
+} asr_slot_rules;
+/* Gives an occupied slot rules (NULL: none); slot = -1: the rules that every
+ * slot starts with when it is filled from now on, by prefill (continuous
+ * batching included) or asr_debug_set_encoder_out.  asr_set_slot_mask changes a
+ * slot's mask alone (a grammar's state after each token).  asr_set_masks writes
+ * rows [first, first + n) of the mask table from host words
+ * [n][ceil(vocab / 32)], synchronously.  Steps of rows with rules return the
+ * best allowed token in argmax (asr_step, asr_serve_step); logits stay the
+ * model's own.  Errors: ESTATE (no hypotheses block), EINVAL. */
+asr_status asr_set_slot_rules(asr_ctx* ctx, int32_t slot, const asr_slot_rules* rules);
+asr_status asr_set_slot_mask(asr_ctx* ctx, int32_t slot, int32_t mask);
+asr_status asr_set_masks(asr_ctx* ctx, int32_t first, int32_t n, const uint32_t* words);
+
+/* asr_step that also gives each decode row's k best tokens under its rules and
+ * their log-probabilities (k in [1, 16]; host arrays [n_decode][k], -1 and -inf
+ * where fewer tokens are allowed; see asr_logit_rules).  argmax is the first
+ * of them.  Errors as asr_step, ESTATE without a hypotheses block, EDEVICE when
+ * a row's rules allow no token (its argmax is then -1) or a logit is NaN or
+ * infinite. */
+asr_status asr_step_topk(asr_ctx* ctx, const asr_step_in* in, asr_step_out* out, int32_t k,
+                         int32_t* tokens, float* logprobs);
 
 /* ---- operators of a decode step with several hypotheses per clip --------
  * Stateless calls on device memory: every pointer below is a device pointer

@@ -37,6 +37,8 @@ EXPORTED = [
     "asr_serve_plan",
     "asr_serve_tokens", "asr_serve_simulate", "asr_serve_stats",
     "asr_attend_shared_size", "asr_attend_shared", "asr_logit_rules_size", "asr_logit_rules",
+    "asr_hypotheses_size", "asr_bind_hypotheses", "asr_fork_slot", "asr_set_masks",
+    "asr_set_slot_rules", "asr_set_slot_mask", "asr_step_topk",
 ]
 
 
@@ -105,6 +107,13 @@ class Rules(C.Structure):
         ("out_ld", C.c_int64), ("token", C.c_void_p), ("logprob", C.c_void_p)]
 
 
+class SlotRules(C.Structure):
+    _fields_ = [("repetition", C.c_float), ("frequency", C.c_float), ("presence", C.c_float),
+                ("temperature", C.c_float), ("n_prompt", C.c_int32), ("mask", C.c_int32),
+                ("n_bias", C.c_int32), ("bias_token", C.POINTER(C.c_int32)),
+                ("bias_value", C.POINTER(C.c_float))]
+
+
 class AsrError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 8 else status}: {msg}")
@@ -165,6 +174,13 @@ def _load():
         "asr_attend_shared": [P(Attention), vp, C.c_size_t, vp],
         "asr_logit_rules_size": [P(Rules), P(C.c_size_t)],
         "asr_logit_rules": [P(Rules), vp, C.c_size_t, vp],
+        "asr_hypotheses_size": [vp, i32, i32, P(C.c_size_t)],
+        "asr_bind_hypotheses": [vp, i32, i32, vp, C.c_size_t],
+        "asr_fork_slot": [vp, i32, i32],
+        "asr_set_masks": [vp, i32, i32, vp],
+        "asr_set_slot_rules": [vp, i32, P(SlotRules)],
+        "asr_set_slot_mask": [vp, i32, i32],
+        "asr_step_topk": [vp, P(StepIn), P(StepOut), i32, P(i32), P(f)],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -226,14 +242,17 @@ class _Operator:
     them may change between calls."""
 
     def __init__(self, device, workspace, size, run, args):
+        import torch
         self._dev, self._run, self._args = device, run, args
+        # the current stream's handle without a Stream object around it (1.8 us of a 10-us call)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda i: torch.cuda.current_stream(i).cuda_stream)
         self._ref = C.byref(args)
         n = C.c_size_t()
         _check(size(self._ref, C.byref(n)))
         self.workspace_bytes = n.value
         self._ws = workspace
         if workspace is None:
-            import torch
             self._ws = torch.empty(max(n.value, 1), dtype=torch.uint8, device=device)
         self._ws_ptr, self._ws_bytes = self._ws.data_ptr(), self._ws.numel()
 
@@ -250,12 +269,12 @@ class _Operator:
     def _launch(self, stream):
         import torch
         if torch.cuda.current_device() == self._dev.index:
-            st = stream or torch.cuda.current_stream(self._dev)
-            _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st.cuda_stream))
+            st = self._raw_stream(self._dev.index) if stream is None else stream.cuda_stream
+            _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st))
             return
         with torch.cuda.device(self._dev):
-            st = stream or torch.cuda.current_stream(self._dev)
-            _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st.cuda_stream))
+            st = self._raw_stream(self._dev.index) if stream is None else stream.cuda_stream
+            _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st))
 
 
 class SharedAttention(_Operator):
@@ -474,8 +493,9 @@ class Context:
         return n.value
 
     # -- step -----------------------------------------------------------------
-    def step(self, prefill_ids=(), slots=(), tokens=(), want_logits=False):
-        """Returns dict(slot_of, argmax, done, logits)."""
+    def step(self, prefill_ids=(), slots=(), tokens=(), want_logits=False, topk=0):
+        """Returns dict(slot_of, argmax, done, logits); with topk also top_token and top_logprob
+        [rows][topk] (see asr_step_topk)."""
         pids, p_pids = _i64(list(prefill_ids) or [0])
         sl, p_sl = _i32(list(slots) or [0])
         tk, p_tk = _i32(list(tokens) or [0])
@@ -490,9 +510,66 @@ class Context:
             p_lg = logits.ctypes.data_as(C.POINTER(C.c_float))
         sin = StepIn(P, p_pids, D, p_sl, p_tk, p_lg)
         sout = StepOut(p_so, p_am, p_dn)
-        _check(lib.asr_step(self.h, C.byref(sin), C.byref(sout)))
+        out = {}
+        if topk:
+            top = np.zeros((max(D, 1), topk), np.int32)
+            logp = np.zeros((max(D, 1), topk), np.float32)
+            _check(lib.asr_step_topk(self.h, C.byref(sin), C.byref(sout), topk,
+                                     top.ctypes.data_as(C.POINTER(C.c_int32)),
+                                     logp.ctypes.data_as(C.POINTER(C.c_float))))
+            out = {"top_token": top[:D], "top_logprob": logp[:D]}
+        else:
+            _check(lib.asr_step(self.h, C.byref(sin), C.byref(sout)))
         return {"slot_of": slot_of[:P].copy(), "argmax": am[:D].copy(),
-                "done": done[:D].astype(bool), "logits": logits}
+                "done": done[:D].astype(bool), "logits": logits, **out}
+
+    # -- hypotheses and rules ---------------------------------------------------
+    def hypotheses_size(self, max_bias=0, n_masks=0) -> int:
+        n = C.c_size_t()
+        _check(lib.asr_hypotheses_size(self.h, max_bias, n_masks, C.byref(n)))
+        return n.value
+
+    def bind_hypotheses(self, max_bias=0, n_masks=0, block=None):
+        """Binds the block that forked slots and rules need (allocated here when None)."""
+        import torch
+        if block is None:
+            block = torch.empty(self.hypotheses_size(max_bias, n_masks), dtype=torch.uint8,
+                                device=f"cuda:{self.device}")
+        _check(lib.asr_bind_hypotheses(self.h, max_bias, n_masks, C.c_void_p(block.data_ptr()),
+                                       block.numel()))
+        self._hyp_block = block
+        return block
+
+    def fork_slot(self, src, dst):
+        """Makes dst a hypothesis of src's sequence (asr_fork_slot)."""
+        _check(lib.asr_fork_slot(self.h, src, dst))
+
+    def set_masks(self, first, allowed):
+        """Rows of the mask table from a bool array [n][vocab] of allowed tokens."""
+        allowed = np.atleast_2d(np.asarray(allowed, bool))
+        n, V = allowed.shape
+        if V != self.cfg.vocab:
+            raise ValueError(f"masks must cover the vocabulary of {self.cfg.vocab}")
+        bits = np.zeros((n, (V + 31) // 32 * 32), np.uint8)
+        bits[:, :V] = allowed
+        words = np.ascontiguousarray(np.packbits(bits, axis=1, bitorder="little"))
+        _check(lib.asr_set_masks(self.h, first, n, words.ctypes.data))
+
+    def set_slot_rules(self, slot, repetition=1.0, frequency=0.0, presence=0.0, temperature=1.0,
+                       n_prompt=0, mask=-1, bias=()):
+        """Rules of a slot (-1: of every slot filled from now on); bias: (token, value) pairs."""
+        tok, p_tok = _i32([t for t, _ in bias] or [0])
+        val = np.ascontiguousarray([v for _, v in bias] or [0.0], dtype=np.float32)
+        r = SlotRules(repetition, frequency, presence, temperature, n_prompt, mask, len(bias),
+                      p_tok, val.ctypes.data_as(C.POINTER(C.c_float)))
+        _check(lib.asr_set_slot_rules(self.h, slot, C.byref(r)))
+
+    def clear_slot_rules(self, slot):
+        _check(lib.asr_set_slot_rules(self.h, slot, None))
+
+    def set_slot_mask(self, slot, mask):
+        """The row of the mask table that a slot's next tokens must follow (-1: none)."""
+        _check(lib.asr_set_slot_mask(self.h, slot, mask))
 
     def release_slot(self, slot):
         _check(lib.asr_release_slot(self.h, slot))

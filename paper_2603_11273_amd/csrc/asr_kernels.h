@@ -162,6 +162,15 @@ void decode_cross_attn(const float* q, const T* cache, int64_t slot_stride, int6
 template <typename T>
 void decode_cross_merge(const float* part, int D, int n_head, T* out, hipStream_t s);
 
+// The new key and value of each row (float32 qkv [D][3d]) into its slot's cache,
+// and copies of positions [p0, p1) of all layers and heads from slot to slot
+// (`blocks` = layers * 2 * heads, each [kTextCtx][64]).
+template <typename T>
+void decode_append_kv(const float* qkv, T* cache, int64_t slot_stride, int64_t layer_off,
+                      const int32_t* slots, const int32_t* pos, int D, int n_head, hipStream_t s);
+template <typename T>
+void copy_self_kv(const T* src, T* dst, int blocks, int p0, int p1, hipStream_t s);
+
 template <typename T>
 void embed(const T* tok_emb, const float* pos_emb, const int32_t* tokens, const int32_t* pos,
            int D, int d, float* h, hipStream_t s);
@@ -221,6 +230,17 @@ struct RulesLaunch {
 };
 size_t rules_ws_bytes(int rows, int vocab, int k);
 void logit_rules(const RulesLaunch& a, bool bf16, hipStream_t s);
+
+// What a decode step knows of its rows into the per-slot arrays that the rules
+// read: the token at the row's position, the history's length, the scalars of
+// the slot's rules (row arrays, D apart, in the order of the members).
+struct SlotRuleArrays {
+  int32_t *history, *history_len, *prompt_len, *mask_of, *bias_len;
+  float *repetition, *frequency, *presence, *temperature;
+};
+constexpr int kRuleScalars = 7;   // prompt_len, mask_of, bias_len, repetition, frequency, presence, temperature
+void note_rows(const SlotRuleArrays& a, const int32_t* slots, const int32_t* tokens, const int32_t* pos,
+               const int32_t* scalars, int D, hipStream_t s);
 
 // Log-mel front-end.  pcm_ptrs[i] is a device pointer to clip i's samples.
 struct MelTables {

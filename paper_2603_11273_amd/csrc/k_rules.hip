@@ -482,7 +482,28 @@ void rules(const RulesLaunch& a, hipStream_t s) {
   if (a.k > 0) k_rules_join<<<a.rows, 64, ((size_t)chunks * a.k + RU_CAND) * sizeof(uint2), s>>>(a, chunks);
 }
 
+__global__ __launch_bounds__(64) void k_note_rows(SlotRuleArrays a, const int32_t* slots, const int32_t* tokens,
+                                                  const int32_t* pos, const int32_t* scalars, int D) {
+  const int i = blockIdx.x * 64 + threadIdx.x;
+  if (i >= D) return;
+  const int slot = slots[i], p = pos[i];
+  a.history[(int64_t)slot * kTextCtx + p] = tokens[i];
+  a.history_len[slot] = p + 1;
+  a.prompt_len[slot] = scalars[i];
+  a.mask_of[slot] = scalars[D + i];
+  a.bias_len[slot] = scalars[2 * D + i];
+  a.repetition[slot] = __int_as_float(scalars[3 * D + i]);
+  a.frequency[slot] = __int_as_float(scalars[4 * D + i]);
+  a.presence[slot] = __int_as_float(scalars[5 * D + i]);
+  a.temperature[slot] = __int_as_float(scalars[6 * D + i]);
+}
+
 }  // namespace
+
+void note_rows(const SlotRuleArrays& a, const int32_t* slots, const int32_t* tokens, const int32_t* pos,
+               const int32_t* scalars, int D, hipStream_t s) {
+  if (D > 0) k_note_rows<<<(D + 63) / 64, 64, 0, s>>>(a, slots, tokens, pos, scalars, D);
+}
 
 size_t rules_ws_bytes(int rows, int vocab, int k) {
   const size_t chunks = (vocab + RU_CHUNK - 1) / RU_CHUNK;

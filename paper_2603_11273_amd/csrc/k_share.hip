@@ -531,4 +531,39 @@ hipError_t attend_shared(const ShareLaunch& c, bool bf16, hipStream_t s) {
   return bf16 ? attend<bf16_t>(c, s) : attend<float>(c, s);
 }
 
+// One wave per (row, head): lane = dim.
+template <typename T>
+__global__ __launch_bounds__(64) void k_append_kv(const float* __restrict__ qkv, T* cache, int64_t slot_stride,
+                                                  int64_t layer_off, const int32_t* __restrict__ slots,
+                                                  const int32_t* __restrict__ pos, int n_head) {
+  const int h = blockIdx.x, row = blockIdx.y, lane = threadIdx.x, d = n_head * kHeadDim;
+  T* k = cache + (int64_t)slots[row] * slot_stride + layer_off + ((int64_t)h * kTextCtx + pos[row]) * kHeadDim;
+  const float* src = qkv + (int64_t)row * 3 * d + h * kHeadDim + lane;
+  St<T>::st(k, lane, src[d]);
+  St<T>::st(k + (int64_t)n_head * kTextCtx * kHeadDim, lane, src[2 * d]);
+}
+template <typename T>
+void decode_append_kv(const float* qkv, T* cache, int64_t slot_stride, int64_t layer_off, const int32_t* slots,
+                      const int32_t* pos, int D, int n_head, hipStream_t s) {
+  if (D > 0) k_append_kv<T><<<dim3(n_head, D), 64, 0, s>>>(qkv, cache, slot_stride, layer_off, slots, pos, n_head);
+}
+template void decode_append_kv<float>(const float*, float*, int64_t, int64_t, const int32_t*, const int32_t*, int, int,
+                                      hipStream_t);
+template void decode_append_kv<bf16_t>(const float*, bf16_t*, int64_t, int64_t, const int32_t*, const int32_t*, int, int,
+                                       hipStream_t);
+
+// One block per (layer, key or value, head): 16 bytes a thread.
+__global__ __launch_bounds__(256) void k_copy_runs(const uint4* __restrict__ src, uint4* __restrict__ dst, int ld, int first, int n) {
+  const int64_t at = (int64_t)blockIdx.x * ld + first;
+  for (int i = threadIdx.x; i < n; i += 256) dst[at + i] = src[at + i];
+}
+template <typename T>
+void copy_self_kv(const T* src, T* dst, int blocks, int p0, int p1, hipStream_t s) {
+  constexpr int U = kHeadDim * sizeof(T) / 16;         // 16-byte units of a position
+  if (p1 > p0)
+    k_copy_runs<<<blocks, 256, 0, s>>>((const uint4*)src, (uint4*)dst, kTextCtx * U, p0 * U, (p1 - p0) * U);
+}
+template void copy_self_kv<float>(const float*, float*, int, int, int, hipStream_t);
+template void copy_self_kv<bf16_t>(const bf16_t*, bf16_t*, int, int, int, hipStream_t);
+
 }  // namespace asr

@@ -58,6 +58,43 @@ struct Slot {
   int32_t steps_left = 0;
 };
 
+// A slot's place in a family of hypotheses: `root` holds the cross cache that
+// all of them read and the self cache of positions below the root's `shared`;
+// `kids` counts the slots that read this one's (beside itself).
+struct Family {
+  int32_t root = -1;      // -1: the slot's own caches
+  int32_t kids = 0;
+  int32_t shared = 0;     // of a root with kids
+};
+
+// A slot's rules (the biases' entries are in device memory).
+struct Rules {
+  bool active = false;
+  float repetition = 1.f, frequency = 0.f, presence = 0.f, temperature = 1.f;
+  int32_t n_prompt = 0, mask = -1, n_bias = 0;
+};
+
+// The block of asr_bind_hypotheses.
+struct Hypotheses {
+  char* base = nullptr;
+  int32_t max_bias = 0, n_masks = 0;
+  size_t total = 0;
+  size_t history = 0, history_len = 0, prompt_len = 0, mask_of = 0, bias_len = 0, repetition = 0, frequency = 0,
+         presence = 0, temperature = 0, bias_token = 0, bias_value = 0, mask = 0, step = 0, token = 0, logprob = 0,
+         rules_ws = 0, share_ws = 0;
+  size_t rules_ws_size = 0, share_ws_size = 0;
+};
+
+// A decode step: D rows, the last `shared` of them hypotheses in `groups`
+// families of at most `group` rows; k best tokens under rules (0: the argmax).
+struct StepShape {
+  int D = 0, shared = 0, groups = 0, group = 0, k = 0;
+  int64_t self_keys = 0;   // positions of self caches that the step reads (a family's shared ones once)
+  int64_t key(bool logits) const {
+    return (((((int64_t)D * 256 + shared) * 256 + groups) * 256 + group) * 32 + k) * 2 + (logits ? 1 : 0);
+  }
+};
+
 struct EncLayer {
   size_t ln1_g, ln1_b, qkv_w, qkv_b, o_w, o_b, ln2_g, ln2_b, fc1_w, fc1_b, fc2_w, fc2_b;
 };
@@ -113,6 +150,10 @@ struct asr_ctx {
   std::unordered_map<int64_t, Request> waiting;   // submitted, not popped
   std::unordered_map<int64_t, Request> popped;    // popped, not prefilled
   std::vector<Slot> slots;
+  std::vector<Family> family;
+  std::vector<Rules> rules;         // per slot
+  Rules default_rules;
+  Hypotheses hyp;
   // continuous batching (asr_serve_*): the engine owns the slots while on
   ServeEngine serve;
   bool serve_mode = false;
@@ -128,12 +169,12 @@ struct asr_ctx {
   hipEvent_t ev_efork = nullptr, ev_ejoin[kEncGroups - 1] = {};
   std::unordered_map<int64_t, Request> serving;   // admitted, not finished (audio kept
                                                   // for a re-prefill after preemption)
-  // decode steps replayed from HIP graphs, one per (rows, logits wanted),
+  // decode steps replayed from HIP graphs, one per (shape, logits wanted),
   // captured on a private stream at the second step of that shape
   bool decode_graphs = true;
   hipStream_t cap_stream = nullptr;
-  std::unordered_map<int32_t, hipGraphExec_t> dgraph;
-  std::unordered_map<int32_t, int32_t> dshape_seen;
+  std::unordered_map<int64_t, hipGraphExec_t> dgraph;
+  std::unordered_map<int64_t, int32_t> dshape_seen;
   Layout L;
   bool bound = false, loaded = false;
   char* base = nullptr;
@@ -330,6 +371,37 @@ void plan(asr_ctx* c) {
   L.wstage_floats = stage;
   L.wstage = b.take(stage * f4);
   L.total = (b.off + 255) / 256 * 256;
+}
+
+// Keys per part of the hypotheses' attention: fixed, so that a row's result
+// does not depend on the rows beside it.
+constexpr int kHypPart = 384;
+constexpr int kHypParts = (kCtx + kHypPart - 1) / kHypPart;
+static_assert(2 * ((kTextCtx + kHypPart - 1) / kHypPart) <= kHypParts, "records of the self attention");
+
+Hypotheses plan_hypotheses(const asr_ctx* c, int32_t max_bias, int32_t n_masks) {
+  const asr_model_cfg& g = c->cfg;
+  const size_t S = std::max(1, g.max_slots), D = std::max(1, g.max_decode), V = std::max(1, g.vocab);
+  Hypotheses h;
+  h.max_bias = max_bias;
+  h.n_masks = n_masks;
+  Bump b;
+  h.history = b.take(S * kTextCtx * 4);
+  for (size_t* a : {&h.history_len, &h.prompt_len, &h.mask_of, &h.bias_len, &h.repetition, &h.frequency, &h.presence,
+                    &h.temperature})
+    *a = b.take(S * 4);
+  h.bias_token = b.take((S + 1) * max_bias * 4);       // the last row: the rules a slot starts with
+  h.bias_value = b.take((S + 1) * max_bias * 4);
+  h.mask = b.take((size_t)n_masks * ((V + 31) / 32) * 4);
+  h.step = b.take((kRuleScalars * D + 5 * D + 1) * 4);
+  h.token = b.take(D * kRulesMaxK * 4);
+  h.logprob = b.take(D * kRulesMaxK * 4);
+  h.rules_ws_size = rules_ws_bytes((int)D, (int)V, kRulesMaxK);
+  h.rules_ws = b.take(h.rules_ws_size);
+  h.share_ws_size = D * g.n_head * kHypParts * (kHeadDim + 2) * 4;
+  h.share_ws = b.take(h.share_ws_size);
+  h.total = (b.off + 255) / 256 * 256;
+  return h;
 }
 
 // ---------------------------------------------------------------------------
@@ -817,8 +889,9 @@ void drows(asr_ctx* c, int D, int N, int K, double xy_bytes, F&& f) {
 }
 
 template <typename T>
-asr_status decode_rows(asr_ctx* c, int D, const std::vector<int32_t>& pos_host, bool want_logits) {
+asr_status decode_rows(asr_ctx* c, const StepShape& sh, const std::vector<int32_t>& pos_host, bool want_logits) {
   const asr_model_cfg& g = c->cfg;
+  const int D = sh.D, alone = D - sh.shared;           // rows with caches of their own come first
   const int d = g.d_model, F = g.d_ffn, H = g.n_head, V = g.vocab;
   const Layout& L = c->L;
   hipStream_t s = c->stream;
@@ -832,9 +905,54 @@ asr_status decode_rows(asr_ctx* c, int D, const std::vector<int32_t>& pos_host, 
   const int32_t *tokens = slots + D, *pos = tokens + D;
   T* self_cache = c->at<T>(L.self_kv);
   T* cross_cache = c->at<T>(L.cross_kv);
-  double self_keys = 0;
-  for (int i = 0; i < D; ++i) self_keys += pos_host[i] + 1;
+  const double self_keys = (double)sh.self_keys;
+  double self_scores = 0;
+  for (int i = 0; i < D; ++i) self_scores += pos_host[i] + 1;
   const double Dd = (double)D * d;
+  // hypotheses: what the step's second upload holds
+  const Hypotheses& hy = c->hyp;
+  auto hat = [&](size_t off) { return (int32_t*)(hy.base + off); };
+  const int32_t* scalars = hy.base ? hat(hy.step) : nullptr;
+  const int32_t *own_first = scalars + kRuleScalars * D, *own_len = own_first + sh.shared;
+  const int32_t *group_start = own_len + sh.shared, *group_slot = group_start + sh.groups + 1,
+                *group_len = group_slot + sh.groups;
+  // attention of the hypotheses' rows over their family's keys and their own
+  auto attend_family = [&](const T* cache, int64_t stride, int64_t layer_off, int positions, bool self, int64_t q_ld) {
+    asr_attention a{};
+    a.dtype = g.dtype;
+    a.n_head = a.n_kv_head = H;
+    a.rows = sh.shared;
+    a.groups = sh.groups;
+    a.max_group = sh.group;
+    a.max_prefix = positions;
+    a.max_own = self ? positions : 0;
+    a.part_keys = kHypPart;
+    a.scale = 0.125f;
+    a.q = qkv + (int64_t)alone * q_ld;
+    a.q_ld = q_ld;
+    a.out = att + (int64_t)alone * d;
+    a.out_ld = d;
+    a.group_start = group_start;
+    const T* k = cache + layer_off;
+    a.prefix = {k, k + (int64_t)H * positions * kHeadDim, stride, (int64_t)positions * kHeadDim, kHeadDim,
+                g.max_slots, positions, group_slot, nullptr, self ? group_len : nullptr};
+    if (self) {
+      a.own = a.prefix;
+      a.own.slot = slots + alone;
+      a.own.first = own_first;
+      a.own.len = own_len;
+    }
+    return asr_attend_shared(&a, hy.base + hy.share_ws, hy.share_ws_size, s);
+  };
+  asr_status family_st = ASR_OK;
+  auto keep = [&](asr_status st) {
+    if (family_st == ASR_OK) family_st = st;
+  };
+  const SlotRuleArrays rule_arrays{hat(hy.history), hat(hy.history_len), hat(hy.prompt_len), hat(hy.mask_of),
+                                   hat(hy.bias_len), (float*)hat(hy.repetition), (float*)hat(hy.frequency),
+                                   (float*)hat(hy.presence), (float*)hat(hy.temperature)};
+  if (hy.base)
+    timed(c, ASR_K_OTHER, 0.0, 0.0, [&] { note_rows(rule_arrays, slots, tokens, pos, scalars, D, s); });
 
   timed(c, ASR_K_OTHER, 0.0, Dd * (c->es + 8), [&] {
     embed<T>(c->at<T>(L.tok_emb), c->at<float>(L.pos_emb), tokens, pos, D, d,
@@ -873,21 +991,27 @@ asr_status decode_rows(asr_ctx* c, int D, const std::vector<int32_t>& pos_host, 
     const DecLayer& w = L.dec[l];
     norm_product(w.ln1_g, w.ln1_b, w.qkv_w, w.qkv_b, 3 * d, false, qkv);
     const int64_t self_off = (int64_t)l * 2 * H * kTextCtx * kHeadDim;
-    timed(c, ASR_K_DATTN, 4.0 * self_keys * 64 * H, self_keys * 2 * 64 * H * c->es, [&] {
-      decode_self_attn<T>(qkv, self_cache, L.self_stride, self_off, slots, pos, D, H, att, s);
+    timed(c, ASR_K_DATTN, 4.0 * self_scores * 64 * H, self_keys * 2 * 64 * H * c->es, [&] {
+      decode_self_attn<T>(qkv, self_cache, L.self_stride, self_off, slots, pos, alone, H, att, s);
+      if (sh.shared > 0) {
+        decode_append_kv<T>(qkv + (int64_t)alone * 3 * d, self_cache, L.self_stride, self_off, slots + alone,
+                            pos + alone, sh.shared, H, s);
+        keep(attend_family(self_cache, L.self_stride, self_off, kTextCtx, true, 3 * d));
+      }
     });
     resid_product(att, w.o_w, w.o_b);
     norm_product(w.lnx_g, w.lnx_b, w.xq_w, w.xq_b, d, false, qkv);
     const int64_t cross_off = (int64_t)l * 2 * H * kCtx * kHeadDim;
-    timed(c, ASR_K_DATTN, 4.0 * Dd * kCtx, Dd * kCtx * 2 * c->es, [&] {
-      decode_cross_attn<T>(qkv, cross_cache, L.cross_stride, cross_off, slots, D, H, part, s);
+    timed(c, ASR_K_DATTN, 4.0 * Dd * kCtx, (double)(alone + sh.groups) * d * kCtx * 2 * c->es, [&] {
+      decode_cross_attn<T>(qkv, cross_cache, L.cross_stride, cross_off, slots, alone, H, part, s);
+      if (sh.shared > 0) keep(attend_family(cross_cache, L.cross_stride, cross_off, kCtx, false, d));
     });
-    if (D <= kMergeRows) {
+    if (D <= kMergeRows && sh.shared == 0) {
       drows<T>(c, D, d, d, Dd * (c->es + 8), [&] {
         rows_merge_resid<T>(part, c->at<T>(w.xo_w), c->at<float>(w.xo_b), D, d, h, s);
       });
     } else {
-      timed(c, ASR_K_DATTN, 0.0, 0.0, [&] { decode_cross_merge<T>(part, D, H, att, s); });
+      timed(c, ASR_K_DATTN, 0.0, 0.0, [&] { decode_cross_merge<T>(part, alone, H, att, s); });
       resid_product(att, w.xo_w, w.xo_b);
     }
     norm_product(w.ln2_g, w.ln2_b, w.fc1_w, w.fc1_b, F, true, hid);
@@ -914,7 +1038,7 @@ asr_status decode_rows(asr_ctx* c, int D, const std::vector<int32_t>& pos_host, 
           if (c->bf16()) {
             vocab_argmax_bf16((const bf16_t*)xn, c->at<bf16_t>(L.tok_emb), D, V, d,
                               c->at<uint64_t>(L.d_keys), nt,
-                              want_logits ? c->at<float>(L.d_logits) : nullptr, c->stream);
+                              want_logits || sh.k > 0 ? c->at<float>(L.d_logits) : nullptr, c->stream);
           } else {
             vocab_logits_f32((const float*)xn, c->at<float>(L.tok_emb), D, V, d,
                              c->at<float>(L.d_logits), c->stream);
@@ -923,7 +1047,42 @@ asr_status decode_rows(asr_ctx* c, int D, const std::vector<int32_t>& pos_host, 
           }
           argmax_finish(c->at<uint64_t>(L.d_keys), D, nt, c->at<int32_t>(L.d_argmax),
                         c->stream);
+          if (sh.k > 0) {
+            asr_rules r{};
+            r.dtype = ASR_F32;
+            r.rows = D;
+            r.vocab = V;
+            r.sets = g.max_slots;
+            r.masks = hy.n_masks;
+            r.k = sh.k;
+            r.logits = c->at<float>(L.d_logits);
+            r.ld = V;
+            r.set = slots;
+            r.history = rule_arrays.history;
+            r.history_ld = kTextCtx;
+            r.history_len = rule_arrays.history_len;
+            r.prompt_len = rule_arrays.prompt_len;
+            r.repetition = rule_arrays.repetition;
+            r.frequency = rule_arrays.frequency;
+            r.presence = rule_arrays.presence;
+            r.temperature = rule_arrays.temperature;
+            if (hy.max_bias > 0) {
+              r.bias_token = hat(hy.bias_token);
+              r.bias_value = (const float*)hat(hy.bias_value);
+              r.bias_ld = hy.max_bias;
+              r.bias_len = rule_arrays.bias_len;
+            }
+            if (hy.n_masks > 0) {
+              r.mask = (const uint32_t*)hat(hy.mask);
+              r.mask_ld = (V + 31) / 32;
+              r.mask_of = rule_arrays.mask_of;
+            }
+            r.token = hat(hy.token);
+            r.logprob = (float*)hat(hy.logprob);
+            keep(asr_logit_rules(&r, hy.base + hy.rules_ws, hy.rules_ws_size, s));
+          }
         });
+  if (family_st != ASR_OK) return family_st;
   CHECK_LAUNCH();
   return ASR_OK;
 }
@@ -944,11 +1103,36 @@ int32_t steps_for(int64_t n_samples, int32_t max_tokens) {
   return (int32_t)s;
 }
 
+// A slot whose caches others read is not free, occupied or not.
 int free_slot(asr_ctx* c, const std::vector<int>& taken) {
   for (int s = 0; s < c->cfg.max_slots; ++s)
-    if (!c->slots[s].occupied && std::find(taken.begin(), taken.end(), s) == taken.end())
+    if (!c->slots[s].occupied && c->family[s].kids == 0 && std::find(taken.begin(), taken.end(), s) == taken.end())
       return s;
   return -1;
+}
+
+// The slot reads its root's caches no longer.
+void leave_family(asr_ctx* c, int slot) {
+  const int root = c->family[slot].root;
+  if (root < 0) return;
+  c->family[slot].root = -1;
+  if (--c->family[root].kids == 0) c->family[root].shared = 0;
+}
+
+bool in_family(const asr_ctx* c, int slot) { return c->family[slot].root >= 0 || c->family[slot].kids > 0; }
+
+// A slot that is filled anew starts with the default rules.
+asr_status start_rules(asr_ctx* c, int slot) {
+  c->rules[slot] = c->default_rules;
+  const Hypotheses& h = c->hyp;
+  const int n = c->rules[slot].n_bias;
+  if (!h.base || n == 0) return ASR_OK;
+  for (size_t off : {h.bias_token, h.bias_value}) {
+    char* rows = h.base + off;
+    HIPCHK(hipMemcpyAsync(rows + (size_t)slot * h.max_bias * 4, rows + (size_t)c->cfg.max_slots * h.max_bias * 4,
+                          (size_t)n * 4, hipMemcpyDeviceToDevice, c->stream));
+  }
+  return ASR_OK;
 }
 
 }  // namespace
@@ -993,6 +1177,8 @@ asr_status asr_create(const asr_model_cfg* cfg, int32_t device, asr_ctx** out) {
   c->device = device;
   c->es = g.dtype == ASR_BF16 ? 2 : 4;
   c->slots.assign(std::max(g.max_slots, 0), Slot());
+  c->family.assign(c->slots.size(), Family());
+  c->rules.assign(c->slots.size(), Rules());
   c->queue.set_policy(WaitQueue::FCFS, 0, 0);
   plan(c);
   *out = c;
@@ -1036,6 +1222,10 @@ asr_status asr_bind(asr_ctx* c, void* dev_block, size_t bytes, void* stream) {
   for (auto& kv : c->dgraph) (void)hipGraphExecDestroy(kv.second);
   c->dgraph.clear();
   c->dshape_seen.clear();
+  c->hyp = Hypotheses();
+  c->family.assign(c->slots.size(), Family());
+  c->rules.assign(c->slots.size(), Rules());
+  c->default_rules = Rules();
   c->base = (char*)dev_block;
   c->bytes = bytes;
   c->stream = (hipStream_t)stream;
@@ -1174,6 +1364,7 @@ asr_status asr_release_slot(asr_ctx* c, int32_t slot) {
   if (c->serve_mode) return fail(ASR_ESTATE, "context is in continuous-batching mode (asr_serve_*)");
   if (slot < 0 || slot >= c->cfg.max_slots) return fail(ASR_ENOTFOUND, "no such slot");
   c->slots[slot] = Slot();
+  leave_family(c, slot);
   return ASR_OK;
 }
 
@@ -1251,19 +1442,19 @@ asr_status run_prefill(asr_ctx* c, const std::vector<const Request*>& reqs,
   return st;
 }
 
-// Enqueues the decode kernels of D rows on c->stream: directly, or by
-// replaying the HIP graph of this shape.  Every argument of those kernels is
-// a device pointer or a size fixed by (D, logits wanted) -- positions, slots
+// Enqueues the decode kernels of a step on c->stream: directly, or by
+// replaying the HIP graph of its shape.  Every argument of those kernels is
+// a device pointer or a size fixed by (shape, logits wanted) -- positions, slots
 // and tokens are read from device memory -- so one graph serves every step of
 // a shape.  A shape's first step runs directly (it also performs the
 // kernels' one-time attribute set-up); the second is captured on a private
 // stream and replayed from then on.  Per-launch timing always runs directly.
-asr_status decode_launch(asr_ctx* c, int D, const std::vector<int32_t>& pos, bool want_logits) {
+asr_status decode_launch(asr_ctx* c, const StepShape& sh, const std::vector<int32_t>& pos, bool want_logits) {
   auto direct = [&]() {
-    return c->bf16() ? decode_rows<bf16_t>(c, D, pos, want_logits)
-                     : decode_rows<float>(c, D, pos, want_logits);
+    return c->bf16() ? decode_rows<bf16_t>(c, sh, pos, want_logits)
+                     : decode_rows<float>(c, sh, pos, want_logits);
   };
-  const int32_t key = D * 2 + (want_logits ? 1 : 0);
+  const int64_t key = sh.key(want_logits);
   const bool per_launch_timing = (c->timing & ~((1 << ASR_K_PREFILL) | (1 << ASR_K_DECODE) |
                                                 (1 << ASR_K_ENCODE))) != 0;
   if (!c->decode_graphs || per_launch_timing) return direct();
@@ -1293,54 +1484,156 @@ asr_status decode_launch(asr_ctx* c, int D, const std::vector<int32_t>& pos, boo
   return ASR_OK;
 }
 
-// Enqueues a step of D rows ([3][D]: slots, tokens, positions) and the copies of
-// its results.
-asr_status enqueue_decode(asr_ctx* c, int D, const std::vector<int32_t>& rows,
-                          const std::vector<int32_t>& pos, int32_t* argmax, float* logits) {
+// What a step uploads and brings back.
+struct StepIO {
+  std::vector<int32_t> rows;     // [3][D]: slots, tokens, positions
+  std::vector<int32_t> extra;    // for the hypotheses block: see decode_rows
+  std::vector<int32_t> order;    // the caller's row of each of the step's
+  std::vector<int32_t> best;     // [D][k]
+  std::vector<float> logprob;    // [D][k]
+};
+
+// Enqueues a step and the copies of its results (logits: the caller's, a row of
+// the step to order's row).
+asr_status enqueue_decode(asr_ctx* c, const StepShape& sh, StepIO& io, const std::vector<int32_t>& pos, int32_t* argmax,
+                          float* logits) {
   hipStream_t s = c->stream;
-  HIPCHK(hipMemcpyAsync(c->at(c->L.d_rows), rows.data(), rows.size() * 4, hipMemcpyHostToDevice, s));
+  const int D = sh.D;
+  HIPCHK(hipMemcpyAsync(c->at(c->L.d_rows), io.rows.data(), io.rows.size() * 4, hipMemcpyHostToDevice, s));
+  if (!io.extra.empty())
+    HIPCHK(hipMemcpyAsync(c->hyp.base + c->hyp.step, io.extra.data(), io.extra.size() * 4, hipMemcpyHostToDevice, s));
   PhaseMark pm(c, ASR_K_DECODE);
-  asr_status st = decode_launch(c, D, pos, logits != nullptr);
+  asr_status st = decode_launch(c, sh, pos, logits != nullptr);
   if (st != ASR_OK) return st;
   pm.end();
-  HIPCHK(hipMemcpyAsync(argmax, c->at(c->L.d_argmax), D * 4, hipMemcpyDeviceToHost, s));
-  if (logits)
-    HIPCHK(hipMemcpyAsync(logits, c->at(c->L.d_logits), (size_t)D * c->cfg.vocab * 4,
+  if (sh.k > 0) {
+    HIPCHK(hipMemcpyAsync(io.best.data(), c->hyp.base + c->hyp.token, io.best.size() * 4, hipMemcpyDeviceToHost, s));
+    HIPCHK(hipMemcpyAsync(io.logprob.data(), c->hyp.base + c->hyp.logprob, io.logprob.size() * 4,
                           hipMemcpyDeviceToHost, s));
+  } else {
+    HIPCHK(hipMemcpyAsync(argmax, c->at(c->L.d_argmax), D * 4, hipMemcpyDeviceToHost, s));
+  }
+  if (logits) {
+    const size_t V = c->cfg.vocab;
+    if (sh.shared == 0) {
+      HIPCHK(hipMemcpyAsync(logits, c->at(c->L.d_logits), D * V * 4, hipMemcpyDeviceToHost, s));
+    } else {
+      for (int i = 0; i < D; ++i)
+        HIPCHK(hipMemcpyAsync(logits + io.order[i] * V, c->at<float>(c->L.d_logits) + i * V, V * 4,
+                              hipMemcpyDeviceToHost, s));
+    }
+  }
   return ASR_OK;
 }
 
-// Decode rows (slot, token, position) -> argmax (and logits when asked).
-// Returns EDEVICE after the copies when an argmax is a NaN logit's.  The rows
+// The step of the caller's rows: hypotheses behind the others, family by family,
+// and what the hypotheses block needs to know of them.
+StepShape arrange_rows(asr_ctx* c, int D, const int32_t* slots, const int32_t* tokens, const std::vector<int32_t>& pos,
+                       int k, StepIO& io) {
+  StepShape sh;
+  sh.D = D;
+  auto root_of = [&](int i) { return c->family[slots[i]].root >= 0 ? c->family[slots[i]].root : slots[i]; };
+  std::vector<int32_t>& order = io.order;
+  for (int i = 0; i < D; ++i)
+    if (!in_family(c, slots[i])) order.push_back(i);
+  const int alone = (int)order.size();
+  for (int i = 0; i < D; ++i)
+    if (in_family(c, slots[i])) order.push_back(i);
+  std::stable_sort(order.begin() + alone, order.end(), [&](int a, int b) { return root_of(a) < root_of(b); });
+  sh.shared = D - alone;
+  for (int i : order) io.rows.push_back(slots[i]);
+  for (int i : order) io.rows.push_back(tokens[i]);
+  for (int i : order) io.rows.push_back(pos[i]);
+  sh.k = k;
+  for (int j = 0; j < D; ++j)
+    sh.self_keys += pos[order[j]] + 1 - (j < alone ? 0 : c->family[root_of(order[j])].shared);
+  if (!c->hyp.base) return sh;
+  for (int i : order)
+    if (sh.k == 0 && c->rules[slots[i]].active) sh.k = 1;
+  std::vector<int32_t>& x = io.extra;
+  auto as_int = [](float f) {
+    int32_t v;
+    std::memcpy(&v, &f, 4);
+    return v;
+  };
+  for (int i : order) x.push_back(c->rules[slots[i]].n_prompt);
+  for (int i : order) x.push_back(c->rules[slots[i]].mask);
+  for (int i : order) x.push_back(c->rules[slots[i]].n_bias);
+  for (int i : order) x.push_back(as_int(c->rules[slots[i]].repetition));
+  for (int i : order) x.push_back(as_int(c->rules[slots[i]].frequency));
+  for (int i : order) x.push_back(as_int(c->rules[slots[i]].presence));
+  for (int i : order) x.push_back(as_int(c->rules[slots[i]].temperature));
+  if (sh.shared > 0) {
+    std::vector<int32_t> start, root, len;
+    for (int j = alone; j < D; ++j) {
+      const int r = root_of(order[j]);
+      if (root.empty() || root.back() != r) {
+        start.push_back(j - alone);
+        root.push_back(r);
+        len.push_back(c->family[r].shared);
+        sh.self_keys += len.back();
+      }
+      sh.group = std::max(sh.group, j - alone - start.back() + 1);
+    }
+    sh.groups = (int)root.size();
+    start.push_back(sh.shared);
+    for (int j = alone; j < D; ++j) x.push_back(c->family[root_of(order[j])].shared);
+    for (int j = alone; j < D; ++j) x.push_back(pos[order[j]] + 1 - c->family[root_of(order[j])].shared);
+    x.insert(x.end(), start.begin(), start.end());
+    x.insert(x.end(), root.begin(), root.end());
+    x.insert(x.end(), len.begin(), len.end());
+  }
+  io.best.assign((size_t)D * sh.k, -1);
+  io.logprob.assign((size_t)D * sh.k, 0.f);
+  return sh;
+}
+
+// Decode rows (slot, token, position) -> argmax (and logits when asked, and the
+// k best tokens where k > 0).  Returns EDEVICE after the copies when an argmax is a
+// NaN logit's, or no token is allowed.  The rows
 // go up in one copy and their results down in one: each small copy is a trip of
 // its own through the queue (one tiny fp32 row: 282 us with five copies, a flag
 // to clear and a slower argmax, 256 with two).
 asr_status run_decode(asr_ctx* c, int D, const int32_t* slots, const int32_t* tokens,
-                      const std::vector<int32_t>& pos, int32_t* argmax, float* logits) {
+                      const std::vector<int32_t>& pos, int32_t* argmax, float* logits, int k = 0,
+                      int32_t* best = nullptr, float* logprob = nullptr) {
   if (D == 0) return ASR_OK;
-  std::vector<int32_t> rows(slots, slots + D);
-  rows.insert(rows.end(), tokens, tokens + D);
-  rows.insert(rows.end(), pos.begin(), pos.begin() + D);
-  const asr_status st = enqueue_decode(c, D, rows, pos, argmax, logits);
-  // also where the step failed half way: the copies enqueued by then use `rows`
+  StepIO io;
+  const StepShape sh = arrange_rows(c, D, slots, tokens, pos, k, io);
+  std::vector<int32_t> pos_step(D), am(D);
+  for (int i = 0; i < D; ++i) pos_step[i] = pos[io.order[i]];
+  const asr_status st = enqueue_decode(c, sh, io, pos_step, am.data(), logits);
+  // also where the step failed half way: the copies enqueued by then use the step's
   // and the caller's arrays
   const hipError_t synced = hipStreamSynchronize(c->stream);
   if (st != ASR_OK) return st;
   HIPCHK(synced);
-  bool nan = false;
-  for (int i = 0; i < D; ++i)
-    if (argmax[i] < 0) {
-      argmax[i] = -1 - argmax[i];
-      nan = true;
+  const char* bad = nullptr;
+  for (int i = 0; i < D; ++i) {
+    const int row = io.order[i];
+    if (sh.k == 0) {
+      if (am[i] < 0) bad = "NaN logit";
+      argmax[row] = am[i] < 0 ? -1 - am[i] : am[i];
+      continue;
     }
-  return nan ? fail(ASR_EDEVICE, "NaN logit") : ASR_OK;
+    argmax[row] = io.best[(size_t)i * sh.k];
+    if (argmax[row] < 0)
+      bad = "the rules of a row allow no token";
+    else if (std::isnan(io.logprob[(size_t)i * sh.k]))
+      bad = "NaN or infinite logit";
+    for (int j = 0; j < k; ++j) {
+      best[(size_t)row * k + j] = io.best[(size_t)i * k + j];
+      logprob[(size_t)row * k + j] = io.logprob[(size_t)i * k + j];
+    }
+  }
+  return bad ? fail(ASR_EDEVICE, bad) : ASR_OK;
 }
 
 }  // namespace
 
-extern "C" {
+namespace {
 
-asr_status asr_step(asr_ctx* c, const asr_step_in* in, asr_step_out* out) {
+asr_status step(asr_ctx* c, const asr_step_in* in, asr_step_out* out, int k, int32_t* best, float* logprob) {
   asr_status st = need_gpu(c, true);
   if (st != ASR_OK) return st;
   if (!in || !out) return fail(ASR_EINVAL, "NULL argument");
@@ -1395,10 +1688,12 @@ asr_status asr_step(asr_ctx* c, const asr_step_in* in, asr_step_out* out) {
       sl2.steps_left = steps_for(reqs[i]->n_samples, reqs[i]->max_tokens);
       out->slot_of[i] = taken[i];
       c->popped.erase(reqs[i]->id);
+      st = start_rules(c, taken[i]);
+      if (st != ASR_OK) return st;
     }
   }
   if (D > 0) {
-    asr_status dst = run_decode(c, D, in->slots, in->tokens, pos, out->argmax, in->logits);
+    asr_status dst = run_decode(c, D, in->slots, in->tokens, pos, out->argmax, in->logits, k, best, logprob);
     if (dst != ASR_OK && dst != ASR_EDEVICE) return dst;
     for (int i = 0; i < D; ++i) {
       Slot& sl2 = c->slots[in->slots[i]];
@@ -1409,6 +1704,168 @@ asr_status asr_step(asr_ctx* c, const asr_step_in* in, asr_step_out* out) {
     if (dst != ASR_OK) return dst;
   }
   return collect_timing(c);
+}
+
+}  // namespace
+
+extern "C" {
+
+asr_status asr_step(asr_ctx* c, const asr_step_in* in, asr_step_out* out) {
+  return step(c, in, out, 0, nullptr, nullptr);
+}
+
+asr_status asr_step_topk(asr_ctx* c, const asr_step_in* in, asr_step_out* out, int32_t k, int32_t* tokens,
+                         float* logprobs) {
+  asr_status st = need_gpu(c, true);
+  if (st != ASR_OK) return st;
+  if (!c->hyp.base) return fail(ASR_ESTATE, "asr_bind_hypotheses has not been called");
+  if (k < 1 || k > kRulesMaxK) return fail(ASR_EINVAL, "k out of [1, 16]");
+  if (!in || (in->n_decode > 0 && (!tokens || !logprobs))) return fail(ASR_EINVAL, "NULL argument");
+  return step(c, in, out, k, tokens, logprobs);
+}
+
+// ---------------------------------------------------------------------------
+// Hypotheses and rules
+// ---------------------------------------------------------------------------
+asr_status asr_hypotheses_size(const asr_ctx* c, int32_t max_bias, int32_t n_masks, size_t* bytes) {
+  if (!c || !bytes) return fail(ASR_EINVAL, "NULL argument");
+  if (max_bias < 0 || max_bias > (1 << 20) || n_masks < 0 || n_masks > (1 << 20))
+    return fail(ASR_EINVAL, "max_bias and n_masks out of [0, 1048576]");
+  if (c->cfg.n_dec == 0 || c->cfg.max_decode == 0) return fail(ASR_EINVAL, "context does not decode");
+  if (c->cfg.vocab > kRulesMaxVocab) return fail(ASR_EINVAL, "vocabulary above 1048576");
+  *bytes = plan_hypotheses(c, max_bias, n_masks).total;
+  return ASR_OK;
+}
+
+asr_status asr_bind_hypotheses(asr_ctx* c, int32_t max_bias, int32_t n_masks, void* dev_block, size_t bytes) {
+  asr_status st = need_gpu(c, false);
+  if (st != ASR_OK) return st;
+  size_t need = 0;
+  st = asr_hypotheses_size(c, max_bias, n_masks, &need);
+  if (st != ASR_OK) return st;
+  if (!dev_block || ((uintptr_t)dev_block & 255)) return fail(ASR_EINVAL, "block must be 256-byte aligned");
+  if (bytes < need) return fail(ASR_ENOMEM, "bound block smaller than asr_hypotheses_size");
+  for (int i = 0; i < c->cfg.max_slots; ++i)
+    if (in_family(c, i)) return fail(ASR_ESTATE, "slots are hypotheses (release them first)");
+  HIPCHK(hipSetDevice(c->device));
+  // (steps captured without the block, or with another, are of no use)
+  HIPCHK(hipStreamSynchronize(c->stream));
+  for (auto& kv : c->dgraph) (void)hipGraphExecDestroy(kv.second);
+  c->dgraph.clear();
+  c->dshape_seen.clear();
+  c->hyp = plan_hypotheses(c, max_bias, n_masks);
+  c->hyp.base = (char*)dev_block;
+  c->rules.assign(c->slots.size(), Rules());
+  c->default_rules = Rules();
+  // no token known of any position, no token allowed by a mask not written yet
+  fill_u32((uint32_t*)(c->hyp.base + c->hyp.history), 0xffffffffu, (int64_t)c->cfg.max_slots * kTextCtx, c->stream);
+  if (n_masks > 0)
+    fill_u32((uint32_t*)(c->hyp.base + c->hyp.mask), 0u, (int64_t)n_masks * ((c->cfg.vocab + 31) / 32), c->stream);
+  CHECK_LAUNCH();
+  return ASR_OK;
+}
+
+asr_status asr_fork_slot(asr_ctx* c, int32_t src, int32_t dst) {
+  asr_status st = need_gpu(c, true);
+  if (st != ASR_OK) return st;
+  if (c->serve_mode) return fail(ASR_ESTATE, "context is in continuous-batching mode (asr_serve_*)");
+  const Hypotheses& h = c->hyp;
+  if (!h.base) return fail(ASR_ESTATE, "asr_bind_hypotheses has not been called");
+  const int S = c->cfg.max_slots;
+  if (src < 0 || src >= S || !c->slots[src].occupied) return fail(ASR_EINVAL, "source slot not occupied");
+  if (dst < 0 || dst >= S || dst == src) return fail(ASR_EINVAL, "destination slot out of range, or the source");
+  if (c->slots[dst].occupied || c->family[dst].kids > 0) return fail(ASR_EFULL, "destination slot is taken");
+  HIPCHK(hipSetDevice(c->device));
+  const int root = c->family[src].root >= 0 ? c->family[src].root : src;
+  const int pos = c->slots[src].pos;
+  const int shared = c->family[root].kids > 0 ? c->family[root].shared : pos;
+  hipStream_t s = c->stream;
+  const int blocks = c->cfg.n_dec * 2 * c->cfg.n_head;
+  auto copy = [&](auto tag) {
+    using T = decltype(tag);
+    T* cache = c->at<T>(c->L.self_kv);
+    copy_self_kv<T>(cache + (int64_t)src * c->L.self_stride, cache + (int64_t)dst * c->L.self_stride, blocks, shared,
+                    pos, s);
+  };
+  if (c->bf16())
+    copy(bf16_t());
+  else
+    copy(float());
+  CHECK_LAUNCH();
+  auto copy_row = [&](size_t off, size_t row, size_t n) {
+    char* p = h.base + off;
+    return n == 0 ? hipSuccess : hipMemcpyAsync(p + dst * row, p + src * row, n, hipMemcpyDeviceToDevice, s);
+  };
+  HIPCHK(copy_row(h.history, kTextCtx * 4, (size_t)pos * 4));
+  HIPCHK(copy_row(h.bias_token, (size_t)h.max_bias * 4, (size_t)c->rules[src].n_bias * 4));
+  HIPCHK(copy_row(h.bias_value, (size_t)h.max_bias * 4, (size_t)c->rules[src].n_bias * 4));
+  c->slots[dst] = c->slots[src];
+  c->rules[dst] = c->rules[src];
+  c->family[dst].root = root;
+  c->family[root].kids += 1;
+  c->family[root].shared = shared;
+  return ASR_OK;
+}
+
+asr_status asr_set_masks(asr_ctx* c, int32_t first, int32_t n, const uint32_t* words) {
+  asr_status st = need_gpu(c, false);
+  if (st != ASR_OK) return st;
+  const Hypotheses& h = c->hyp;
+  if (!h.base) return fail(ASR_ESTATE, "asr_bind_hypotheses has not been called");
+  if (first < 0 || n < 0 || first > h.n_masks - n) return fail(ASR_EINVAL, "rows out of the mask table");
+  if (n == 0) return ASR_OK;
+  if (!words) return fail(ASR_EINVAL, "NULL argument");
+  HIPCHK(hipSetDevice(c->device));
+  const size_t row = (size_t)((c->cfg.vocab + 31) / 32) * 4;
+  HIPCHK(hipMemcpyAsync(h.base + h.mask + first * row, words, n * row, hipMemcpyHostToDevice, c->stream));
+  HIPCHK(hipStreamSynchronize(c->stream));
+  return ASR_OK;
+}
+
+asr_status asr_set_slot_rules(asr_ctx* c, int32_t slot, const asr_slot_rules* r) {
+  asr_status st = need_gpu(c, false);
+  if (st != ASR_OK) return st;
+  const Hypotheses& h = c->hyp;
+  if (!h.base) return fail(ASR_ESTATE, "asr_bind_hypotheses has not been called");
+  if (slot < -1 || slot >= c->cfg.max_slots) return fail(ASR_EINVAL, "slot out of range");
+  if (slot >= 0 && c->serve_mode)
+    return fail(ASR_ESTATE, "context is in continuous-batching mode (asr_serve_*): its slots start with slot -1's rules");
+  if (slot >= 0 && !c->slots[slot].occupied) return fail(ASR_EINVAL, "slot not occupied");
+  Rules x;
+  if (r) {
+    if (!(r->repetition > 0.f) || !std::isfinite(r->repetition)) return fail(ASR_EINVAL, "repetition must be positive");
+    if (!(r->temperature > 0.f) || !std::isfinite(r->temperature)) return fail(ASR_EINVAL, "temperature must be positive");
+    if (!std::isfinite(r->frequency) || !std::isfinite(r->presence)) return fail(ASR_EINVAL, "penalties must be finite");
+    if (r->n_prompt < 0) return fail(ASR_EINVAL, "n_prompt must be >= 0");
+    if (r->mask < -1 || r->mask >= h.n_masks) return fail(ASR_EINVAL, "mask out of the mask table");
+    if (r->n_bias < 0 || r->n_bias > h.max_bias) return fail(ASR_EINVAL, "n_bias out of [0, max_bias]");
+    if (r->n_bias > 0 && (!r->bias_token || !r->bias_value)) return fail(ASR_EINVAL, "NULL biases");
+    for (int i = 0; i < r->n_bias; ++i)
+      if (r->bias_token[i] < 0 || r->bias_token[i] >= c->cfg.vocab || std::isnan(r->bias_value[i]))
+        return fail(ASR_EINVAL, "bias token out of the vocabulary, or its value a NaN");
+    x = {true, r->repetition, r->frequency, r->presence, r->temperature, r->n_prompt, r->mask, r->n_bias};
+    if (r->n_bias > 0) {
+      HIPCHK(hipSetDevice(c->device));
+      const size_t row = (size_t)(slot < 0 ? c->cfg.max_slots : slot) * h.max_bias * 4, n = (size_t)r->n_bias * 4;
+      HIPCHK(hipMemcpyAsync(h.base + h.bias_token + row, r->bias_token, n, hipMemcpyHostToDevice, c->stream));
+      HIPCHK(hipMemcpyAsync(h.base + h.bias_value + row, r->bias_value, n, hipMemcpyHostToDevice, c->stream));
+      HIPCHK(hipStreamSynchronize(c->stream));
+    }
+  }
+  (slot < 0 ? c->default_rules : c->rules[slot]) = x;
+  return ASR_OK;
+}
+
+asr_status asr_set_slot_mask(asr_ctx* c, int32_t slot, int32_t mask) {
+  asr_status st = need_gpu(c, false);
+  if (st != ASR_OK) return st;
+  if (!c->hyp.base) return fail(ASR_ESTATE, "asr_bind_hypotheses has not been called");
+  if (slot < 0 || slot >= c->cfg.max_slots || !c->slots[slot].occupied) return fail(ASR_EINVAL, "slot not occupied");
+  if (c->serve_mode) return fail(ASR_ESTATE, "context is in continuous-batching mode (asr_serve_*)");
+  if (mask < -1 || mask >= c->hyp.n_masks) return fail(ASR_EINVAL, "mask out of the mask table");
+  c->rules[slot].mask = mask;
+  c->rules[slot].active = true;
+  return ASR_OK;
 }
 
 // ---------------------------------------------------------------------------
@@ -1554,6 +2011,10 @@ asr_status asr_serve_step(asr_ctx* c, int64_t now_us, asr_serve_out* out) {
   }
   const int D = (int)p.dec_id.size(), A = (int)p.admitted.size();
   std::vector<int32_t> tok(D);
+  for (int32_t slot : p.admitted_slot) {
+    st = start_rules(c, slot);
+    if (st != ASR_OK) return st;
+  }
   if (c->serve_overlap && A > 0 && D > 0) {
     // With overlap the engine defers an admitted request's first token to
     // the next step, so this step's decode rows do not depend on its prefill:
@@ -1817,6 +2278,7 @@ asr_status asr_debug_set_encoder_out(asr_ctx* c, const int32_t* slots, const int
     if (slots[i] < 0 || slots[i] >= c->cfg.max_slots) return fail(ASR_EINVAL, "slot out of range");
     for (int j = 0; j < i; ++j)
       if (slots[j] == slots[i]) return fail(ASR_EINVAL, "duplicate slot");
+    if (c->family[slots[i]].kids > 0) return fail(ASR_EINVAL, "slot's caches are read by hypotheses");
     if (ids[i] >= 0 && !c->popped.count(ids[i])) return fail(ASR_EINVAL, "id was not popped");
     if (steps_left[i] < 1 || steps_left[i] > kTextCtx) return fail(ASR_EINVAL, "steps_left out of [1, 448]");
   }
@@ -1842,6 +2304,9 @@ asr_status asr_debug_set_encoder_out(asr_ctx* c, const int32_t* slots, const int
     sl.id = ids[i];
     sl.pos = 0;
     sl.steps_left = steps_left[i];
+    leave_family(c, slots[i]);
+    st = start_rules(c, slots[i]);
+    if (st != ASR_OK) return st;
     if (ids[i] >= 0) c->popped.erase(ids[i]);
   }
   return collect_timing(c);
@@ -1855,7 +2320,17 @@ asr_status asr_debug_get_kv(asr_ctx* c, int32_t slot, int32_t which, float* out)
   if (which != 0 && which != 1) return fail(ASR_EINVAL, "which must be 0 (self) or 1 (cross)");
   HIPCHK(hipSetDevice(c->device));
   const int64_t cnt = which == 0 ? c->L.self_stride : c->L.cross_stride;
-  const size_t off = (which == 0 ? c->L.self_kv : c->L.cross_kv) + (size_t)slot * cnt * c->es;
+  const int root = c->family[slot].root;
+  if (root >= 0 && which == 0) {
+    // a hypothesis's shared positions are its root's; its own copy of them is never read
+    const int blocks = c->cfg.n_dec * 2 * c->cfg.n_head, n = c->family[root].shared;
+    if (c->bf16())
+      copy_self_kv<bf16_t>(c->at<bf16_t>(c->L.self_kv) + root * cnt, c->at<bf16_t>(c->L.self_kv) + slot * cnt, blocks, 0, n, c->stream);
+    else
+      copy_self_kv<float>(c->at<float>(c->L.self_kv) + root * cnt, c->at<float>(c->L.self_kv) + slot * cnt, blocks, 0, n, c->stream);
+  }
+  const int from = root >= 0 && which == 1 ? root : slot;
+  const size_t off = (which == 0 ? c->L.self_kv : c->L.cross_kv) + (size_t)from * cnt * c->es;
   float* tmp = c->at<float>(c->L.wstage);
   if (c->bf16())
     convert_to_f32<bf16_t>(c->at<bf16_t>(off), tmp, cnt, c->stream);
@@ -1875,7 +2350,10 @@ asr_status asr_debug_set_self_kv(asr_ctx* c, int32_t slot, const float* src, int
   if (slot < 0 || slot >= c->cfg.max_slots) return fail(ASR_EINVAL, "slot out of range");
   if (!c->slots[slot].occupied) return fail(ASR_EINVAL, "slot not occupied");
   if (length < 0 || length >= kTextCtx) return fail(ASR_EINVAL, "length out of [0, 447]");
+  if (in_family(c, slot)) return fail(ASR_EINVAL, "slot shares its caches with hypotheses");
   HIPCHK(hipSetDevice(c->device));
+  if (c->hyp.base && length > 0)   // which tokens these positions are is not known
+    fill_u32((uint32_t*)(c->hyp.base + c->hyp.history) + (size_t)slot * kTextCtx, 0xffffffffu, length, c->stream);
   const int64_t cnt = c->L.self_stride;
   const size_t off = c->L.self_kv + (size_t)slot * cnt * c->es;
   float* tmp = c->at<float>(c->L.wstage);
