@@ -421,9 +421,9 @@ asr_status asr_bind_hypotheses(asr_ctx* ctx, int32_t max_bias, int32_t n_masks, 
 
 /* Makes the free slot dst a hypothesis of the sequence in src: the same
  * position, steps left, request id, tokens and rules.  The audio's cross cache
- * and the self cache up to the position of the family's first fork stay where
- * they are and are shared: a step reads them once for all of a family's rows
- * (asr_attend_shared).  What src has decoded since is copied.  Slots of a
+ * and a prompt of 128 positions or more (the self cache up to the position of the
+ * family's first fork) stay where they are and are shared: a step reads them
+ * once for all of a family's rows (asr_attend_shared).  The rest is copied.  Slots of a
  * family decode, fork and are released in any order; a slot whose caches others
  * read stays taken after its release until they are released too
  * (asr_slot_info shows it free, prefill passes it over).  Its caches cannot be

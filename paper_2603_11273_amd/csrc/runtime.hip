@@ -60,7 +60,13 @@ struct Slot {
 
 // A slot's place in a family of hypotheses: `root` holds the cross cache that
 // all of them read and the self cache of positions below the root's `shared`;
-// `kids` counts the slots that read this one's (beside itself).
+// `kids` counts the slots that read this one's (beside itself).  Prompts below
+// kShareFrom positions are copied instead (shared = 0): sharing them takes two
+// launches more a layer, about what reading 120 rows' 128 positions costs
+// (large-v3).  A step of one family of 5 on 40 positions: 1869 us with them
+// shared, 1672 with them copied (1638 as slots of their own); of 24 on 224
+// positions: 4103 with them shared, about 4450 copied (8226).
+constexpr int kShareFrom = 128;
 struct Family {
   int32_t root = -1;      // -1: the slot's own caches
   int32_t kids = 0;
@@ -86,12 +92,15 @@ struct Hypotheses {
 };
 
 // A decode step: D rows, the last `shared` of them hypotheses in `groups`
-// families of at most `group` rows; k best tokens under rules (0: the argmax).
+// families of at most `group` rows, the last `prompts` families (`prompt_rows`
+// rows) with shared prompts; k best tokens under rules (0: the argmax).
 struct StepShape {
-  int D = 0, shared = 0, groups = 0, group = 0, k = 0;
+  int D = 0, shared = 0, groups = 0, group = 0, prompts = 0, prompt_rows = 0, k = 0;
   int64_t self_keys = 0;   // positions of self caches that the step reads (a family's shared ones once)
   int64_t key(bool logits) const {
-    return (((((int64_t)D * 256 + shared) * 256 + groups) * 256 + group) * 32 + k) * 2 + (logits ? 1 : 0);
+    int64_t x = 0;
+    for (int v : {D, shared, groups, group, prompts, prompt_rows}) x = x * 256 + v;   // each at most 128
+    return (x * 32 + k) * 2 + (logits ? 1 : 0);
   }
 };
 
@@ -921,8 +930,9 @@ asr_status decode_rows(asr_ctx* c, const StepShape& sh, const std::vector<int32_
     asr_attention a{};
     a.dtype = g.dtype;
     a.n_head = a.n_kv_head = H;
+    const int skip = self ? sh.groups - sh.prompts : 0;   // (rows in no group are left as they are)
     a.rows = sh.shared;
-    a.groups = sh.groups;
+    a.groups = sh.groups - skip;
     a.max_group = sh.group;
     a.max_prefix = positions;
     a.max_own = self ? positions : 0;
@@ -932,10 +942,10 @@ asr_status decode_rows(asr_ctx* c, const StepShape& sh, const std::vector<int32_
     a.q_ld = q_ld;
     a.out = att + (int64_t)alone * d;
     a.out_ld = d;
-    a.group_start = group_start;
+    a.group_start = group_start + skip;
     const T* k = cache + layer_off;
     a.prefix = {k, k + (int64_t)H * positions * kHeadDim, stride, (int64_t)positions * kHeadDim, kHeadDim,
-                g.max_slots, positions, group_slot, nullptr, self ? group_len : nullptr};
+                g.max_slots, positions, group_slot + skip, nullptr, self ? group_len + skip : nullptr};
     if (self) {
       a.own = a.prefix;
       a.own.slot = slots + alone;
@@ -992,10 +1002,11 @@ asr_status decode_rows(asr_ctx* c, const StepShape& sh, const std::vector<int32_
     norm_product(w.ln1_g, w.ln1_b, w.qkv_w, w.qkv_b, 3 * d, false, qkv);
     const int64_t self_off = (int64_t)l * 2 * H * kTextCtx * kHeadDim;
     timed(c, ASR_K_DATTN, 4.0 * self_scores * 64 * H, self_keys * 2 * 64 * H * c->es, [&] {
-      decode_self_attn<T>(qkv, self_cache, L.self_stride, self_off, slots, pos, alone, H, att, s);
-      if (sh.shared > 0) {
-        decode_append_kv<T>(qkv + (int64_t)alone * 3 * d, self_cache, L.self_stride, self_off, slots + alone,
-                            pos + alone, sh.shared, H, s);
+      const int plain = D - sh.prompt_rows;
+      decode_self_attn<T>(qkv, self_cache, L.self_stride, self_off, slots, pos, plain, H, att, s);
+      if (sh.prompts > 0) {
+        decode_append_kv<T>(qkv + (int64_t)plain * 3 * d, self_cache, L.self_stride, self_off, slots + plain,
+                            pos + plain, sh.prompt_rows, H, s);
         keep(attend_family(self_cache, L.self_stride, self_off, kTextCtx, true, 3 * d));
       }
     });
@@ -1539,7 +1550,11 @@ StepShape arrange_rows(asr_ctx* c, int D, const int32_t* slots, const int32_t* t
   const int alone = (int)order.size();
   for (int i = 0; i < D; ++i)
     if (in_family(c, slots[i])) order.push_back(i);
-  std::stable_sort(order.begin() + alone, order.end(), [&](int a, int b) { return root_of(a) < root_of(b); });
+  std::stable_sort(order.begin() + alone, order.end(), [&](int a, int b) {
+    const int ra = root_of(a), rb = root_of(b);
+    const bool pa = c->family[ra].shared > 0, pb = c->family[rb].shared > 0;
+    return pa != pb ? pb : ra < rb;
+  });
   sh.shared = D - alone;
   for (int i : order) io.rows.push_back(slots[i]);
   for (int i : order) io.rows.push_back(tokens[i]);
@@ -1572,7 +1587,9 @@ StepShape arrange_rows(asr_ctx* c, int D, const int32_t* slots, const int32_t* t
         root.push_back(r);
         len.push_back(c->family[r].shared);
         sh.self_keys += len.back();
+        sh.prompts += len.back() > 0;
       }
+      sh.prompt_rows += len.back() > 0;
       sh.group = std::max(sh.group, j - alone - start.back() + 1);
     }
     sh.groups = (int)root.size();
@@ -1778,7 +1795,7 @@ asr_status asr_fork_slot(asr_ctx* c, int32_t src, int32_t dst) {
   HIPCHK(hipSetDevice(c->device));
   const int root = c->family[src].root >= 0 ? c->family[src].root : src;
   const int pos = c->slots[src].pos;
-  const int shared = c->family[root].kids > 0 ? c->family[root].shared : pos;
+  const int shared = c->family[root].kids > 0 ? c->family[root].shared : pos >= kShareFrom ? pos : 0;
   hipStream_t s = c->stream;
   const int blocks = c->cfg.n_dec * 2 * c->cfg.n_head;
   auto copy = [&](auto tag) {

@@ -36,6 +36,13 @@ class Alone:
         self.args, self.ckv, self.st = (P, shape.n_dec, shape.n_head), ckv, OW.DecoderState(shape.n_dec, shape.d_model)
         self.tokens = []
 
+    def prefill(self, kv, n):
+        """Keys and values [n_dec][2][heads][448][64] of n positions whose tokens nobody knows."""
+        self.tokens = [-1] * n
+        for l in range(kv.shape[0]):
+            for which, cache in ((0, self.st.k), (1, self.st.v)):
+                cache[l] = kv[l, which, :, :n].astype(np.float64).transpose(1, 0, 2).reshape(n, -1)
+
     def step(self, token):
         P, n_dec, n_head = self.args
         self.tokens.append(int(token))
@@ -52,9 +59,10 @@ def clone(seq):
 
 @pytest.mark.parametrize("name,dtype", [("tiny", "f32"), ("base", "bf16")])
 @pytest.mark.parametrize("graphs", [False, True])
-def test_families_follow_the_oracle(name, dtype, graphs):
-    """Two clips; clip 0 grows a family of five over forks at positions 0, 3 and 6, of the root and of a
-    hypothesis, and loses its root; clip 1 decodes beside it alone."""
+@pytest.mark.parametrize("prompt", [0, 130])
+def test_families_follow_the_oracle(name, dtype, graphs, prompt):
+    """Two clips, with and without a prompt so long that a family shares it; clip 0 grows a family of five
+    over forks of the root and of a hypothesis, and loses its root; clip 1 decodes beside it alone."""
     shape, seed = shape_of(name, dtype), 20261101
     ctx, E = context(shape, seed, 8)
     ctx.set_decode_graphs(graphs)
@@ -62,6 +70,11 @@ def test_families_follow_the_oracle(name, dtype, graphs):
     ckv = [OW.cross_kv(e.astype(np.float64), P, shape.n_dec) for e in E]
     seqs = {0: Alone(shape, P, ckv[0]), 1: Alone(shape, P, ckv[1])}
     rng = np.random.default_rng(seed)
+    if prompt:
+        for s in (0, 1):
+            kv = synth.self_kv_prefix(seed, s, shape.n_dec, shape.n_head).numpy()
+            ctx.debug_set_self_kv(s, kv, prompt)
+            seqs[s].prefill(kv, prompt)
 
     def step(slots):
         tokens = rng.integers(0, V, len(slots))
@@ -86,13 +99,13 @@ def test_families_follow_the_oracle(name, dtype, graphs):
     fork(0, 3)
     for _ in range(3):
         step([3, 1, 0, 2])                         # the family's rows in no order, another row among them
-    fork(3, 4)                                     # has three tokens of its own: copied
+    fork(3, 4)                                     # after 1 + 3 + 3 tokens, three of its own: copied
     fork(0, 5)
     for _ in range(2):
         step([0, 1, 2, 3, 4, 5])
-    kv = ctx.debug_get_kv(4, 0)
-    own = ctx.debug_get_kv(3, 0)
-    assert np.array_equal(kv[:, :, :, :7], own[:, :, :, :7])
+    kv, own = ctx.debug_get_kv(4, 0), ctx.debug_get_kv(3, 0)
+    assert np.array_equal(kv[:, :, :, :prompt + 7], own[:, :, :, :prompt + 7])
+    assert not np.array_equal(kv[:, :, :, prompt + 7], own[:, :, :, prompt + 7])
     ctx.release_slot(0)                            # its caches stay: 2 to 5 read them
     del seqs[0]
     for _ in range(2):
@@ -105,11 +118,14 @@ def test_families_follow_the_oracle(name, dtype, graphs):
     step([4, 1])                                   # the last one reads its root's caches still
 
 
-def test_rows_beside_a_family_and_hypotheses_of_any_batch_keep_their_bits():
+@pytest.mark.parametrize("prompt", [0, 200])
+def test_rows_beside_a_family_and_hypotheses_of_any_batch_keep_their_bits(prompt):
     shape, seed = shape_of("base", "bf16"), 20261102
     got = []
     for plan in ("alone", "family"):
         ctx, _ = context(shape, seed, 8, bind=plan == "family")
+        if prompt:
+            ctx.debug_set_self_kv(0, synth.self_kv_prefix(seed, 0, shape.n_dec, shape.n_head).numpy(), prompt)
         rows = []
         for t in (5, 6, 7, 8):
             if plan == "family" and t == 6:
