@@ -472,8 +472,10 @@ asr_status asr_step_topk(asr_ctx* ctx, const asr_step_in* in, asr_step_out* out,
  * of the current device unless it says host, work is enqueued on `stream`
  * (NULL = default stream) and the calls neither allocate nor synchronise, so
  * they may be captured into graphs.  Scratch is the caller's: `ws` of at least
- * the bytes that the _size call gives, 256-byte aligned.  It carries nothing
- * from one call to the next; calls that may overlap need blocks of their own.
+ * the bytes that the _size call gives, 256-byte aligned, its first 16384 bytes
+ * zeros before its first call (they count blocks, and every call leaves them
+ * zeros).  Calls of any sizes may share one, one after the other; calls that may
+ * overlap need blocks of their own.
  * Sizes and pointers are checked (EINVAL, ENOMEM for a small ws); what lies in
  * device memory (lengths, slots, tokens) is kept in bounds by the kernels as
  * stated. */

@@ -239,7 +239,8 @@ def logmel_noalloc(clips, n_mels, out, stream=None):
 class _Operator:
     """What the plans of the stateless operators share: the tensors they keep, their scratch and
     the call.  Tensors are taken as they lie (no copies) and must stay where they are; what is in
-    them may change between calls."""
+    them may change between calls.  A workspace given to a plan starts as zeros; plans may share
+    one if their calls never overlap."""
 
     def __init__(self, device, workspace, size, run, args):
         import torch
@@ -253,7 +254,7 @@ class _Operator:
         self.workspace_bytes = n.value
         self._ws = workspace
         if workspace is None:
-            self._ws = torch.empty(max(n.value, 1), dtype=torch.uint8, device=device)
+            self._ws = torch.zeros(max(n.value, 1), dtype=torch.uint8, device=device)
         self._ws_ptr, self._ws_bytes = self._ws.data_ptr(), self._ws.numel()
 
     def _need(self, t, name, dtype, shape, device, ld=False):

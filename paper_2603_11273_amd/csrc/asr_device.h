@@ -267,4 +267,32 @@ __device__ __forceinline__ float wave_max_lanes(float v) {
   return from_ordered_u32(wave_max_u32(ordered_u32(v)));
 }
 
+// ---------------------------------------------------------------------------
+// Results that another block of the same launch reads
+// ---------------------------------------------------------------------------
+// The L2 caches of the XCDs are not kept alike for ordinary accesses, and a fence
+// over the device writes back and drops all of one (24 x 5 rows on 1500 keys:
+// 49 -> 553 us).  So only what is handed over goes past them: agent-scope stores
+// and loads, which are performed where all XCDs see them.  A block counts itself
+// once the stores of all its threads are (each waits for its own, then the
+// barrier); who counts last reads after that.
+template <typename V>
+__device__ __forceinline__ void store_agent(V* p, V v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename V>
+__device__ __forceinline__ V load_agent(const V* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// True in every thread of the last of `blocks` blocks to arrive; the counter, 0
+// before the first, goes round to 0 with the last.
+__device__ __forceinline__ bool arrive_last(uint32_t* counter, uint32_t blocks) {
+  __shared__ int last;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicInc(counter, blocks - 1) == blocks - 1;
+  __syncthreads();
+  return last;
+}
+
 }  // namespace asr

@@ -197,6 +197,9 @@ struct ShareLaunch {
   int32_t np, no, prefix_part, own_part;
   float* rec;
 };
+// Words at the start of every workspace of the decode operators: counters, zeros
+// between calls.
+constexpr int kCounters = 4096;
 hipError_t attend_shared(const ShareLaunch& a, bool bf16, hipStream_t s);
 // 16-column query tiles that a block holds, of `cols` queries of a group and cache head
 int share_query_tiles(int cols);
@@ -227,6 +230,9 @@ struct RulesLaunch {
   int32_t* token;
   float* logprob;
   float* ws;                                      // rules_ws_bytes
+  // zeros, one per row, left as zeros: the row's last block joins its blocks' results;
+  // NULL: a second kernel does
+  uint32_t* counters;
 };
 size_t rules_ws_bytes(int rows, int vocab, int k);
 void logit_rules(const RulesLaunch& a, bool bf16, hipStream_t s);

@@ -8,9 +8,12 @@
 // lists) and read back by the threads that own the tokens, so nothing of the
 // vocabulary's size is cleared, written or read besides the logits themselves.
 // The 256 threads leave their maximum, their sum of exponentials and their k best
-// tokens; a second, short kernel joins a row's.  HBM bounds a batch of rows, two
-// launches a single one; long histories would be read once for 4096 tokens, so
-// with those a block is 1024 threads with the same work each.
+// tokens; a row's last block joins them.  HBM bounds a batch of rows, a chain of
+// loads a single one; long histories would be read once for 4096 tokens, so
+// with those a block is 1024 threads with the same work each (and the join, which
+// would cost them registers, a kernel of its own).
+#include <algorithm>
+
 #include "asr_device.h"
 
 // Every operation below is rounded by itself, as the definition has it: two
@@ -123,8 +126,32 @@ __device__ __forceinline__ void count_tokens(const int32_t* list, int marked, in
   }
 }
 
-// The better of two results comes first.
-__device__ __forceinline__ bool better(uint2 a, uint2 b) { return a.x > b.x || (a.x == b.x && a.y < b.y); }
+// A result: the better of two is the larger one, 0 is none.
+__device__ __forceinline__ uint64_t result_of(uint32_t rank, int token) { return (uint64_t)rank << 32 | ~(uint32_t)token; }
+
+// What one block leaves for another to read (of the same launch where there are
+// counters).
+__device__ __forceinline__ void leave(const RulesLaunch& a, uint64_t* p, uint64_t v) {
+  if (a.counters)
+    store_agent(p, v);
+  else
+    *p = v;
+}
+__device__ __forceinline__ uint64_t left_by(const RulesLaunch& a, const uint64_t* p) {
+  return a.counters ? load_agent(p) : *p;
+}
+
+// How many of the first n lanes' results x are better than `mine`.
+__device__ __forceinline__ int better(uint64_t x, int n, uint64_t mine) {
+  int count = 0;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const uint64_t y = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(x >> 32), i) << 32 |
+                       (uint32_t)__builtin_amdgcn_readlane((uint32_t)x, i);
+    count += y > mine;
+  }
+  return count;
+}
 
 // A rank such that at least k of the lanes' largest ranks lie at or above it (1
 // where there are not so many above 0): the wave's k best do too, and few others.
@@ -142,10 +169,10 @@ constexpr int RU_CAND = 64;                  // candidates of a wave
 constexpr uint32_t kLowest = 0x00800000u;    // rank of the lowest finite float
 
 template <typename T, int SUBS>
-__device__ __forceinline__ void rules_block(const RulesLaunch& a, int chunks) {
+__device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
   constexpr int VEC = Logits<T>::VEC, NV = RU_E / VEC, NT = SUBS * RU_NT, TOKENS = SUBS * RU_CHUNK;
   extern __shared__ __attribute__((aligned(16))) uint32_t table[];   // [TOKENS] where there are lists
-  __shared__ uint2 cand[SUBS * 4][RU_CAND];
+  __shared__ uint64_t cand[SUBS * 4][RU_CAND];
   __shared__ int cand_n[SUBS * 4];
   __shared__ float wave_ms[SUBS * 4][2];
   const int tid = threadIdx.x % RU_NT, sub = threadIdx.x / RU_NT, lane = threadIdx.x & 63;
@@ -278,7 +305,7 @@ __device__ __forceinline__ void rules_block(const RulesLaunch& a, int chunks) {
       }
     }
   }
-  if (a.k == 0) return;
+  if (a.k == 0) return false;
   // past the vocabulary: -inf, whatever the rules made of it
   if (v0 + RU_CHUNK > V) {
 #pragma unroll
@@ -312,7 +339,7 @@ __device__ __forceinline__ void rules_block(const RulesLaunch& a, int chunks) {
       const uint64_t in = __ballot(z[i] >= least);
       if (!in) continue;
       const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0));
-      if (z[i] >= least && at < RU_CAND) cand[wave][at] = uint2{rank_of(z[i]), (uint32_t)token_of(i)};
+      if (z[i] >= least && at < RU_CAND) cand[wave][at] = result_of(rank_of(z[i]), token_of(i));
       n += __popcll(in);
     }
   }
@@ -333,28 +360,28 @@ __device__ __forceinline__ void rules_block(const RulesLaunch& a, int chunks) {
       const int l = best_lane(r, token_of(tok));
       if (l < 0) break;
       if (lane == l) {
-        cand[wave][n] = uint2{r, (uint32_t)token_of(tok)};
+        cand[wave][n] = result_of(r, token_of(tok));
         given |= 1u << tok;
       }
     }
   }
   if (lane == 0) cand_n[wave] = n;
   __syncthreads();
-  if (v0 >= V) return;
+  if (v0 >= V) return true;
   // the 256 threads': a candidate's place is the number of better ones
   const int chunk = blockIdx.x * SUBS + sub, w0 = wave & ~3;
-  uint2* keys = (uint2*)(a.ws + (int64_t)a.rows * chunks * 2) + ((int64_t)row * chunks + chunk) * a.k;
-  const uint2 mine = lane < n ? cand[wave][lane] : uint2{0u, 0u};
+  uint64_t* keys = (uint64_t*)(a.ws + (int64_t)a.rows * chunks * 2) + ((int64_t)row * chunks + chunk) * a.k;
+  const uint64_t mine = lane < n ? cand[wave][lane] : 0;
   int place = 0, have = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     const int m = __builtin_amdgcn_readfirstlane(cand_n[w0 + w]);
     have += m;
-    for (int i = 0; i < m; ++i) place += better(cand[w0 + w][i], mine);
+    place += better(lane < m ? cand[w0 + w][lane] : 0, m, mine);
   }
-  if (lane < n && place < a.k) keys[place] = mine;
+  if (lane < n && place < a.k) leave(a, keys + place, mine);
   if (wave == w0) {
-    if (lane >= have && lane < a.k) keys[lane] = uint2{0u, 0u};
+    if (lane >= have && lane < a.k) leave(a, keys + lane, 0);
     if (lane == 0) {
       float M = wave_ms[w0][0], S = 0.f;
 #pragma unroll
@@ -364,48 +391,49 @@ __device__ __forceinline__ void rules_block(const RulesLaunch& a, int chunks) {
         S += wave_ms[w0 + w][0] == M
                  ? wave_ms[w0 + w][1]
                  : wave_ms[w0 + w][1] * __builtin_amdgcn_exp2f((wave_ms[w0 + w][0] - M) * 1.4426950408889634f);
-      *((float2*)a.ws + (int64_t)row * chunks + chunk) = float2{M, S};
+      leave(a, (uint64_t*)a.ws + (int64_t)row * chunks + chunk, (uint64_t)__float_as_uint(S) << 32 | __float_as_uint(M));
     }
   }
+  return true;
 }
 
-template <typename T>
-__global__ __launch_bounds__(RU_NT) void k_rules(RulesLaunch a, int chunks) {
-  rules_block<T, 1>(a, chunks);
-}
-// (two of these blocks fit a CU only with at most 64 vector and 80 scalar
-// registers a wave: 256 rows of 131071, 32768 tokens of history 151 -> 110 us)
-template <typename T>
-__global__ __launch_bounds__(RU_LONG * RU_NT) __attribute__((amdgpu_waves_per_eu(8), amdgpu_num_sgpr(80)))
-void k_rules_long(RulesLaunch a, int chunks) {
-  rules_block<T, RU_LONG>(a, chunks);
+// The wave's LDS writes are done before its next reads.
+__device__ __forceinline__ void wave_lds_done() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
 }
 
 // A row's blocks joined, one wave a row, in the same way: a floor under the k
 // best, the few above it, the place of each.
-__global__ __launch_bounds__(64) void k_rules_join(RulesLaunch a, int chunks) {
+// rules_lds: the lists, then RU_CAND candidates (one wave: its LDS accesses keep
+// their order).
+__device__ __forceinline__ void join_row(const RulesLaunch& a, int chunks, int row, int lane, uint64_t* rules_lds) {
   constexpr int LISTS = kRulesMaxVocab / RU_CHUNK / 64;
-  extern __shared__ uint2 rules_lds[];                 // the lists, then RU_CAND candidates
-  const int row = blockIdx.x, lane = threadIdx.x, n = chunks * a.k;
-  const uint2* keys = (const uint2*)(a.ws + (int64_t)a.rows * chunks * 2) + (int64_t)row * n;
-  const float2* ms = (const float2*)a.ws + (int64_t)row * chunks;
+  const int n = chunks * a.k;
+  const uint64_t* keys = (const uint64_t*)(a.ws + (int64_t)a.rows * chunks * 2) + (int64_t)row * n;
+  const uint64_t* ms = (const uint64_t*)a.ws + (int64_t)row * chunks;
   float m[LISTS], s[LISTS], M = -INFINITY;
 #pragma unroll
   for (int i = 0; i < LISTS; ++i) {
     const int c = lane + 64 * i;
-    const float2 x = c < chunks ? ms[c] : float2{-INFINITY, 0.f};
-    m[i] = x.x;
-    s[i] = x.y;
-    M = fmaxf(M, x.x);
+    m[i] = -INFINITY;
+    s[i] = 0.f;
+    if (c < chunks) {
+      const uint64_t x = left_by(a, ms + c);
+      m[i] = __uint_as_float((uint32_t)x);
+      s[i] = __uint_as_float((uint32_t)(x >> 32));
+    }
+    M = fmaxf(M, m[i]);
   }
   uint32_t largest = 0;
   for (int i0 = 0; i0 < n; i0 += 4 * 64) {
-    uint2 x[4];
+    uint64_t x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = i0 + 64 * i + lane < n ? keys[i0 + 64 * i + lane] : uint2{0u, 0u};
+    for (int i = 0; i < 4; ++i) x[i] = i0 + 64 * i + lane < n ? left_by(a, keys + i0 + 64 * i + lane) : 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      largest = max(largest, x[i].x);
+      largest = max(largest, (uint32_t)(x[i] >> 32));
       if (i0 + 64 * i + lane < n) rules_lds[i0 + 64 * i + lane] = x[i];
     }
   }
@@ -415,29 +443,29 @@ __global__ __launch_bounds__(64) void k_rules_join(RulesLaunch a, int chunks) {
   for (int i = 0; i < LISTS; ++i)
     S += m[i] == M ? s[i] : s[i] * __builtin_amdgcn_exp2f((m[i] - M) * 1.4426950408889634f);
   const float log_sum = logf(wave_sum_lanes(S));
-  __syncthreads();
-  auto put = [&](int place, uint2 x) {
-    const float z = x.x == 0xffffffffu ? NAN : from_ordered_u32(x.x);
-    a.token[(int64_t)row * a.k + place] = x.x ? (int)x.y : -1;
-    a.logprob[(int64_t)row * a.k + place] = x.x ? (z - M) - log_sum : -INFINITY;
+  wave_lds_done();
+  auto put = [&](int place, uint64_t x) {
+    const uint32_t r = (uint32_t)(x >> 32);
+    const float z = r == 0xffffffffu ? NAN : from_ordered_u32(r);
+    a.token[(int64_t)row * a.k + place] = x ? (int)~(uint32_t)x : -1;
+    a.logprob[(int64_t)row * a.k + place] = x ? (z - M) - log_sum : -INFINITY;
   };
-  uint2* cand = rules_lds + n;
+  uint64_t* cand = rules_lds + n;
   const uint32_t least = rank_floor(largest, a.k);
   int have = 0;
   for (int i0 = 0; i0 < n; i0 += 64) {
-    const uint2 x = i0 + lane < n ? rules_lds[i0 + lane] : uint2{0u, 0u};
-    const uint64_t in = __ballot(x.x >= least);
+    const uint64_t x = i0 + lane < n ? rules_lds[i0 + lane] : 0;
+    const uint64_t in = __ballot((uint32_t)(x >> 32) >= least);
     const int at = have + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0));
-    if (x.x >= least && at < RU_CAND) cand[at] = x;
+    if ((uint32_t)(x >> 32) >= least && at < RU_CAND) cand[at] = x;
     have += __popcll(in);
   }
-  __syncthreads();
+  wave_lds_done();
   if (have <= RU_CAND) {
-    const uint2 mine = lane < have ? cand[lane] : uint2{0u, 0u};
-    int place = 0;
-    for (int i = 0; i < have; ++i) place += better(cand[i], mine);
+    const uint64_t mine = lane < have ? cand[lane] : 0;
+    const int place = better(mine, have, mine);
     if (lane < have && place < a.k) put(place, mine);
-    if (lane >= have && lane < a.k) put(lane, uint2{0u, 0u});
+    if (lane >= have && lane < a.k) put(lane, 0);
     return;
   }
   // many equal ones: lane l goes down the sorted lists of blocks l, l + 64, ...
@@ -445,21 +473,21 @@ __global__ __launch_bounds__(64) void k_rules_join(RulesLaunch a, int chunks) {
 #pragma unroll
   for (int i = 0; i < LISTS; ++i) at[i] = 0;
   for (int i = 0; i < a.k; ++i) {
-    uint2 x = {0u, 0u};
+    uint64_t x = 0;
     int from = 0;
 #pragma unroll
     for (int j = 0; j < LISTS; ++j) {
       const int c = lane + 64 * j;
       if (c >= chunks || at[j] >= a.k) continue;
-      const uint2 y = rules_lds[c * a.k + at[j]];
-      if (y.x > x.x) {                                 // (equal: the lower chunk has the lower tokens)
+      const uint64_t y = rules_lds[c * a.k + at[j]];
+      if (y > x) {
         x = y;
         from = j;
       }
     }
-    const int l = best_lane(x.x, (int)x.y);
+    const int l = best_lane((uint32_t)(x >> 32), (int)~(uint32_t)x);
     if (l < 0) {
-      if (lane == 0) put(i, uint2{0u, 0u});
+      if (lane == 0) put(i, 0);
     } else if (lane == l) {
       put(i, x);
 #pragma unroll
@@ -469,17 +497,40 @@ __global__ __launch_bounds__(64) void k_rules_join(RulesLaunch a, int chunks) {
 }
 
 template <typename T>
+__global__ __launch_bounds__(RU_NT) void k_rules(RulesLaunch a, int chunks) {
+  if (!rules_block<T, 1>(a, chunks) || !a.counters) return;
+  extern __shared__ __attribute__((aligned(16))) uint32_t table[];
+  const int row = blockIdx.y;
+  if (!arrive_last(a.counters + row, gridDim.x) || threadIdx.x >= 64) return;
+  join_row(a, chunks, row, threadIdx.x, (uint64_t*)table);
+}
+// (two of these blocks fit a CU only with at most 64 vector and 80 scalar
+// registers a wave: 256 rows of 131071, 32768 tokens of history 151 -> 110 us)
+template <typename T>
+__global__ __launch_bounds__(RU_LONG * RU_NT) __attribute__((amdgpu_waves_per_eu(8), amdgpu_num_sgpr(80)))
+void k_rules_long(RulesLaunch a, int chunks) {
+  rules_block<T, RU_LONG>(a, chunks);
+}
+
+__global__ __launch_bounds__(64) void k_rules_join(RulesLaunch a, int chunks) {
+  extern __shared__ uint64_t rules_lds[];
+  join_row(a, chunks, blockIdx.x, threadIdx.x, rules_lds);
+}
+
+template <typename T>
 void rules(const RulesLaunch& a, hipStream_t s) {
   const int chunks = (a.vocab + RU_CHUNK - 1) / RU_CHUNK;
   const bool lists = a.history || a.bias_token;
+  const size_t join_lds = a.k > 0 ? ((size_t)chunks * a.k + RU_CAND) * sizeof(uint64_t) : 0;
   if (a.history_ld >= kLongHistory) {
     static_assert(RU_LONG * RU_CHUNK * 4 <= 65536, "dynamic LDS without asking");
     k_rules_long<T><<<dim3((chunks + RU_LONG - 1) / RU_LONG, a.rows), RU_LONG * RU_NT,
                       lists ? RU_LONG * RU_CHUNK * 4 : 0, s>>>(a, chunks);
+    if (a.k > 0) k_rules_join<<<a.rows, 64, join_lds, s>>>(a, chunks);
   } else {
-    k_rules<T><<<dim3(chunks, a.rows), RU_NT, lists ? RU_CHUNK * 4 : 0, s>>>(a, chunks);
+    k_rules<T><<<dim3(chunks, a.rows), RU_NT, std::max<size_t>(lists ? RU_CHUNK * 4 : 0, a.counters ? join_lds : 0), s>>>(a, chunks);
+    if (a.k > 0 && !a.counters) k_rules_join<<<a.rows, 64, join_lds, s>>>(a, chunks);
   }
-  if (a.k > 0) k_rules_join<<<a.rows, 64, ((size_t)chunks * a.k + RU_CAND) * sizeof(uint2), s>>>(a, chunks);
 }
 
 __global__ __launch_bounds__(64) void k_note_rows(SlotRuleArrays a, const int32_t* slots, const int32_t* tokens,

@@ -140,7 +140,7 @@ asr_status plan_attention(const asr_attention* a, ShareLaunch* s, size_t* bytes)
   const double blocks = ((double)units * s->np + 8.0 * tiles) + (double)own_units * s->no;
   if (blocks > 2147483647.0 || (double)a->rows * a->n_head > 2e9) return fail(ASR_EINVAL, "too much work for one call");
   const int64_t parts = s->np + s->no;
-  *bytes = parts > 1 ? (size_t)a->rows * a->n_head * parts * (kHeadDim + 2) * 4 : 0;
+  *bytes = parts > 1 ? kCounters * 4 + (size_t)a->rows * a->n_head * parts * (kHeadDim + 2) * 4 : 0;
   return ASR_OK;
 }
 
@@ -161,8 +161,8 @@ asr_status plan_rules(const asr_rules* r, RulesLaunch* s, size_t* bytes) {
   if (r->mask && r->mask_ld < (r->vocab + 31) / 32) return fail(ASR_EINVAL, "mask_ld shorter than the vocabulary");
   *s = {r->logits, r->ld, r->rows, r->vocab, r->sets, r->set, r->history, r->history_ld, r->history_len, r->prompt_len,
         r->repetition, r->frequency, r->presence, r->bias_token, r->bias_value, r->bias_ld, r->bias_len, r->mask,
-        r->mask_ld, r->masks, r->mask_of, r->temperature, r->out, r->out_ld, r->k, r->token, r->logprob, nullptr};
-  *bytes = rules_ws_bytes(r->rows, r->vocab, r->k);
+        r->mask_ld, r->masks, r->mask_of, r->temperature, r->out, r->out_ld, r->k, r->token, r->logprob, nullptr, nullptr};
+  *bytes = r->k > 0 ? kCounters * 4 + rules_ws_bytes(r->rows, r->vocab, r->k) : 0;
   return ASR_OK;
 }
 
@@ -199,7 +199,7 @@ asr_status asr_attend_shared(const asr_attention* a, void* ws, size_t ws_bytes, 
     if (!aligned(a->q, 16) || !aligned(a->out, 16)) return fail(ASR_EINVAL, "q and out must be 16-byte aligned");
     st = check_ws(ws, ws_bytes, need);
     if (st != ASR_OK) return st;
-    s.rec = (float*)ws;
+    s.rec = (float*)ws + kCounters;
     return launched(attend_shared(s, a->dtype == ASR_BF16, (hipStream_t)stream));
   });
 }
@@ -228,7 +228,12 @@ asr_status asr_logit_rules(const asr_rules* r, void* ws, size_t ws_bytes, void* 
     if (!r->out && r->k == 0) return fail(ASR_EINVAL, "nothing asked for: neither out nor k");
     st = check_ws(ws, ws_bytes, need);
     if (st != ASR_OK) return st;
-    s.ws = (float*)ws;
+    s.ws = (float*)ws + kCounters;
+    // up to a block a CU the row's last block joins the others' results, above that
+    // a second kernel does (us, 10 best of 51866 tokens: 5 rows 11.8 / 12.4, 64 rows
+    // 15.1 / 15.5, 128 rows 25.3 / 24.4; one launch also spares the host 4 us)
+    const int64_t blocks = (int64_t)r->rows * ((r->vocab + kRulesChunk - 1) / kRulesChunk);
+    s.counters = r->k > 0 && blocks <= cu_count() ? (uint32_t*)ws : nullptr;
     logit_rules(s, r->dtype == ASR_BF16, (hipStream_t)stream);
     return launched(hipSuccess);
   });

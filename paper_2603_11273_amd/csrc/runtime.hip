@@ -405,9 +405,9 @@ Hypotheses plan_hypotheses(const asr_ctx* c, int32_t max_bias, int32_t n_masks) 
   h.step = b.take((kRuleScalars * D + 5 * D + 1) * 4);
   h.token = b.take(D * kRulesMaxK * 4);
   h.logprob = b.take(D * kRulesMaxK * 4);
-  h.rules_ws_size = rules_ws_bytes((int)D, (int)V, kRulesMaxK);
+  h.rules_ws_size = kCounters * 4 + rules_ws_bytes((int)D, (int)V, kRulesMaxK);
   h.rules_ws = b.take(h.rules_ws_size);
-  h.share_ws_size = D * g.n_head * kHypParts * (kHeadDim + 2) * 4;
+  h.share_ws_size = kCounters * 4 + D * g.n_head * kHypParts * (kHeadDim + 2) * 4;
   h.share_ws = b.take(h.share_ws_size);
   h.total = (b.off + 255) / 256 * 256;
   return h;
@@ -1776,6 +1776,7 @@ asr_status asr_bind_hypotheses(asr_ctx* c, int32_t max_bias, int32_t n_masks, vo
   c->default_rules = Rules();
   // no token known of any position, no token allowed by a mask not written yet
   fill_u32((uint32_t*)(c->hyp.base + c->hyp.history), 0xffffffffu, (int64_t)c->cfg.max_slots * kTextCtx, c->stream);
+  for (size_t ws : {c->hyp.rules_ws, c->hyp.share_ws}) fill_u32((uint32_t*)(c->hyp.base + ws), 0u, kCounters, c->stream);
   if (n_masks > 0)
     fill_u32((uint32_t*)(c->hyp.base + c->hyp.mask), 0u, (int64_t)n_masks * ((c->cfg.vocab + 31) / 32), c->stream);
   CHECK_LAUNCH();

@@ -258,12 +258,13 @@ def test_no_temperature_below_or_at_zero():
 
 
 def test_a_row_does_not_depend_on_its_batch():
-    """The same logits and rules at other places of a batch (other alignments of an odd row): the same bits."""
+    """The same logits and rules at other places of a batch (other alignments of an odd row; 40 rows, which
+    another kernel joins): the same bits."""
     rng = np.random.default_rng(11)
     V, one = 51865, normal(np.random.default_rng(1), 1, 51865)
     for dtype in (F32, BF16):
         got = []
-        for rows, at in ((1, 0), (4, 1), (4, 2), (6, 5)):
+        for rows, at in ((1, 0), (4, 1), (4, 2), (6, 5), (40, 33)):
             logits = normal(rng, rows, V)
             logits[at] = one
             rules = all_rules(np.random.default_rng(2), 1, V)

@@ -255,3 +255,30 @@ def test_capture_and_streams(dtype):
             torch.cuda.synchronize()
             assert torch.equal(c.out, eager), step
     c.check(c.out, prefix_len=np.array([700 - 97 * 3, 30 // 4, 1500 - 3]))
+
+
+def test_one_workspace_for_calls_of_many_sizes():
+    """Attention of one part and of many, with and without own keys, and rules, one after the other over one
+    block: what counts blocks in it is zeros again after every call."""
+    from paper_2603_11273_amd import asr
+    cases = [Case(20 + i, d, **kw) for i, (d, kw) in enumerate([
+        (BF16, dict(sizes=[5], prefix=[1500], own=[40], heads=6, kv=6)), (F32, dict(sizes=[1, 3], prefix=[700, 0], own=[0, 90])),
+        (BF16, dict(sizes=[20], prefix=[900], own=[5])), (F32, dict(sizes=[2], prefix=[0], own=[300, 0])),
+        (BF16, dict(sizes=[1] * 9, prefix=[130, 0, 1], own=[1, 0, 500], heads=8, kv=2))])]
+    size = max(c.plan().workspace_bytes for c in cases)
+    block = torch.zeros(max(size, 1 << 20), dtype=torch.uint8, device="cuda")
+    plans = [c.plan(workspace=block) for c in cases]
+    logits = torch.randn((7, 50001), device="cuda")
+    rules = [asr.LogitRules(n, 50001, F32, k=k, device="cuda:0", workspace=block) for n, k in ((7, 5), (2, 16))]
+    token, logprob = (torch.zeros((7, 16), dtype=t, device="cuda") for t in (torch.int32, F32))
+    want = torch.sort(logits, dim=1, descending=True, stable=True).indices
+    for _ in range(3):
+        for c, plan in zip(cases, plans):
+            c.out.fill_(7.0)
+            plan(c.q, c.out)
+            for r, n, k in zip(rules, (7, 2), (5, 16)):
+                r(logits[:n], token=token.view(-1)[:n * k].view(n, k), logprob=logprob.view(-1)[:n * k].view(n, k))
+                assert torch.equal(token.view(-1)[:n * k].view(n, k).long(), want[:n, :k])
+            assert not block[:16384].any()
+    for c in cases:
+        c.check(c.out)

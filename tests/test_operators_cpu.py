@@ -35,11 +35,11 @@ def size(fn, args):
 
 def test_sizes():
     st, n = size(asr.lib.asr_attend_shared_size, attention(part_keys=128))
-    assert st == asr.ASR_OK and n == 6 * 4 * 2 * 66 * 4          # two parts: shared and own
+    assert st == asr.ASR_OK and n == 16384 + 6 * 4 * 2 * 66 * 4  # two parts: shared and own
     st, n = size(asr.lib.asr_attend_shared_size, attention(max_own=0))
     assert st == asr.ASR_OK and n == 0                           # one part: no records
     st, n = size(asr.lib.asr_logit_rules_size, rules(vocab=4097, mask_ld=129))
-    assert st == asr.ASR_OK and n == 3 * 2 * (1 + 2) * 8
+    assert st == asr.ASR_OK and n == 16384 + 3 * 2 * (1 + 2) * 8
     assert size(asr.lib.asr_logit_rules_size, rules(k=0)) == (asr.ASR_OK, 0)
 
 
