@@ -496,13 +496,16 @@ __device__ __forceinline__ void join_row(const RulesLaunch& a, int chunks, int r
   }
 }
 
-template <typename T>
+// (JOINED by itself: it takes registers that a full GPU would miss)
+template <typename T, bool JOINED>
 __global__ __launch_bounds__(RU_NT) void k_rules(RulesLaunch a, int chunks) {
-  if (!rules_block<T, 1>(a, chunks) || !a.counters) return;
-  extern __shared__ __attribute__((aligned(16))) uint32_t table[];
-  const int row = blockIdx.y;
-  if (!arrive_last(a.counters + row, gridDim.x) || threadIdx.x >= 64) return;
-  join_row(a, chunks, row, threadIdx.x, (uint64_t*)table);
+  const bool some = rules_block<T, 1>(a, chunks);
+  if constexpr (JOINED) {
+    extern __shared__ __attribute__((aligned(16))) uint32_t table[];
+    const int row = blockIdx.y;
+    if (some && arrive_last(a.counters + row, gridDim.x) && threadIdx.x < 64)
+      join_row(a, chunks, row, threadIdx.x, (uint64_t*)table);
+  }
 }
 // (two of these blocks fit a CU only with at most 64 vector and 80 scalar
 // registers a wave: 256 rows of 131071, 32768 tokens of history 151 -> 110 us)
@@ -528,7 +531,11 @@ void rules(const RulesLaunch& a, hipStream_t s) {
                       lists ? RU_LONG * RU_CHUNK * 4 : 0, s>>>(a, chunks);
     if (a.k > 0) k_rules_join<<<a.rows, 64, join_lds, s>>>(a, chunks);
   } else {
-    k_rules<T><<<dim3(chunks, a.rows), RU_NT, std::max<size_t>(lists ? RU_CHUNK * 4 : 0, a.counters ? join_lds : 0), s>>>(a, chunks);
+    const size_t lds = lists ? RU_CHUNK * 4 : 0;
+    if (a.counters)
+      k_rules<T, true><<<dim3(chunks, a.rows), RU_NT, std::max(lds, join_lds), s>>>(a, chunks);
+    else
+      k_rules<T, false><<<dim3(chunks, a.rows), RU_NT, lds, s>>>(a, chunks);
     if (a.k > 0 && !a.counters) k_rules_join<<<a.rows, 64, join_lds, s>>>(a, chunks);
   }
 }
