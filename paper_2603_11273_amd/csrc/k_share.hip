@@ -135,13 +135,15 @@ struct KeyTile<bf16_t> {
   using Frag = bf16x8;
   // o += V^T p, the probabilities as bf16 pairs hi + lo (hi cut off, not
   // rounded: one byte permute for two): a single rounding to bf16 would add as
-  // much error again as the rounding of the result
+  // much error again as the rounding of the result.  hi is cut from the float
+  // below, so lo is never 0 where p is not: an infinite value stays infinite
   static __device__ __forceinline__ void accumulate(const Frag* f, const float* p, f32x4* o) {
     uint4 hi, lo;
     uint32_t *hw = (uint32_t*)&hi, *lw = (uint32_t*)&lo;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t a = __float_as_uint(p[2 * i]), b = __float_as_uint(p[2 * i + 1]);
+      const uint32_t a = __builtin_elementwise_sub_sat(__float_as_uint(p[2 * i]), 1u);
+      const uint32_t b = __builtin_elementwise_sub_sat(__float_as_uint(p[2 * i + 1]), 1u);
       hw[i] = __builtin_amdgcn_perm(b, a, 0x07060302);
       lw[i] = pack2_bf16(p[2 * i] - __uint_as_float(a & 0xffff0000u),
                          p[2 * i + 1] - __uint_as_float(b & 0xffff0000u));

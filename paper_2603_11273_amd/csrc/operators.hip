@@ -138,7 +138,8 @@ asr_status plan_attention(const asr_attention* a, ShareLaunch* s, size_t* bytes)
   s->np = parts_of(a->max_prefix, s->prefix_part);
   s->no = parts_of(a->max_own, s->own_part);
   const double blocks = ((double)units * s->np + 8.0 * tiles) + (double)own_units * s->no;
-  if (blocks > 2147483647.0 || (double)a->rows * a->n_head > 2e9) return fail(ASR_EINVAL, "too much work for one call");
+  // (a launch has fewer than 2^32 threads: 256 a block, 64 a row and head)
+  if (blocks >= 16777216.0 || (double)a->rows * a->n_head >= 67108864.0) return fail(ASR_EINVAL, "too much work for one call");
   const int64_t parts = s->np + s->no;
   *bytes = parts > 1 ? kCounters * 4 + (size_t)a->rows * a->n_head * parts * (kHeadDim + 2) * 4 : 0;
   return ASR_OK;
@@ -199,7 +200,7 @@ asr_status asr_attend_shared(const asr_attention* a, void* ws, size_t ws_bytes, 
     if (!aligned(a->q, 16) || !aligned(a->out, 16)) return fail(ASR_EINVAL, "q and out must be 16-byte aligned");
     st = check_ws(ws, ws_bytes, need);
     if (st != ASR_OK) return st;
-    s.rec = (float*)ws + kCounters;
+    s.rec = need ? (float*)ws + kCounters : nullptr;
     return launched(attend_shared(s, a->dtype == ASR_BF16, (hipStream_t)stream));
   });
 }

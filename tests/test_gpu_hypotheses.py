@@ -146,6 +146,22 @@ def test_rows_beside_a_family_and_hypotheses_of_any_batch_keep_their_bits(prompt
     assert all(np.array_equal(a, b) for a, b in zip(*got))
 
 
+def test_a_large_family():
+    """40 hypotheses of one prompt (queries for every size of tile) give the bits that two of them give."""
+    shape, seed = shape_of("base", "bf16"), 20261107
+    got = []
+    for n in (2, 20, 40):
+        ctx, _ = context(shape, seed, 40, clips=1)
+        ctx.debug_set_self_kv(0, synth.self_kv_prefix(seed, 0, shape.n_dec, shape.n_head).numpy(), 150)
+        for dst in range(1, n):
+            ctx.fork_slot(0, dst)
+        for t in (5, 6, 7):
+            out = ctx.step(slots=list(range(n)), tokens=[t] * n, want_logits=True, topk=3)
+        assert all(np.array_equal(x, out["logits"][0]) for x in out["logits"])
+        got.append((out["logits"][0], out["top_token"][n - 1], out["top_logprob"][n - 1]))
+    assert all(np.array_equal(a, b) for g in got[1:] for a, b in zip(g, got[0]))
+
+
 def test_taken_and_held_slots():
     from paper_2603_11273_amd import asr
     shape, seed = shape_of("tiny", "f32"), 20261103

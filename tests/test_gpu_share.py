@@ -213,6 +213,13 @@ def test_infinite_value_and_nan_key_stay_with_their_row():
     assert torch.isfinite(out[d]).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_an_infinite_value_of_weight_one(dtype):
+    c = Case(15, dtype, sizes=[1], prefix=[1], own=[0], heads=1, kv=1)
+    c.pv[c.prefix_slot[0], 0, 0, :3] = torch.tensor([float("inf"), -float("inf"), 2.0]).to(dtype)
+    assert c.plan()(c.q, c.out)[0, :3].tolist() == [float("inf"), -float("inf"), 2.0]
+
+
 def test_offsets_past_32_bits():
     """Two slots more than 2^32 bytes apart, a group's shared keys in the far one."""
     n, gap = 300, (1 << 31) + 64

@@ -44,7 +44,7 @@ def test_sizes():
 
 
 @pytest.mark.parametrize("kw", [
-    dict(dtype=2), dict(n_head=0), dict(n_kv_head=3), dict(n_kv_head=0), dict(n_head=1 << 20, n_kv_head=1), dict(rows=-1),
+    dict(dtype=2), dict(n_head=0), dict(rows=1 << 25, n_head=8), dict(n_kv_head=3), dict(n_kv_head=0), dict(n_head=1 << 20, n_kv_head=1), dict(rows=-1),
     dict(groups=-1), dict(max_group=0), dict(max_group=7), dict(max_prefix=-1), dict(max_own=-1), dict(max_prefix=101),
     dict(max_own=21), dict(part_keys=64), dict(part_keys=200), dict(part_keys=8320), dict(part_keys=-128),
     dict(scale=float("nan")), dict(scale=float("inf")), dict(prefix__k=None), dict(own__v=None), dict(prefix__k=A + 8),
