@@ -81,9 +81,11 @@ __device__ __forceinline__ int best_lane(uint32_t rank, int token) {
 // The history's n entries into the block's table: the first `marked` as seen, the
 // others counted.  Every block reads the whole list, so what counts is the
 // instructions of an entry: 16 a thread without a test while there are so many,
-// then four.  What is no token, or none of the block's, ends far above them.
+// then fewer.  What is no token, or none of the block's, ends far above them.
+// first: entries threadIdx.x + i NT, i < RU_FIRST, loaded ahead (short histories).
+constexpr int RU_FIRST = 4;
 template <int NT, int TOKENS>
-__device__ __forceinline__ void count_tokens(const int32_t* list, int marked, int n, int b0, uint32_t* table) {
+__device__ __forceinline__ void count_tokens(const int32_t* list, const int* first, int marked, int n, int b0, uint32_t* table) {
   int from = 0;
   for (; n - from >= 16 * NT; from += 16 * NT) {
     i32x4u tok[4];
@@ -108,13 +110,19 @@ __device__ __forceinline__ void count_tokens(const int32_t* list, int marked, in
           atomicAdd(&table[u], 1u);
       });
   }
-  for (; from < n; from += 4 * NT) {
-    int tok[4];
+  constexpr int W = NT > RU_NT ? 8 : 4;
+  for (; from < n; from += W * NT) {
+    int tok[W];
     const int at = from + (int)threadIdx.x;
+    if (from > 0 || !first) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) tok[i] = list[min(at + i * NT, n - 1)];
+      for (int i = 0; i < W; ++i) tok[i] = list[min(at + i * NT, n - 1)];
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < RU_FIRST; ++i) tok[i] = first[i];
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
       const int j = at + i * NT;
       const uint32_t u = (uint32_t)tok[i] - (uint32_t)b0;
       if (j >= n || u >= TOKENS) continue;
@@ -199,6 +207,22 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
   const bool ruled = set >= 0 && set < a.sets;
   if (!ruled) set = 0;
   const bool some = ruled && a.sets > 0;
+  // ... and of its lists what fits, before their lengths are known (rows are as long as they say)
+  const int32_t* hist = a.history + (int64_t)set * a.history_ld;
+  int said[RU_FIRST] = {};
+  if (SUBS == 1 && some && a.history) {
+#pragma unroll
+    for (int i = 0; i < RU_FIRST; ++i)
+      if (i * NT < a.history_ld) said[i] = hist[min((int)threadIdx.x + i * NT, (int)a.history_ld - 1)];
+  }
+  const int32_t* bt = a.bias_token + (int64_t)set * a.bias_ld;
+  const float* bv = a.bias_value + (int64_t)set * a.bias_ld;
+  int bias_tok = -1;
+  float bias_val = 0.f;
+  if (some && a.bias_token && lane < a.bias_ld) {
+    bias_tok = bt[lane];
+    bias_val = bv[lane];
+  }
   const int hist_len = some && a.history ? a.history_len[set] : 0;
   const int prompt = some && a.history && a.prompt_len ? a.prompt_len[set] : 0;
   const int bias_len = some && a.bias_token ? a.bias_len[set] : 0;
@@ -222,7 +246,7 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
 #pragma unroll
     for (int i = 0; i < RU_E / 4; ++i) *(uint4*)(table + (i * NT + (int)threadIdx.x) * 4) = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
-    count_tokens<NT, TOKENS>(a.history + (int64_t)set * a.history_ld, prompt, hist_n, b0, table);
+    count_tokens<NT, TOKENS>(hist, SUBS == 1 ? said : nullptr, prompt, hist_n, b0, table);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < RU_E / 4; ++i) {
@@ -249,12 +273,10 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
 #pragma unroll
     for (int i = 0; i < RU_E / 4; ++i) *(float4*)(sums + (i * NT + (int)threadIdx.x) * 4) = float4{0.f, 0.f, 0.f, 0.f};
     __syncthreads();
-    const int32_t* bt = a.bias_token + (int64_t)set * a.bias_ld;
-    const float* bv = a.bias_value + (int64_t)set * a.bias_ld;
     for (int j0 = 0; j0 < bias_n; j0 += 64) {
       const bool in = j0 + lane < bias_n;
-      const int tok = in ? bt[j0 + lane] : -1;
-      const float val = in ? bv[j0 + lane] : 0.f;
+      const int tok = !in ? -1 : j0 ? bt[j0 + lane] : bias_tok;
+      const float val = !in ? 0.f : j0 ? bv[j0 + lane] : bias_val;
       const uint32_t u = (uint32_t)tok - (uint32_t)b0;
       uint64_t hit = __ballot(tok >= 0 && u < TOKENS && (tok & (SUBS * 4 - 1)) == wave);
       while (hit) {
@@ -371,15 +393,24 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
   // the 256 threads': a candidate's place is the number of better ones
   const int chunk = blockIdx.x * SUBS + sub, w0 = wave & ~3;
   uint64_t* keys = (uint64_t*)(a.ws + (int64_t)a.rows * chunks * 2) + ((int64_t)row * chunks + chunk) * a.k;
-  const uint64_t mine = lane < n ? cand[wave][lane] : 0;
-  int place = 0, have = 0;
+  int m[4], have = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const int m = __builtin_amdgcn_readfirstlane(cand_n[w0 + w]);
-    have += m;
-    place += better(lane < m ? cand[w0 + w][lane] : 0, m, mine);
+  for (int w = 0; w < 4; ++w) have += m[w] = __builtin_amdgcn_readfirstlane(cand_n[w0 + w]);
+  if (have <= 64) {                                    // one wave, a candidate a lane
+    if (wave == w0) {
+      const int w = (lane >= m[0]) + (lane >= m[0] + m[1]) + (lane >= m[0] + m[1] + m[2]);
+      const int at = lane - (w > 0 ? m[0] : 0) - (w > 1 ? m[1] : 0) - (w > 2 ? m[2] : 0);
+      const uint64_t mine = lane < have ? cand[w0 + w][at] : 0;
+      const int place = better(mine, have, mine);
+      if (lane < have && place < a.k) leave(a, keys + place, mine);
+    }
+  } else {
+    const uint64_t mine = lane < n ? cand[wave][lane] : 0;
+    int place = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) place += better(lane < m[w] ? cand[w0 + w][lane] : 0, m[w], mine);
+    if (lane < n && place < a.k) leave(a, keys + place, mine);
   }
-  if (lane < n && place < a.k) leave(a, keys + place, mine);
   if (wave == w0) {
     if (lane >= have && lane < a.k) leave(a, keys + lane, 0);
     if (lane == 0) {
