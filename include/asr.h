@@ -25,8 +25,9 @@
  *   - Time is never read from a clock: callers pass now_us / arrival_us, so
  *     every ordering is reproducible.
  *   - Host buffers belong to the caller.  Device memory is ONE caller-provided
- *     block (asr_bind) that the library sub-allocates and never frees; the
- *     library itself never allocates device memory.
+ *     block (asr_bind) that the library sub-allocates and never frees (and, for
+ *     hypotheses and rules, a second one: asr_bind_hypotheses); the library
+ *     itself never allocates device memory.
  *   - GPU work is enqueued on the stream given to asr_bind.  A prefill may
  *     fork onto streams the context owns (default priority): its clip groups
  *     (asr_set_encoder_streams) and, with overlapped prefill, the whole
@@ -167,7 +168,8 @@ typedef struct {
 
 typedef struct {
   int32_t* slot_of;  /* [n_prefill] slot given to each prefilled request */
-  int32_t* argmax;   /* [n_decode] argmax of each row's logits, lowest index on ties */
+  int32_t* argmax;   /* [n_decode] argmax of each row's logits, lowest index on ties (under
+                        the slot's rules, where it has any: asr_set_slot_rules) */
   int32_t* done;     /* [n_decode] 1 when the row's slot has no steps left */
 } asr_step_out;
 
@@ -194,8 +196,8 @@ typedef enum {
   ASR_K_ATTN = 2,       /* encoder flash attention */
   ASR_K_LN = 3,         /* LayerNorms */
   ASR_K_DGEMM = 4,      /* decode GEMMs (+ split-K reduce) */
-  ASR_K_DATTN = 5,      /* decode self + cross attention */
-  ASR_K_VOCAB = 6,      /* vocabulary GEMM + argmax */
+  ASR_K_DATTN = 5,      /* decode self + cross attention, of hypotheses' families too */
+  ASR_K_VOCAB = 6,      /* vocabulary GEMM + argmax, or the rules and the best tokens */
   ASR_K_OTHER = 7,
   ASR_K_PREFILL = 8,    /* whole prefill phase of asr_step (mel .. cross K/V) */
   ASR_K_DECODE = 9,     /* whole decode phase of asr_step (embed .. argmax) */
@@ -549,9 +551,9 @@ asr_status asr_attend_shared(const asr_attention* a, void* ws, size_t ws_bytes, 
  *   out (may be NULL): z, float32; it may be the logits themselves (float32,
  * out_ld = ld).  k in [0, 16] best tokens per row, larger z first, the lower
  * token of equal ones, a NaN before everything: token and logprob [rows][k],
- * logprob = z - log sum_v e^z.  A token with z = -inf is never given: where the
- * others run out, token = -1 and logprob = -inf (a row whose mask allows
- * nothing has only these).
+ * logprob = z - L, L = log sum_v e^z in float32 (so off by half a step of L).  A
+ * token with z = -inf is never given: where the others run out, token = -1 and
+ * logprob = -inf (a row whose mask allows nothing has only these).
  *   vocab at most 1048576, rows at most 65535. */
 typedef struct {
   int32_t dtype;       /* asr_dtype of the logits */

@@ -2,8 +2,9 @@
 
 The processed logits are float32 operations rounded one by one, so they and the
 chosen tokens are compared bit for bit with the same operations in numpy.  The
-log-probabilities are compared with 64 bits; their tolerance: 2^-24 of each of
-the two subtractions' results, and a relative error of the sum that the
+log-probabilities are compared with 64 bits; their tolerance: 2^-24 of L = M +
+log sum (one rounding; where |M| is 4096 or more, of z - M instead) and of the
+result, 2^-23 of the logarithm, and a relative error of the sum that the
 logarithm turns into an absolute one: at most 48 additions follow one another
 (16 in a lane, then trees over lanes, waves and blocks of up to 13 lists), the
 exponential is off by 2^-22 and its argument by 2^-23 of z - M, weighted with
@@ -86,7 +87,8 @@ def best(z, k):
         if not z[v] == -np.inf:
             token[i], logp[i] = v, (z[v].astype(np.float64) - M) - log_sum
             if np.isfinite(log_sum):
-                tol[i] = off + 2.0 ** -23 * (abs(z[v] - M) + abs(log_sum) + 1e-3)
+                rounded = abs(M + log_sum) if abs(M) < 4096 else abs(z[v] - M)
+                tol[i] = off + 2.0 ** -24 * (rounded + abs(logp[i])) + 2.0 ** -23 * abs(log_sum)
     return token, logp, tol
 
 
