@@ -244,6 +244,9 @@ class _Operator:
 
     def __init__(self, device, workspace, size, run, args):
         import torch
+        if workspace is not None and (workspace.device != device or workspace.dtype != torch.uint8
+                                      or not workspace.is_contiguous()):
+            raise TypeError(f"workspace must be contiguous bytes (torch.uint8) on {device}")
         self._dev, self._run, self._args = device, run, args
         # the current stream's handle without a Stream object around it (1.8 us of a 10-us call)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -266,6 +269,11 @@ class _Operator:
         if not (t.is_contiguous() or (ld and t.stride(-1) == 1)):
             raise TypeError(f"{name} must be contiguous")
         return t.data_ptr()
+
+    @staticmethod
+    def _ld(t):
+        """Elements from row to row (of a single row torch may say anything)."""
+        return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
     def _launch(self, stream):
         import torch
@@ -335,7 +343,7 @@ class SharedAttention(_Operator):
         a = self._args
         a.q = self._need(q, "q", torch.float32, self._shape, self._dev, ld=True)
         a.out = self._need(out, "out", self._dtype, self._shape, self._dev, ld=True)
-        a.q_ld, a.out_ld = q.stride(0), out.stride(0)
+        a.q_ld, a.out_ld = self._ld(q), self._ld(out)
         self._launch(stream)
         return out
 
@@ -363,6 +371,8 @@ class LogitRules(_Operator):
                              temperature) if t is not None]
         dev = torch.device(device if device is not None else
                            given[0].device if given else torch.cuda.current_device())
+        if dev.type != "cuda":
+            raise TypeError(f"rules are applied on a GPU, not on {dev}")
         if dev.index is None:
             dev = torch.device(dev.type, torch.cuda.current_device())
         n = rows if sets is None else sets
@@ -389,9 +399,9 @@ class LogitRules(_Operator):
         import torch
         a = self._args
         a.logits = self._need(logits, "logits", self._dtype, self._shape, self._dev, ld=True)
-        a.ld = logits.stride(0)
+        a.ld = self._ld(logits)
         a.out = self._need(out, "out", torch.float32, self._shape, self._dev, ld=True)
-        a.out_ld = 0 if out is None else out.stride(0)
+        a.out_ld = 0 if out is None else self._ld(out)
         a.token = self._need(token, "token", torch.int32, self._best, self._dev)
         a.logprob = self._need(logprob, "logprob", torch.float32, self._best, self._dev)
         self._launch(stream)

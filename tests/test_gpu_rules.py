@@ -304,3 +304,16 @@ def test_capture_and_replay():
         other(x, **b)
         torch.cuda.synchronize()
         assert all(torch.equal(a[n], b[n]) for n in a), step
+
+
+def test_a_single_row_of_any_stride():
+    from paper_2603_11273_amd import asr
+    x = torch.from_numpy(normal(np.random.default_rng(13), 1, 5001)).cuda()
+    column = torch.empty((5001, 1), device="cuda").copy_(x.t())
+    plan = asr.LogitRules(1, 5001, F32, k=3, device="cuda:0")
+    got = []
+    for logits in (x, column.t()):
+        token, logprob = torch.empty((1, 3), dtype=torch.int32, device="cuda"), torch.empty((1, 3), device="cuda")
+        plan(logits, torch.empty((5001, 1), device="cuda").t(), token, logprob)
+        got.append((token, logprob))
+    assert column.t().stride(0) == 1 and torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])

@@ -289,3 +289,17 @@ def test_one_workspace_for_calls_of_many_sizes():
             assert not block[:16384].any()
     for c in cases:
         c.check(c.out)
+
+
+def test_a_single_row_of_any_stride_and_refused_workspaces():
+    """torch gives the stride of a dimension of one element as it likes."""
+    c = Case(31, F32, sizes=[1], prefix=[70], own=[9])
+    q = torch.empty((c.heads * 64, 1), device="cuda").copy_(c.q.t()).t()
+    assert q.is_contiguous() and q.stride(0) == 1
+    out = torch.full((c.heads * 64, 1), 7.0, device="cuda").t()
+    c.plan()(q, out)
+    c.check(out)
+    for ws in (torch.zeros(1 << 20, dtype=torch.uint8), torch.zeros(1 << 20, device="cuda"),
+               torch.zeros(1 << 21, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(TypeError):
+            c.plan(workspace=ws)

@@ -101,3 +101,20 @@ def test_rules_scratch_refused():
     assert asr.lib.asr_logit_rules(None, A, need, None) == asr.ASR_EINVAL
     assert asr.lib.asr_logit_rules_size(C.byref(rules()), None) == asr.ASR_EINVAL
     assert asr.lib.asr_logit_rules(C.byref(rules(rows=0, logits=None)), None, 0, None) == asr.ASR_OK
+
+
+def test_plans_refuse_host_memory():
+    torch = pytest.importorskip("torch")
+    zeros = lambda *shape, **kw: torch.zeros(*shape, **kw)  # noqa: E731
+    with pytest.raises(TypeError):
+        asr.LogitRules(2, 100, torch.float32, k=1, device="cpu")
+    with pytest.raises(TypeError):
+        asr.LogitRules(2, 100, torch.float32, k=1, temperature=zeros(2))
+    with pytest.raises(TypeError):
+        asr.LogitRules(2, 100, torch.float32, k=1, device="cuda:0", temperature=zeros(2))
+    with pytest.raises(TypeError):
+        asr.LogitRules(2, 100, torch.float32, k=1, device="cuda:0", workspace=zeros(1 << 20, dtype=torch.uint8))
+    with pytest.raises(TypeError):
+        keys = zeros(1, 2, 8, 64)
+        asr.SharedAttention(keys, keys, n_head=2, rows=1, groups=1, max_group=1,
+                            group_start=zeros(2, dtype=torch.int32))
