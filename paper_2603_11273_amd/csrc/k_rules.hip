@@ -173,6 +173,13 @@ __device__ __forceinline__ uint32_t rank_floor(uint32_t largest, int k) {
   return t ? t : 1u;
 }
 
+// The wave's LDS writes are done before its next reads.
+__device__ __forceinline__ void wave_lds_done() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
 constexpr int RU_CAND = 64;                  // candidates of a wave
 constexpr uint32_t kLowest = 0x00800000u;    // rank of the lowest finite float
 
@@ -266,19 +273,22 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
     }
   }
   if (bias_n > 0) {
-    // the biases in the order of their list, so that a token given twice has
-    // one sum: of 64 entries, those that are a wave's in turn
-    float* sums = (float*)table;
-    if (hist_n > 0) __syncthreads();
+    // the biases in the order of their list, so that a token given twice has one
+    // sum: each wave adds up those of its own tokens, in their places of the table
+    // (which no other wave reads any more)
+    float* sums = (float*)own;
+    const auto place = [&](int i) { return i * 4 / VEC * RU_NT * VEC + tid * VEC + i * 4 % VEC; };
+    bool some_hit = false;
+    const auto add = [&](int tok, float val) {
+      const uint32_t u = (uint32_t)tok - (uint32_t)v0;
+      uint64_t hit = __ballot(tok >= 0 && u < RU_CHUNK && (int)(u / (64 * VEC) & 3) == (wave & 3));
+      if (!hit) return;
+      if (!some_hit) {
 #pragma unroll
-    for (int i = 0; i < RU_E / 4; ++i) *(float4*)(sums + (i * NT + (int)threadIdx.x) * 4) = float4{0.f, 0.f, 0.f, 0.f};
-    __syncthreads();
-    for (int j0 = 0; j0 < bias_n; j0 += 64) {
-      const bool in = j0 + lane < bias_n;
-      const int tok = !in ? -1 : j0 ? bt[j0 + lane] : bias_tok;
-      const float val = !in ? 0.f : j0 ? bv[j0 + lane] : bias_val;
-      const uint32_t u = (uint32_t)tok - (uint32_t)b0;
-      uint64_t hit = __ballot(tok >= 0 && u < TOKENS && (tok & (SUBS * 4 - 1)) == wave);
+        for (int i = 0; i < RU_E / 4; ++i) *(float4*)(sums + place(i)) = float4{0.f, 0.f, 0.f, 0.f};
+        wave_lds_done();
+        some_hit = true;
+      }
       while (hit) {
         const int l = __ffsll((unsigned long long)hit) - 1;
         hit &= hit - 1;
@@ -286,16 +296,30 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
         const float vl = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(val), l));
         if (lane == 0) sums[ul] += vl;
       }
-    }
-    __syncthreads();
+    };
+    add(lane < bias_n ? bias_tok : -1, bias_val);
+    for (int j0 = 64; j0 < bias_n; j0 += 256) {
+      int tok[4];
+      float val[4];
 #pragma unroll
-    for (int i = 0; i < RU_E / 4; ++i) {
-      const int u = i * 4 / VEC * RU_NT * VEC + tid * VEC + i * 4 % VEC;
-      const float4 x = *(const float4*)((const float*)own + u);
-      z[4 * i] = z[4 * i] + x.x;
-      z[4 * i + 1] = z[4 * i + 1] + x.y;
-      z[4 * i + 2] = z[4 * i + 2] + x.z;
-      z[4 * i + 3] = z[4 * i + 3] + x.w;
+      for (int i = 0; i < 4; ++i) {
+        const int j = min(j0 + 64 * i + lane, bias_n - 1);
+        tok[i] = bt[j];
+        val[i] = bv[j];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) add(j0 + 64 * i + lane < bias_n ? tok[i] : -1, val[i]);
+    }
+    if (some_hit) {
+      wave_lds_done();
+#pragma unroll
+      for (int i = 0; i < RU_E / 4; ++i) {
+        const float4 x = *(const float4*)(sums + place(i));
+        z[4 * i] = z[4 * i] + x.x;
+        z[4 * i + 1] = z[4 * i + 1] + x.y;
+        z[4 * i + 2] = z[4 * i + 2] + x.z;
+        z[4 * i + 3] = z[4 * i + 3] + x.w;
+      }
     }
   }
   if (masked) {
@@ -426,13 +450,6 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
     }
   }
   return true;
-}
-
-// The wave's LDS writes are done before its next reads.
-__device__ __forceinline__ void wave_lds_done() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
 }
 
 // A row's blocks joined, one wave a row, in the same way: a floor under the k

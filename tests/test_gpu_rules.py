@@ -317,3 +317,17 @@ def test_a_single_row_of_any_stride():
         plan(logits, torch.empty((5001, 1), device="cuda").t(), token, logprob)
         got.append((token, logprob))
     assert column.t().stride(0) == 1 and torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [300, 4096])
+def test_many_biases(n, dtype):
+    """Hundreds of biases on few tokens and on many, sums in list order across the whole list."""
+    V = 20011
+    rng = np.random.default_rng(14)
+    rules = all_rules(rng, 4, V, n=n, b=777)
+    rules["bias_token"][0] = rng.integers(8100, 8300, 777)
+    rules["bias_token"][1] = rng.integers(0, 3, 777) * 5000
+    rules["bias_value"][:] = rng.uniform(-1e3, 1e3, (4, 777))
+    rules["bias_len"][:] = [777, 770, 321, 65]
+    check(normal(rng, 4, V), rules, 6, dtype)
