@@ -149,11 +149,12 @@ __device__ __forceinline__ uint64_t left_by(const RulesLaunch& a, const uint64_t
   return a.counters ? load_agent(p) : *p;
 }
 
-// How many of the first n lanes' results x are better than `mine`.
-__device__ __forceinline__ int better(uint64_t x, int n, uint64_t mine) {
+// How many of the results x of the lanes `in` are better than `mine`.
+__device__ __forceinline__ int better(uint64_t x, uint64_t in, uint64_t mine) {
   int count = 0;
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) {
+  while (in) {
+    const int i = __ffsll((unsigned long long)in) - 1;
+    in &= in - 1;
     const uint64_t y = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(x >> 32), i) << 32 |
                        (uint32_t)__builtin_amdgcn_readlane((uint32_t)x, i);
     count += y > mine;
@@ -189,6 +190,7 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
   extern __shared__ __attribute__((aligned(16))) uint32_t table[];   // [TOKENS] where there are lists
   __shared__ uint64_t cand[SUBS * 4][RU_CAND];
   __shared__ int cand_n[SUBS * 4];
+  __shared__ uint32_t cand_least[SUBS * 4];
   __shared__ float wave_ms[SUBS * 4][2];
   const int tid = threadIdx.x % RU_NT, sub = threadIdx.x / RU_NT, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -376,9 +378,10 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
   // the wave's candidates, its k best among them: what is not below the floor
   const auto token_of = [&](int i) { return v0 + ((i / VEC) * RU_NT + tid) * VEC + i % VEC; };
   int n = RU_CAND + 1;
+  uint32_t least_rank = 0;
   if (sum == sum) {                                    // (a NaN or +inf would not compare: the other way)
-    const float least = a.k == 1 ? fmaxf(mx, -3.402823466e38f)
-                                 : from_ordered_u32(max(rank_floor(rank_of(largest), a.k), kLowest));
+    least_rank = max(a.k == 1 ? rank_of(mx) : rank_floor(rank_of(largest), a.k), kLowest);
+    const float least = from_ordered_u32(least_rank);
     n = 0;
 #pragma unroll
     for (int i = 0; i < RU_E; ++i) {
@@ -390,6 +393,7 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
     }
   }
   if (n > RU_CAND) {
+    least_rank = 0;
     // many equal ones: k rounds, each lane offering the best that it has not yet given
     uint32_t given = 0;
     for (n = 0; n < a.k; ++n) {
@@ -411,28 +415,40 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
       }
     }
   }
-  if (lane == 0) cand_n[wave] = n;
+  if (lane == 0) {
+    cand_n[wave] = n;
+    cand_least[wave] = least_rank;
+  }
   __syncthreads();
   if (v0 >= V) return true;
-  // the 256 threads': a candidate's place is the number of better ones
+  // the 256 threads': a candidate's place is the number of better ones, and none
+  // below the highest floor of their waves has a place below k
   const int chunk = blockIdx.x * SUBS + sub, w0 = wave & ~3;
   uint64_t* keys = (uint64_t*)(a.ws + (int64_t)a.rows * chunks * 2) + ((int64_t)row * chunks + chunk) * a.k;
   int m[4], have = 0;
+  uint32_t least = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) have += m[w] = __builtin_amdgcn_readfirstlane(cand_n[w0 + w]);
+  for (int w = 0; w < 4; ++w) {
+    have += m[w] = __builtin_amdgcn_readfirstlane(cand_n[w0 + w]);
+    least = max(least, (uint32_t)__builtin_amdgcn_readfirstlane(cand_least[w0 + w]));
+  }
+  const auto above = [&](uint64_t x) { return __ballot(x && (uint32_t)(x >> 32) >= least); };
   if (have <= 64) {                                    // one wave, a candidate a lane
     if (wave == w0) {
       const int w = (lane >= m[0]) + (lane >= m[0] + m[1]) + (lane >= m[0] + m[1] + m[2]);
       const int at = lane - (w > 0 ? m[0] : 0) - (w > 1 ? m[1] : 0) - (w > 2 ? m[2] : 0);
       const uint64_t mine = lane < have ? cand[w0 + w][at] : 0;
-      const int place = better(mine, have, mine);
+      const int place = better(mine, above(mine), mine);
       if (lane < have && place < a.k) leave(a, keys + place, mine);
     }
   } else {
     const uint64_t mine = lane < n ? cand[wave][lane] : 0;
     int place = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) place += better(lane < m[w] ? cand[w0 + w][lane] : 0, m[w], mine);
+    for (int w = 0; w < 4; ++w) {
+      const uint64_t x = lane < m[w] ? cand[w0 + w][lane] : 0;
+      place += better(x, above(x), mine);
+    }
     if (lane < n && place < a.k) leave(a, keys + place, mine);
   }
   if (wave == w0) {
@@ -515,7 +531,7 @@ __device__ __forceinline__ void join_row(const RulesLaunch& a, int chunks, int r
   wave_lds_done();
   if (have <= RU_CAND) {
     const uint64_t mine = lane < have ? cand[lane] : 0;
-    const int place = better(mine, have, mine);
+    const int place = better(mine, __ballot(lane < have), mine);
     if (lane < have && place < a.k) put(place, mine);
     if (lane >= have && lane < a.k) put(lane, 0);
     return;
