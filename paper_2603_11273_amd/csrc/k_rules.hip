@@ -59,6 +59,34 @@ struct Logits<bf16_t> {
   }
 };
 
+// x / d of N values, correctly rounded, one divisor for all.  With r the rounded
+// 1 / d, q = x r is off by 2 steps at most, one correction q += r (x - q d) makes
+// it one of the two floats around x / d, and a second one, by Markstein's theorem,
+// the nearest: 5 instructions where a division by itself takes 11.  The theorem
+// wants x - q d exact, hence no quotient or residual near the ends of the range;
+// a wave with such values (infinities among them) divides.
+template <int N>
+__device__ __forceinline__ void divide(const float* x, float d, float r, float* y) {
+  float hi = 0.f;
+  uint32_t lo = 0xffffffffu;                           // (of the magnitudes' bits but zeros')
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    hi = fmaxf(hi, fabsf(x[i]));
+    lo = min(lo, (__float_as_uint(x[i]) << 1) - 1u);
+  }
+  if (!(d >= 0x1p-20f && d <= 0x1p20f) || __any(hi > 0x1p100f || lo < (__builtin_bit_cast(uint32_t, 0x1p-70f) << 1) - 1u)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = x[i] / d;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float q = x[i] * r;
+    q = fmaf(fmaf(-q, d, x[i]), r, q);
+    y[i] = fmaf(fmaf(-q, d, x[i]), r, q);
+  }
+}
+
 // Order of the results: larger first, a NaN before all, the lower token of two
 // equal ones (0 and -0 are); 0 for what is never chosen.
 __device__ __forceinline__ uint32_t rank_of(float z) {
@@ -257,6 +285,7 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
     __syncthreads();
     count_tokens<NT, TOKENS>(hist, SUBS == 1 ? said : nullptr, prompt, hist_n, b0, table);
     __syncthreads();
+    const float rep_r = 1.f / rep;
 #pragma unroll
     for (int i = 0; i < RU_E / 4; ++i) {
       const int u = i * 4 / VEC * RU_NT * VEC + tid * VEC + i * 4 % VEC;
@@ -264,10 +293,12 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
       const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
       // (few of the wave's tokens were said, mostly none: no division for them)
       if (!__any(c4.x | c4.y | c4.z | c4.w)) continue;
+      float q[4];
+      divide<4>(z + 4 * i, rep, rep_r, q);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float x = z[4 * i + j];
-        x = x > 0.f ? x / rep : x * rep;
+        x = x > 0.f ? q[j] : x * rep;
         const uint32_t times = c[j] & ~kSeen;
         if (times) x = (x - freq * (float)times) - pres;
         z[4 * i + j] = c[j] ? x : z[4 * i + j];
@@ -324,16 +355,15 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
       }
     }
   }
+  if (temp > 0.f && temp != 1.f) divide<RU_E>(z, temp, 1.f / temp, z);
   if (masked) {
+    // (after the division, which infinities would slow down)
+    const float none = temp > 0.f ? -INFINITY / temp : -INFINITY;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < VEC; ++j)
-        if (!(words[i] >> j & 1)) z[i * VEC + j] = -INFINITY;
-  }
-  if (temp > 0.f && temp != 1.f) {
-#pragma unroll
-    for (int i = 0; i < RU_E; ++i) z[i] = z[i] / temp;
+        if (!(words[i] >> j & 1)) z[i * VEC + j] = none;
   }
   if (a.out) {
     float* dst = a.out + (int64_t)row * a.out_ld + v0;

@@ -331,3 +331,22 @@ def test_many_biases(n, dtype):
     rules["bias_value"][:] = rng.uniform(-1e3, 1e3, (4, 777))
     rules["bias_len"][:] = [777, 770, 321, 65]
     check(normal(rng, 4, V), rules, 6, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_divisions_of_any_size(dtype):
+    """Quotients are float32's own: ordinary values, all exponents, zeros, values at the range's ends."""
+    rng = np.random.default_rng(15)
+    by = np.array([0.7, np.float32(1) / 3, 1.9999999, 1.0000001, 2.0 ** -20, 2.0 ** 20, 1e-25, 1e25, 3.0, np.inf], f)
+    rows, V = len(by), 9001
+    x = normal(rng, rows, V)
+    wild = (rng.standard_normal((rows, V)) * np.exp2(rng.uniform(-140, 126, (rows, V)))).astype(f)
+    x[:, 4500:] = wild[:, 4500:]                            # whole waves of them, and some among ordinary ones
+    x[:, :2000:50] = wild[:, :2000:50]
+    x[:, 2000:4000:7] = 0.0
+    rules = {"temperature": by, "history": rng.integers(0, V, (rows, 3000)).astype(np.int32),
+             "history_len": np.full(rows, 3000, np.int32), "repetition": by[::-1].copy(),
+             "allowed": rng.random((1, V)) < 0.9, "mask_of": np.zeros(rows, np.int32)}
+    with np.errstate(all="ignore"):
+        check(x, rules, 0, dtype)
+        check(x, {"temperature": by}, 0, dtype)
