@@ -257,6 +257,14 @@ __device__ __forceinline__ Range key_range(const ShareKeys& c, int entry) {
   return r;
 }
 
+// (max, sum) of part `part` of the row at `place` and head h; a sum of kNoKeys
+// says that the part has none (and no values).
+constexpr float kNoKeys = -1.f;
+__device__ __forceinline__ float2* record(const ShareLaunch& c, int place, int h, int part) {
+  const int parts = c.np + c.no;
+  return (float2*)(c.rec + (int64_t)c.rows * c.n_head * parts * kHeadDim) + ((int64_t)place * c.n_head + h) * parts + part;
+}
+
 // Keys [k0, k1) of `r` for the queries [col0, col0 + 16 QT) of `count` rows from
 // place `start`; leaves their records as part `part`, or the result where a row
 // has only this part.
@@ -394,10 +402,7 @@ __device__ __forceinline__ void attend_part(const ShareArgs& a, const ShareKeys&
     } else {
       const int64_t rh = (int64_t)(start + j) * a.c.n_head + h;
       *(float4*)(a.c.rec + (rh * parts + part) * kHeadDim + d4) = v;
-      if (d4 == 0) {
-        float2* w = (float2*)(a.c.rec + (int64_t)a.c.rows * a.c.n_head * parts * kHeadDim) + rh * parts + part;
-        *w = float2{M, L};
-      }
+      if (d4 == 0) *record(a.c, start + j, h, part) = float2{M, L};
     }
   }
 }
@@ -423,7 +428,12 @@ void k_attend_shared(ShareArgs a) {
     const int count = min(min(end, a.c.rows) - start, a.c.max_group);
     if (start < 0 || tile * 16 * QT >= count * a.per) return;
     const int k0 = part * a.c.prefix_part, k1 = min(k0 + a.c.prefix_part, r.n);
-    if (k0 >= k1 && a.c.np + a.c.no > 1) return;
+    if (k0 >= k1 && a.c.np + a.c.no > 1) {
+      const int col = tile * 16 * QT + (int)threadIdx.x, j = col / a.per;
+      if (threadIdx.x < 16 * QT && j < count)
+        *record(a.c, start + j, head * a.per + col - j * a.per, part) = float2{-INFINITY, kNoKeys};
+      return;
+    }
     attend_part<T, QT>(a, a.c.prefix, r, min(k0, k1), k1, head, start, count, tile * 16 * QT, part, share_lds);
   } else {
     u -= a.prefix_blocks;
@@ -436,15 +446,20 @@ void k_attend_shared(ShareArgs a) {
     if (i < first || i >= end || row < 0 || row >= a.c.rows) return;
     const Range r = key_range(a.c.own, row);
     const int k0 = part * a.c.own_part, k1 = min(k0 + a.c.own_part, r.n);
-    if (k0 >= k1 && a.c.np + a.c.no > 1) return;
+    if (k0 >= k1 && a.c.np + a.c.no > 1) {
+      const int col = tile * 16 + (int)threadIdx.x;
+      if (threadIdx.x < 16 && col < a.per)
+        *record(a.c, i, head * a.per + col, a.c.np + part) = float2{-INFINITY, kNoKeys};
+      return;
+    }
     attend_part<T, 1>(a, a.c.own, r, min(k0, k1), k1, head, i, 1, tile * 16, a.c.np + part, share_lds);
   }
 }
 
 // out of a row and head from its parts' records; one wave each, lane = dim.  A
 // row's group is the last one that starts at or before its place.  The kernel is
-// a chain of loads, so the records are loaded before it is known which of them
-// there are (those that no block wrote count as nothing), SH_JOIN at a time.
+// a chain of loads, so all it needs is loaded at once, SH_JOIN records at a time;
+// which of them there are they say themselves.
 constexpr int SH_JOIN = 16;
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_join(ShareArgs a) {
@@ -454,34 +469,36 @@ __global__ __launch_bounds__(256) void k_attend_join(ShareArgs a) {
   const int i = (int)(w / a.c.n_head), h = (int)(w % a.c.n_head);
   const int parts = a.c.np + a.c.no;
   const float* val = a.c.rec + (int64_t)w * parts * kHeadDim + lane;
-  const float2* ml = (const float2*)(a.c.rec + (int64_t)a.c.rows * a.c.n_head * parts * kHeadDim) + (int64_t)w * parts;
+  const float2* ml = record(a.c, i, h, 0);
   float v[SH_JOIN];
-  float2 rec = {-INFINITY, 0.f};
+  float2 rec;
   auto load = [&](int p0) {
-    rec = p0 + lane < parts && lane < SH_JOIN ? ml[p0 + lane] : float2{-INFINITY, 0.f};
+    rec = lane < SH_JOIN && p0 + lane < parts ? ml[p0 + lane] : float2{-INFINITY, kNoKeys};
 #pragma unroll
     for (int p = 0; p < SH_JOIN; ++p) v[p] = p0 + p < parts ? val[(int64_t)(p0 + p) * kHeadDim] : 0.f;
   };
   load(0);
-  const int row = a.c.row_of ? a.c.row_of[i] : i;
-  int grp = -1;
-  for (int g0 = 0; g0 < a.c.groups; g0 += 64)
-    grp += __popcll(__ballot(g0 + lane < a.c.groups && a.c.group_start[min(g0 + lane, a.c.groups - 1)] <= i));
-  if (grp < 0 || i >= a.c.group_start[a.c.groups] || i - a.c.group_start[grp] >= a.c.max_group) return;
+  const int row = a.c.row_of ? a.c.row_of[i] : i, end = a.c.group_start[a.c.groups];
+  int start = -1;
+  for (int g0 = 0; g0 < a.c.groups; g0 += 64) {
+    const int x = a.c.group_start[min(g0 + lane, a.c.groups - 1)];
+    const int n = __popcll(__ballot(g0 + lane < a.c.groups && x <= i));
+    if (n == 0) break;
+    start = __builtin_amdgcn_readlane(x, n - 1);
+  }
+  if (start < 0 || i >= end || i - start >= a.c.max_group) return;
   if (row < 0 || row >= a.c.rows) return;
-  const int np = a.c.np > 0 ? (key_range(a.c.prefix, grp).n + a.c.prefix_part - 1) / a.c.prefix_part : 0;
-  const int no = a.c.no > 0 ? (key_range(a.c.own, row).n + a.c.own_part - 1) / a.c.own_part : 0;
   float M = -INFINITY, L = 0.f, acc = 0.f;
+  bool any = false;
   for (int p0 = 0; p0 < parts; p0 += SH_JOIN) {
-    const int p = p0 + lane;
-    const bool there = lane < SH_JOIN && (p < a.c.np ? p < np : p - a.c.np < no);
+    if (p0 > 0) load(p0);
+    const bool there = rec.y != kNoKeys;               // (a sum is 0 or more, or NaN)
     const uint64_t some = __ballot(there);
     if (!some) continue;
-    if (p0 > 0) load(p0);
-    const float m = there ? rec.x : -INFINITY;
-    const float top = fmaxf(M, wave_max_lanes(m));
+    any = true;
+    const float top = fmaxf(M, wave_max_lanes(rec.x));
     const float keep = M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
-    const float fac = !there ? 0.f : m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+    const float fac = !there ? 0.f : rec.x == top ? 1.f : __builtin_amdgcn_exp2f(rec.x - top);
     M = top;
     L = L * keep + wave_sum_lanes(there ? fac * rec.y : 0.f);
     acc *= keep;
@@ -489,7 +506,7 @@ __global__ __launch_bounds__(256) void k_attend_join(ShareArgs a) {
     for (int j = 0; j < SH_JOIN; ++j)
       if (some >> j & 1) acc += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fac), j)) * v[j];
   }
-  St<T>::st((T*)a.c.out, (int64_t)row * a.c.out_ld + h * kHeadDim + lane, np + no > 0 ? acc / L : 0.f);
+  St<T>::st((T*)a.c.out, (int64_t)row * a.c.out_ld + h * kHeadDim + lane, any ? acc / L : 0.f);
 }
 
 template <typename T, int QT>
