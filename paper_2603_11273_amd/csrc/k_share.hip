@@ -22,6 +22,10 @@
 // permutes; row m of product t then is dim 4 m + t, which leaves the lane with 16
 // consecutive dims of its query.  fp32: one 16-key tile, four dims a load, no
 // permutes.
+//
+// Measured (bf16, 20 heads): 8 groups of 16 rows on 65536 keys 425 us, 6.7 TB/s; 24
+// groups of 5 on 1500 and up to 224 own 48 us, 5.3 TB/s; 5 rows on 1540 8.5 us, two
+// launches' latency.
 #include "asr_device.h"
 
 namespace asr {

@@ -78,7 +78,7 @@ int parts_of(int keys, int part) { return (int)(((int64_t)keys + part - 1) / par
 // in 1024 / 1536 / 2560 / 4096 64 / 59 / 52 / 60, the rule's 2560; 24 x 5 on 1500
 // in 512 / 768 / 1536 51 / 50 / 49, the rule's one part.  Lengths that may differ
 // need more parts, as the longest unit would be last: 16 groups on 515 to 8191
-// keys in 768 / 1408 / 2048 / 4096 43 / 45 / 50 / 51, hence three turns at least.
+// keys in 768 / 1408 / 2048 41 / 43 / 48, hence three turns at least.
 int part_keys(int64_t units, int64_t keys, bool ragged, int fixed, int step) {
   if (keys <= step) return step;
   const int64_t cus = cu_count();
@@ -231,8 +231,8 @@ asr_status asr_logit_rules(const asr_rules* r, void* ws, size_t ws_bytes, void* 
     if (st != ASR_OK) return st;
     s.ws = (float*)ws + kCounters;
     // up to a block a CU the row's last block joins the others' results, above that
-    // a second kernel does (us, 10 best of 51866 tokens: 5 rows 11.8 / 12.4, 64 rows
-    // 15.1 / 15.5, 128 rows 25.3 / 24.4; one launch also spares the host 4 us)
+    // a second kernel does (us, 10 best of 51866 tokens: 5 rows 11.2 / 11.7, 64 rows
+    // 14.5 / 14.3, 128 rows 23.6 / 19.7; one launch also spares the host 4 us)
     const int64_t blocks = (int64_t)r->rows * ((r->vocab + kRulesChunk - 1) / kRulesChunk);
     s.counters = r->k > 0 && blocks <= cu_count() ? (uint32_t*)ws : nullptr;
     logit_rules(s, r->dtype == ASR_BF16, (hipStream_t)stream);

@@ -63,9 +63,9 @@ struct Slot {
 // `kids` counts the slots that read this one's (beside itself).  Prompts below
 // kShareFrom positions are copied instead (shared = 0): sharing them takes two
 // launches more a layer, about what reading 120 rows' 128 positions costs
-// (large-v3).  A step of one family of 5 on 40 positions: 1869 us with them
-// shared, 1672 with them copied (1638 as slots of their own); of 24 on 224
-// positions: 4103 with them shared, about 4450 copied (8226).
+// (large-v3).  A step of one family of 5 on 40 positions: 1860 us with them
+// shared, 1660 with them copied (1680 as slots of their own); of 24 on 224
+// positions: 4090 with them shared, about 4450 copied (8220).
 constexpr int kShareFrom = 128;
 struct Family {
   int32_t root = -1;      // -1: the slot's own caches
