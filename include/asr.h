@@ -268,7 +268,7 @@ typedef struct {
   int32_t policy;         /* policy the step ran under (asr_policy) */
   int64_t* preempted;     int32_t n_preempted;
   int64_t* admitted;      int32_t* admitted_slot;  int32_t n_admitted;
-  int64_t* decoded;       int32_t* token;          int32_t n_decoded;  /* token -1: no model ran */
+  int64_t* decoded;       int32_t* token;          int32_t n_decoded;  /* token -1: no model ran, or no next token */
   int64_t* finished;      int32_t n_finished;
 } asr_serve_out;
 
@@ -277,7 +277,11 @@ typedef struct {
  * occupied or popped requests wait; EINVAL for an inconsistent config. */
 asr_status asr_serve_config(asr_ctx* ctx, const asr_serve_cfg* cfg);
 /* One engine step on the GPU: plan, prefill the admitted requests, decode
- * every running request, commit.  Synchronises on the bound stream. */
+ * every running request, commit.  Synchronises on the bound stream.  A request
+ * whose rules (asr_set_slot_rules) allow no next token finishes with those it
+ * has; its token in this step is -1.  So does one whose logits hold a NaN (or,
+ * under rules, whose best logit is infinite), and the step then returns EDEVICE
+ * with `out` filled and every other request one token on. */
 asr_status asr_serve_step(asr_ctx* ctx, int64_t now_us, asr_serve_out* out);
 /* The same schedule without running the model (tokens -1), for queue-only
  * contexts (device = -1; ESTATE otherwise): simulations and CPU tests. */

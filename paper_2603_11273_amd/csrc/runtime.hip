@@ -1605,15 +1605,19 @@ StepShape arrange_rows(asr_ctx* c, int D, const int32_t* slots, const int32_t* t
   return sh;
 }
 
+// What keeps a row from having a next token, if anything does.
+enum class RowFault : char { NONE, NO_TOKEN, NOT_FINITE };
+
 // Decode rows (slot, token, position) -> argmax (and logits when asked, and the
 // k best tokens where k > 0).  Returns EDEVICE after the copies when an argmax is a
-// NaN logit's, or no token is allowed.  The rows
+// NaN logit's, or no token is allowed; with `faults` OK, and what each row has.  The rows
 // go up in one copy and their results down in one: each small copy is a trip of
 // its own through the queue (one tiny fp32 row: 282 us with five copies, a flag
 // to clear and a slower argmax, 256 with two).
 asr_status run_decode(asr_ctx* c, int D, const int32_t* slots, const int32_t* tokens,
                       const std::vector<int32_t>& pos, int32_t* argmax, float* logits, int k = 0,
-                      int32_t* best = nullptr, float* logprob = nullptr) {
+                      int32_t* best = nullptr, float* logprob = nullptr, std::vector<RowFault>* faults = nullptr) {
+  if (faults) faults->assign(D, RowFault::NONE);
   if (D == 0) return ASR_OK;
   StepIO io;
   const StepShape sh = arrange_rows(c, D, slots, tokens, pos, k, io);
@@ -1626,24 +1630,28 @@ asr_status run_decode(asr_ctx* c, int D, const int32_t* slots, const int32_t* to
   if (st != ASR_OK) return st;
   HIPCHK(synced);
   const char* bad = nullptr;
+  auto fault = [&](int row, RowFault f, const char* what) {
+    bad = what;
+    if (faults) (*faults)[row] = f;
+  };
   for (int i = 0; i < D; ++i) {
     const int row = io.order[i];
     if (sh.k == 0) {
-      if (am[i] < 0) bad = "NaN logit";
+      if (am[i] < 0) fault(row, RowFault::NOT_FINITE, "NaN logit");
       argmax[row] = am[i] < 0 ? -1 - am[i] : am[i];
       continue;
     }
     argmax[row] = io.best[(size_t)i * sh.k];
     if (argmax[row] < 0)
-      bad = "the rules of a row allow no token";
+      fault(row, RowFault::NO_TOKEN, "the rules of a row allow no token");
     else if (std::isnan(io.logprob[(size_t)i * sh.k]))
-      bad = "NaN or infinite logit";
+      fault(row, RowFault::NOT_FINITE, "NaN or infinite logit");
     for (int j = 0; j < k; ++j) {
       best[(size_t)row * k + j] = io.best[(size_t)i * k + j];
       logprob[(size_t)row * k + j] = io.logprob[(size_t)i * k + j];
     }
   }
-  return bad ? fail(ASR_EDEVICE, bad) : ASR_OK;
+  return bad && !faults ? fail(ASR_EDEVICE, bad) : ASR_OK;
 }
 
 }  // namespace
@@ -1964,8 +1972,9 @@ asr_status serve_plan_step(asr_ctx* c, int64_t now_us, const asr_serve_out* out,
   return ASR_OK;
 }
 
-void serve_finish(asr_ctx* c, const ServePlan& p, const int32_t* tokens, asr_serve_out* out) {
-  std::vector<int64_t> fin = c->serve.commit(p, tokens);
+void serve_finish(asr_ctx* c, const ServePlan& p, const int32_t* tokens, asr_serve_out* out,
+                  const std::vector<char>* ended = nullptr) {
+  std::vector<int64_t> fin = c->serve.commit(p, tokens, nullptr, ended);
   out->policy = p.policy;
   out->n_preempted = (int32_t)p.preempted.size();
   for (size_t i = 0; i < p.preempted.size(); ++i) out->preempted[i] = p.preempted[i];
@@ -2029,6 +2038,7 @@ asr_status asr_serve_step(asr_ctx* c, int64_t now_us, asr_serve_out* out) {
   }
   const int D = (int)p.dec_id.size(), A = (int)p.admitted.size();
   std::vector<int32_t> tok(D);
+  std::vector<RowFault> faults;
   for (int32_t slot : p.admitted_slot) {
     st = start_rules(c, slot);
     if (st != ASR_OK) return st;
@@ -2053,17 +2063,31 @@ asr_status asr_serve_step(asr_ctx* c, int64_t now_us, asr_serve_out* out) {
     gemm_set_cu_reserve(0);
     c->stream = main_stream;
     if (st == ASR_OK)
-      st = run_decode(c, D, p.dec_slot.data(), p.dec_token.data(), p.dec_pos, tok.data(), nullptr);
+      st = run_decode(c, D, p.dec_slot.data(), p.dec_token.data(), p.dec_pos, tok.data(), nullptr, 0, nullptr, nullptr,
+                      &faults);
     HIPCHK(hipStreamSynchronize(c->pstream));    // the prefill and its stage's host arrays
     if (st != ASR_OK) return st;
   } else {
     st = run_prefill(c, reqs, p.admitted_slot);
     if (st != ASR_OK) return st;
-    st = run_decode(c, D, p.dec_slot.data(), p.dec_token.data(), p.dec_pos, tok.data(), nullptr);
+    st = run_decode(c, D, p.dec_slot.data(), p.dec_token.data(), p.dec_pos, tok.data(), nullptr, 0, nullptr, nullptr,
+                    &faults);
     if (st != ASR_OK) return st;
   }
-  serve_finish(c, p, tok.data(), out);
-  return collect_timing(c);
+  // a row without a next token ends its request: planned again it would fail again,
+  // and nothing else would move
+  std::vector<char> ended(D, 0);
+  int64_t broken = -1;
+  for (int i = 0; i < D; ++i) {
+    if (faults[i] == RowFault::NONE) continue;
+    ended[i] = 1;
+    tok[i] = -1;
+    if (faults[i] == RowFault::NOT_FINITE) broken = p.dec_id[i];
+  }
+  serve_finish(c, p, tok.data(), out, &ended);
+  st = collect_timing(c);
+  if (st != ASR_OK || broken < 0) return st;
+  return fail(ASR_EDEVICE, "NaN or infinite logit of request " + std::to_string(broken));
 }
 
 asr_status asr_serve_simulate(asr_ctx* c, const asr_sim_cost* cost, int64_t t0_us, int32_t n,

@@ -113,7 +113,7 @@ ServePlan ServeEngine::plan(int64_t now_us, WaitQueue& q) {
 }
 
 std::vector<int64_t> ServeEngine::commit(const ServePlan& p, const int32_t* tokens,
-                                         std::vector<int32_t>* gen_after) {
+                                         std::vector<int32_t>* gen_after, const std::vector<char>* ended) {
   std::vector<int64_t> finished;
   if (gen_after) gen_after->assign(p.dec_id.size(), 0);
   for (size_t i = 0; i < p.dec_id.size(); ++i) {
@@ -121,6 +121,11 @@ std::vector<int64_t> ServeEngine::commit(const ServePlan& p, const int32_t* toke
     auto it = std::find_if(run_.begin(), run_.end(),
                            [&](const RunEntry& r) { return r.q.id == p.dec_id[i]; });
     if (it == run_.end()) continue;
+    if (ended && (*ended)[i]) {
+      it->total = it->generated;
+      if (gen_after) (*gen_after)[i] = it->generated;
+      continue;
+    }
     const int32_t t = tokens ? tokens[i] : -1;
     it->tokens.push_back(t);
     it->last_token = t;

@@ -87,11 +87,13 @@ class ServeEngine {
   ServePlan plan(int64_t now_us, WaitQueue& q);
 
   // Apply a step's outputs: tokens[i] is the token produced by decode row i
-  // (NULL when no model ran: tokens are recorded as -1).  Returns the ids
-  // that finished; gen_after (optional) receives each decode row's token
-  // count after the step.
+  // (NULL when no model ran: tokens are recorded as -1).  A row that `ended`
+  // (optional) marks has no next token: its request finishes with those it has.
+  // Returns the ids that finished; gen_after (optional) receives each decode
+  // row's token count after the step.
   std::vector<int64_t> commit(const ServePlan& p, const int32_t* tokens,
-                              std::vector<int32_t>* gen_after = nullptr);
+                              std::vector<int32_t>* gen_after = nullptr,
+                              const std::vector<char>* ended = nullptr);
 
   // Tokens of a finished request (once), false when unknown.
   bool take_result(int64_t id, std::vector<int32_t>* tokens);

@@ -1,0 +1,168 @@
+// Hypotheses, rules and their decode steps on the CPU: the program defines the HIP calls of the
+// library itself ("device" memory is host memory, kernels do nothing, copies happen at once), says
+// what the kernels left for the copies back, and checks what the library makes of it.  One scenario
+// per name on the command line.
+#include <cmath>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <functional>
+#include <string>
+#include <vector>
+
+#include "asr.h"
+
+namespace {
+// called before each copy to the host with what it copies and its number since the last wait
+std::function<void(void* src, size_t n, int number)> results;
+int copies = 0;
+int graphs = 0;          // that are kept
+constexpr int kToHost = 2;
+}  // namespace
+
+extern "C" {
+int hipGetDeviceCount(int* n) { *n = 1; return 0; }
+int hipSetDevice(int) { return 0; }
+int hipGetDevice(int* d) { *d = 0; return 0; }
+int hipDeviceGetAttribute(int* v, int, int) { *v = 256; return 0; }
+int hipOccupancyMaxActiveBlocksPerMultiprocessor(int* n, const void*, int, size_t) { *n = 1; return 0; }
+int hipFuncSetAttribute(const void*, int, int) { return 0; }
+int hipLaunchKernel(const void*, unsigned long long, unsigned long long, void**, size_t, void*) { return 0; }
+int hipGetLastError() { return 0; }
+const char* hipGetErrorString(int) { return "made to fail"; }
+int hipMemcpyAsync(void* dst, const void* src, size_t n, int kind, void*) {
+  if (kind == kToHost && results) results(const_cast<void*>(src), n, copies++);
+  memcpy(dst, src, n);
+  return 0;
+}
+int hipStreamSynchronize(void*) { copies = 0; return 0; }
+int hipDeviceSynchronize() { return 0; }
+int hipStreamCreateWithFlags(void** s, unsigned) { *s = malloc(1); return 0; }
+int hipStreamDestroy(void* s) { free(s); return 0; }
+int hipEventCreateWithFlags(void** e, unsigned) { *e = malloc(1); return 0; }
+int hipEventDestroy(void* e) { free(e); return 0; }
+int hipEventRecord(void*, void*) { return 0; }
+int hipStreamWaitEvent(void*, void*, unsigned) { return 0; }
+int hipStreamBeginCapture(void*, int) { return 0; }
+int hipStreamEndCapture(void*, void** g) { *g = malloc(1); return 0; }
+int hipGraphDestroy(void* g) { free(g); return 0; }
+int hipGraphInstantiate(void** ex, void*, void*, char*, size_t) { *ex = malloc(1); ++graphs; return 0; }
+int hipGraphExecDestroy(void* ex) { free(ex); --graphs; return 0; }
+int hipGraphLaunch(void*, void*) { return 0; }
+}
+
+#define OK(x)                                                                       \
+  do {                                                                              \
+    if ((x) != ASR_OK) return printf("%s: %s\n", #x, asr_last_error()), 1;          \
+  } while (0)
+#define CHECK(x)                                                                    \
+  do {                                                                              \
+    if (!(x)) return printf("line %d: %s (last error: %s)\n", __LINE__, #x, asr_last_error()), 1; \
+  } while (0)
+
+namespace {
+
+struct Context {
+  asr_ctx* c = nullptr;
+  void *block = nullptr, *hyp = nullptr;
+  ~Context() {
+    if (c) asr_destroy(c);
+    free(block);
+    free(hyp);
+  }
+  int make(int n_enc, int slots, int vocab, int max_bias, int n_masks) {
+    asr_model_cfg cfg{80, 64, n_enc, 1, 1, 64, vocab, ASR_F32, slots, 1, slots, 16};
+    OK(asr_create(&cfg, 0, &c));
+    size_t bytes = 0;
+    OK(asr_workspace_size(c, &bytes));
+    block = aligned_alloc(256, bytes);
+    memset(block, 0, bytes);
+    OK(asr_bind(c, block, bytes, nullptr));
+    int32_t n = 0;
+    OK(asr_n_params(c, &n));
+    std::vector<std::vector<float>> data(n);
+    std::vector<const float*> tensors(n);
+    for (int i = 0; i < n; ++i) {
+      int64_t numel = 0;
+      OK(asr_param_numel(c, i, &numel));
+      data[i].resize(numel);
+      tensors[i] = data[i].data();
+    }
+    OK(asr_load_weights(c, tensors.data(), n, 0));
+    OK(asr_hypotheses_size(c, max_bias, n_masks, &bytes));
+    hyp = aligned_alloc(256, bytes);
+    memset(hyp, 0, bytes);
+    OK(asr_bind_hypotheses(c, max_bias, n_masks, hyp, bytes));
+    return 0;
+  }
+};
+
+// Three requests on two slots under default rules: a row whose rules allow no token and a row
+// with a NaN end their own requests, and everything else goes on.
+int serve() {
+  Context x;
+  if (x.make(1, 2, 40, 0, 1)) return 1;
+  asr_slot_rules rules{1.f, 0.f, 0.f, 1.f, 0, 0, 0, nullptr, nullptr};
+  OK(asr_set_slot_rules(x.c, -1, &rules));
+  asr_serve_cfg cfg{};
+  cfg.cross_tokens = 1500;
+  cfg.max_admit = 1;
+  cfg.tok_num = 27;
+  cfg.tok_den = 10;
+  cfg.start_token = 1;
+  OK(asr_serve_config(x.c, &cfg));
+  std::vector<float> pcm(64000, 0.f);
+  for (int64_t id = 0; id < 3; ++id) OK(asr_submit(x.c, id, pcm.data(), (int64_t)pcm.size(), 16000, 0, 0, 0, 0));
+  int64_t preempted[2], admitted[2], decoded[2], finished[2];
+  int32_t slot[2], token[2];
+  asr_serve_out out{2, 0, preempted, 0, admitted, slot, 0, decoded, token, 0, finished, 0};
+  int now = 0, dead = -1;
+  bool nan = false;
+  results = [&](void* src, size_t n, int number) {
+    for (size_t i = 0; i < n / 4; ++i) {
+      if (number == 0)
+        ((int32_t*)src)[i] = (int)i == dead && !nan ? -1 : 7 + now;
+      else
+        ((float*)src)[i] = (int)i == dead && nan ? NAN : -0.5f;
+    }
+  };
+  auto step = [&] { return asr_serve_step(x.c, now++, &out); };
+  for (int i = 0; i < 3; ++i) OK(step());
+  CHECK(out.n_decoded == 2 && decoded[0] == 0 && decoded[1] == 1 && out.n_finished == 0);
+  dead = 0;                                            // request 0, with three tokens by now
+  OK(step());
+  CHECK(out.n_decoded == 2 && token[0] == -1 && token[1] == 7 + now);
+  CHECK(out.n_finished == 1 && finished[0] == 0);
+  int32_t got[448], n = 0;
+  OK(asr_serve_tokens(x.c, 0, got, 448, &n));
+  CHECK(n == 3 && got[0] >= 7 && got[1] >= 7 && got[2] >= 7);
+  dead = -1;
+  OK(step());                                          // request 2 takes its slot
+  CHECK(out.n_admitted == 1 && admitted[0] == 2 && out.n_decoded == 2 && out.n_finished == 0);
+  dead = 1;                                            // (rows in the order of admission)
+  nan = true;
+  CHECK(step() == ASR_EDEVICE && strstr(asr_last_error(), "request 2"));
+  CHECK(out.n_decoded == 2 && token[1] == -1 && out.n_finished == 1 && finished[0] == 2);
+  OK(asr_serve_tokens(x.c, 2, got, 448, &n));
+  CHECK(n == 1);
+  dead = -1;
+  for (int i = 0; i < 40 && !(out.n_finished == 1 && finished[0] == 1); ++i) OK(step());
+  OK(asr_serve_tokens(x.c, 1, got, 448, &n));
+  CHECK(n == 11);                                      // 4 s at 2.7 tokens a second
+  for (int i = 0; i < n; ++i) CHECK(got[i] >= 7);
+  printf("serve: ok\n");
+  return 0;
+}
+
+}  // namespace
+
+int main(int argc, char** argv) {
+  for (int i = 1; i < argc; ++i) {
+    const std::string name = argv[i];
+    results = nullptr;
+    copies = 0;
+    const int bad = name == "serve" ? serve() : (printf("no scenario %s\n", argv[i]), 1);
+    if (bad) return bad;
+  }
+  return 0;
+}
