@@ -180,7 +180,9 @@ typedef struct {
  * position + 1 keys, produces its argmax; the position then advances).
  * Prefill happens before decode, so a slot prefilled here may be decoded in
  * the same call.  Errors: ESTATE, ENODEV, EINVAL (bad id/slot/token,
- * duplicate slot, position at 448), EFULL (no free slot), EDEVICE. */
+ * duplicate slot, position at 448), EFULL (no free slot), EDEVICE (a HIP
+ * error; or, with all arrays filled and every slot a step further, a row whose
+ * logits hold a NaN or whose rules allow no token: argmax -1). */
 asr_status asr_step(asr_ctx* ctx, const asr_step_in* in, asr_step_out* out);
 
 /* Frees a slot for reuse. */
@@ -469,7 +471,8 @@ asr_status asr_set_masks(asr_ctx* ctx, int32_t first, int32_t n, const uint32_t*
  * where fewer tokens are allowed; see asr_logit_rules).  argmax is the first
  * of them.  Errors as asr_step, ESTATE without a hypotheses block, EDEVICE when
  * a row's rules allow no token (its argmax is then -1) or a logit is NaN or
- * infinite. */
+ * +infinite: as in asr_step, all the arrays are filled then and every slot is a
+ * step further (a search goes on with the other rows). */
 asr_status asr_step_topk(asr_ctx* ctx, const asr_step_in* in, asr_step_out* out, int32_t k,
                          int32_t* tokens, float* logprobs);
 

@@ -15,6 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libasr_mi355x.so")
 
 ASR_OK, ASR_EINVAL, ASR_ENOMEM, ASR_EFULL, ASR_ENOTFOUND, ASR_ESTATE, ASR_ENODEV, ASR_EDEVICE = range(8)
+NOT_WRITTEN = -(1 << 31)     # in a result before a call: no token, no policy
 STATUS_NAMES = ["OK", "EINVAL", "ENOMEM", "EFULL", "ENOTFOUND", "ESTATE", "ENODEV", "EDEVICE"]
 FCFS, SJF, HRRN = 0, 1, 2
 F32, BF16 = 0, 1
@@ -115,9 +116,13 @@ class SlotRules(C.Structure):
 
 
 class AsrError(RuntimeError):
+    """An error status.  `results`: what the call would have returned, where it did all its work and
+    only a row of it has no next token (Context.step, Context.serve_step); None otherwise."""
+
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES[status] if 0 <= status < 8 else status}: {msg}")
         self.status = status
+        self.results = None
 
 
 def _load():
@@ -192,9 +197,11 @@ def _load():
 lib = _load()
 
 
-def _check(status):
+def _check(status, results=None):
     if status != ASR_OK:
-        raise AsrError(status, lib.asr_last_error().decode())
+        error = AsrError(status, lib.asr_last_error().decode())
+        error.results = results
+        raise error
 
 
 def _ptr(a):
@@ -506,13 +513,15 @@ class Context:
     # -- step -----------------------------------------------------------------
     def step(self, prefill_ids=(), slots=(), tokens=(), want_logits=False, topk=0):
         """Returns dict(slot_of, argmax, done, logits); with topk also top_token and top_logprob
-        [rows][topk] (see asr_step_topk)."""
+        [rows][topk] (see asr_step_topk).  Where a row has no next token (its rules allow none, or
+        its logits hold a NaN) the slots are a step further all the same: the AsrError's `results`
+        are this dict, of every row."""
         pids, p_pids = _i64(list(prefill_ids) or [0])
         sl, p_sl = _i32(list(slots) or [0])
         tk, p_tk = _i32(list(tokens) or [0])
         P, D = len(prefill_ids), len(slots)
         slot_of, p_so = _i32(np.zeros(max(P, 1)))
-        am, p_am = _i32(np.zeros(max(D, 1)))
+        am, p_am = _i32(np.full(max(D, 1), NOT_WRITTEN))
         done, p_dn = _i32(np.zeros(max(D, 1)))
         logits = None
         p_lg = None
@@ -525,14 +534,16 @@ class Context:
         if topk:
             top = np.zeros((max(D, 1), topk), np.int32)
             logp = np.zeros((max(D, 1), topk), np.float32)
-            _check(lib.asr_step_topk(self.h, C.byref(sin), C.byref(sout), topk,
-                                     top.ctypes.data_as(C.POINTER(C.c_int32)),
-                                     logp.ctypes.data_as(C.POINTER(C.c_float))))
+            status = lib.asr_step_topk(self.h, C.byref(sin), C.byref(sout), topk,
+                                       top.ctypes.data_as(C.POINTER(C.c_int32)),
+                                       logp.ctypes.data_as(C.POINTER(C.c_float)))
             out = {"top_token": top[:D], "top_logprob": logp[:D]}
         else:
-            _check(lib.asr_step(self.h, C.byref(sin), C.byref(sout)))
-        return {"slot_of": slot_of[:P].copy(), "argmax": am[:D].copy(),
-                "done": done[:D].astype(bool), "logits": logits, **out}
+            status = lib.asr_step(self.h, C.byref(sin), C.byref(sout))
+        results = {"slot_of": slot_of[:P].copy(), "argmax": am[:D].copy(),
+                   "done": done[:D].astype(bool), "logits": logits, **out}
+        _check(status, results if D > 0 and (am[:D] != NOT_WRITTEN).all() else None)
+        return results
 
     # -- hypotheses and rules ---------------------------------------------------
     def hypotheses_size(self, max_bias=0, n_masks=0) -> int:
@@ -603,19 +614,22 @@ class Context:
         tok = np.zeros(cap, np.int32)
         p64 = lambda a: a.ctypes.data_as(C.POINTER(C.c_int64))  # noqa: E731
         p32 = lambda a: a.ctypes.data_as(C.POINTER(C.c_int32))  # noqa: E731
-        out = ServeOut(cap, 0, p64(bufs["preempted"]), 0, p64(bufs["admitted"]), p32(slot), 0,
+        out = ServeOut(cap, NOT_WRITTEN, p64(bufs["preempted"]), 0, p64(bufs["admitted"]), p32(slot), 0,
                        p64(bufs["decoded"]), p32(tok), 0, p64(bufs["finished"]), 0)
-        _check(fn(self.h, now_us, C.byref(out)))
-        return {"policy": out.policy,
-                "preempted": bufs["preempted"][:out.n_preempted].tolist(),
-                "admitted": bufs["admitted"][:out.n_admitted].tolist(),
-                "admitted_slot": slot[:out.n_admitted].tolist(),
-                "decoded": bufs["decoded"][:out.n_decoded].tolist(),
-                "token": tok[:out.n_decoded].tolist(),
-                "finished": bufs["finished"][:out.n_finished].tolist()}
+        status = fn(self.h, now_us, C.byref(out))
+        results = {"policy": out.policy,
+                   "preempted": bufs["preempted"][:out.n_preempted].tolist(),
+                   "admitted": bufs["admitted"][:out.n_admitted].tolist(),
+                   "admitted_slot": slot[:out.n_admitted].tolist(),
+                   "decoded": bufs["decoded"][:out.n_decoded].tolist(),
+                   "token": tok[:out.n_decoded].tolist(),
+                   "finished": bufs["finished"][:out.n_finished].tolist()}
+        _check(status, results if out.policy != NOT_WRITTEN else None)
+        return results
 
     def serve_step(self, now_us):
-        """One continuous-batching step on the GPU (see asr_serve_step)."""
+        """One continuous-batching step on the GPU (see asr_serve_step).  Where a request ended with
+        a NaN logit, the AsrError's `results` are what this returns otherwise."""
         return self._serve(lib.asr_serve_step, now_us)
 
     def serve_plan(self, now_us):

@@ -39,3 +39,40 @@ def test_served_requests_end_where_their_rules_allow_nothing(overlap):
         else:
             assert sorted(tokens) == [5, 5, 700, 700, 2110, 2110]
     assert all(not ctx.slot_info(s)["occupied"] for s in range(3))
+
+
+@pytest.mark.parametrize("k", [0, 4])
+def test_a_search_goes_on_beside_a_dead_end(k):
+    """Of three hypotheses one comes to a mask that allows nothing: the error holds the others' results, and
+    they are those of a step without the dead one."""
+    from paper_2603_11273_amd import asr
+    shape, seed = synth.reduced_shape(synth.SHAPES["base"], 0, 2, vocab=V, dtype="bf16"), 20261202
+    got = []
+    for dead in (False, True):
+        ctx = make_context(shape, seed, max_slots=4, max_prefill=1, max_decode=4)
+        ctx.bind_hypotheses(n_masks=2)
+        ctx.set_masks(1, np.ones((1, V), bool))      # (row 0 stays as bound: nothing)
+        ctx.debug_set_encoder_out([0], [-1], [40], synth.encoder_output(seed, 0, shape.d_model).numpy()[None])
+        ctx.step(slots=[0], tokens=[3])
+        for s in (1, 2):
+            ctx.fork_slot(0, s)
+            ctx.set_slot_rules(s, repetition=1.2, mask=1)
+        ctx.set_slot_rules(0, presence=0.5)
+        ctx.set_slot_mask(1, 0 if dead else 1)
+        rows = []
+        for t in (5, 6):
+            if dead:
+                with pytest.raises(asr.AsrError) as e:
+                    ctx.step(slots=[0, 1, 2], tokens=[t, t + 1, t + 2], want_logits=True, topk=k)
+                out = e.value.results
+                assert e.value.status == asr.ASR_EDEVICE and out["argmax"][1] == -1
+                if k:
+                    assert (out["top_token"][1] == -1).all() and (out["top_logprob"][1] == -np.inf).all()
+            else:
+                out = ctx.step(slots=[0, 1, 2], tokens=[t, t + 1, t + 2], want_logits=True, topk=k)
+            rows.append([out[n][i] for n in ("argmax", "logits") + (("top_token", "top_logprob") if k else ())
+                         for i in (0, 2)] + [out["logits"][1]])
+            assert ctx.slot_info(1)["position"] == t - 3
+        got.append(rows)
+    for a, b in zip(*got):
+        assert all(np.array_equal(x, y) for x, y in zip(a, b))
