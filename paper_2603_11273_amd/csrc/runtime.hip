@@ -1629,6 +1629,19 @@ asr_status run_decode(asr_ctx* c, int D, const int32_t* slots, const int32_t* to
   const hipError_t synced = hipStreamSynchronize(c->stream);
   if (st != ASR_OK) return st;
   HIPCHK(synced);
+  // A row that goes by the rules' results only because another row has rules: what
+  // they cannot say (the best of infinite logits) its own argmax does.
+  auto by_argmax = [&](int i) {
+    if (sh.k == 0) return true;
+    const size_t at = (size_t)i * sh.k;
+    return k == 0 && !c->rules[slots[io.order[i]]].active && (io.best[at] < 0 || std::isnan(io.logprob[at]));
+  };
+  for (int i = 0; i < D && sh.k > 0; ++i) {
+    if (!by_argmax(i)) continue;
+    HIPCHK(hipMemcpyAsync(am.data(), c->at(c->L.d_argmax), D * 4, hipMemcpyDeviceToHost, c->stream));
+    HIPCHK(hipStreamSynchronize(c->stream));
+    break;
+  }
   const char* bad = nullptr;
   auto fault = [&](int row, RowFault f, const char* what) {
     bad = what;
@@ -1636,7 +1649,7 @@ asr_status run_decode(asr_ctx* c, int D, const int32_t* slots, const int32_t* to
   };
   for (int i = 0; i < D; ++i) {
     const int row = io.order[i];
-    if (sh.k == 0) {
+    if (by_argmax(i)) {
       if (am[i] < 0) fault(row, RowFault::NOT_FINITE, "NaN logit");
       argmax[row] = am[i] < 0 ? -1 - am[i] : am[i];
       continue;

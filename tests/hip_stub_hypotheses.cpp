@@ -154,6 +154,55 @@ int serve() {
   return 0;
 }
 
+// A row without rules in a step with one that has some: infinite logits, all of them -infinite
+// and NaN ones give what they give without the other row.
+int beside() {
+  Context x;
+  if (x.make(0, 3, 40, 0, 1)) return 1;
+  int32_t slots[3] = {0, 1, 2}, left[3] = {40, 40, 40}, tokens[3] = {1, 2, 3}, argmax[3], done[3], best[6];
+  int64_t ids[3] = {-1, -1, -1};
+  float logprob[6];
+  std::vector<float> E(1500 * 64);
+  for (int i = 0; i < 3; ++i) OK(asr_debug_set_encoder_out(x.c, slots + i, ids + i, left + i, 1, E.data(), 0));
+  asr_slot_rules rules{1.5f, 0.f, 0.f, 1.f, 0, -1, 0, nullptr, nullptr};
+  OK(asr_set_slot_rules(x.c, 1, &rules));
+  asr_step_in in{0, nullptr, 3, slots, tokens, nullptr};
+  asr_step_out out{nullptr, argmax, done};
+  int32_t token[3] = {5, 6, -1}, own[3] = {9, 30, 0};
+  float lp[3] = {NAN, -0.5f, -INFINITY};
+  int asked = 0;
+  results = [&](void* src, size_t n, int) {
+    const void* from[3] = {token, lp, own};
+    if (asked < 3 && n == 12) memcpy(src, from[asked], n);
+    ++asked;
+  };
+  auto step = [&] { return asked = 0, asr_step(x.c, &in, &out); };
+  OK(step());
+  CHECK(asked == 3 && argmax[0] == 9 && argmax[1] == 6 && argmax[2] == 0);
+  own[2] = -1 - 17;                                    // a NaN at 17
+  CHECK(step() == ASR_EDEVICE && strstr(asr_last_error(), "NaN"));
+  CHECK(argmax[0] == 9 && argmax[1] == 6 && argmax[2] == 17);
+  token[2] = 8;
+  lp[0] = lp[2] = -1.f;
+  OK(step());
+  CHECK(asked == 2 && argmax[0] == 5 && argmax[1] == 6 && argmax[2] == 8);
+  lp[1] = NAN;                                         // of the row with rules
+  CHECK(step() == ASR_EDEVICE && asked == 2);
+  lp[1] = -1.f;
+  lp[0] = NAN;                                         // asked for candidates, a row's are what they are
+  results = [&](void* src, size_t n, int number) {
+    for (size_t i = 0; i < n / 4; ++i)
+      if (number == 0)
+        ((int32_t*)src)[i] = 5 + (int)i;
+      else
+        ((float*)src)[i] = i == 0 ? NAN : -1.f;
+  };
+  CHECK(asr_step_topk(x.c, &in, &out, 2, best, logprob) == ASR_EDEVICE);
+  CHECK(argmax[0] == 5 && argmax[2] == 9 && best[5] == 10);
+  printf("beside: ok\n");
+  return 0;
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -161,7 +210,9 @@ int main(int argc, char** argv) {
     const std::string name = argv[i];
     results = nullptr;
     copies = 0;
-    const int bad = name == "serve" ? serve() : (printf("no scenario %s\n", argv[i]), 1);
+    const int bad = name == "serve"    ? serve()
+                    : name == "beside" ? beside()
+                                       : (printf("no scenario %s\n", argv[i]), 1);
     if (bad) return bad;
   }
   return 0;

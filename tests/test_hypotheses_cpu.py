@@ -37,6 +37,11 @@ def test_a_row_without_a_next_token_ends_its_request_alone(stub):
     stub("serve")
 
 
+def test_a_row_without_rules_beside_one_with_rules(stub):
+    """Infinite and NaN logits of a row without rules are answered as they are without the other row."""
+    stub("beside")
+
+
 class FakeLibrary:
     """The entry points of a step: `status`, and what they write where they get so far."""
 
