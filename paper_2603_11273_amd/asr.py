@@ -247,7 +247,9 @@ class _Operator:
     """What the plans of the stateless operators share: the tensors they keep, their scratch and
     the call.  Tensors are taken as they lie (no copies) and must stay where they are; what is in
     them may change between calls.  A workspace given to a plan starts as zeros; plans may share
-    one if their calls never overlap."""
+    one if their calls never overlap.  A plan's own may be used on any stream as soon as the plan is
+    made (under capture: in that graph alone), and stays until the calls are done; calls held by a
+    captured graph need the plan kept."""
 
     def __init__(self, device, workspace, size, run, args):
         import torch
@@ -263,8 +265,14 @@ class _Operator:
         _check(size(self._ref, C.byref(n)))
         self.workspace_bytes = n.value
         self._ws = workspace
+        self._streams = None                   # a given block: its streams are the program's matter
         if workspace is None:
             self._ws = torch.zeros(max(n.value, 1), dtype=torch.uint8, device=device)
+            # calls may come on any stream, and count on the zeros
+            home = torch.cuda.current_stream(device)
+            if not torch.cuda.is_current_stream_capturing():
+                home.synchronize()
+            self._streams = {home.cuda_stream}
         self._ws_ptr, self._ws_bytes = self._ws.data_ptr(), self._ws.numel()
 
     def _need(self, t, name, dtype, shape, device, ld=False):
@@ -284,12 +292,15 @@ class _Operator:
 
     def _launch(self, stream):
         import torch
+        st = self._raw_stream(self._dev.index) if stream is None else stream.cuda_stream
+        if self._streams is not None and st not in self._streams:
+            # the plan's own block is not to be handed out again before this stream is done with it
+            self._ws.record_stream(torch.cuda.current_stream(self._dev) if stream is None else stream)
+            self._streams.add(st)
         if torch.cuda.current_device() == self._dev.index:
-            st = self._raw_stream(self._dev.index) if stream is None else stream.cuda_stream
             _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st))
             return
         with torch.cuda.device(self._dev):
-            st = self._raw_stream(self._dev.index) if stream is None else stream.cuda_stream
             _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st))
 
 

@@ -1,0 +1,93 @@
+"""The plans of the stateless operators (asr.SharedAttention, asr.LogitRules)
+as host code: when their scratch is ready, which streams it is tied to, what a
+call hands over.  Streams, tensors and the library's call are stand-ins."""
+from types import SimpleNamespace
+
+import pytest
+
+asr = pytest.importorskip("paper_2603_11273_amd.asr")
+torch = pytest.importorskip("torch")
+
+
+class Stream:
+    def __init__(self, handle, log):
+        self.cuda_stream, self.log = handle, log
+
+    def synchronize(self):
+        self.log.append(("wait", self.cuda_stream))
+
+
+class Tensor:
+    """As much of a device tensor as a plan looks at."""
+    made = 0
+
+    def __init__(self, shape, dtype, log=None):
+        Tensor.made += 4096
+        self.at, self.shape, self.dtype, self.log = Tensor.made, tuple(shape), dtype, log
+        self.device = torch.device("cuda", 0)
+
+    def data_ptr(self):
+        return self.at
+
+    def numel(self):
+        return 1 << 20
+
+    def stride(self, dim):
+        return 1 if dim in (-1, len(self.shape) - 1) else self.shape[-1]
+
+    def is_contiguous(self):
+        return True
+
+    def record_stream(self, stream):
+        self.log.append(("keep for", stream.cuda_stream))
+
+
+@pytest.fixture
+def gpu(monkeypatch):
+    """A device whose current stream is `current[0]`, and the order of what happens on it."""
+    log = []
+    state = SimpleNamespace(log=log, current=[Stream(11, log)], capturing=False)
+
+    def zeros(n, dtype, device):
+        log.append(("fill", state.current[0].cuda_stream))
+        return Tensor((n,), dtype, log)
+    monkeypatch.setattr(torch, "zeros", zeros)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: state.current[0])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: state.capturing)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: state.current[0].cuda_stream, raising=False)
+    return state
+
+
+def rules(gpu, **kw):
+    plan = asr.LogitRules(2, 100, torch.float32, k=1, device="cuda:0", **kw)
+    plan._run = lambda ref, ws, n, stream: gpu.log.append(("run", stream)) or asr.ASR_OK
+    return plan, dict(logits=Tensor((2, 100), torch.float32), token=Tensor((2, 1), torch.int32),
+                      logprob=Tensor((2, 1), torch.float32))
+
+
+def test_scratch_is_zeros_before_a_call_on_any_stream(gpu):
+    plan, args = rules(gpu)
+    assert gpu.log == [("fill", 11), ("wait", 11)]
+    del gpu.log[:]
+    other = Stream(22, gpu.log)
+    plan(**args, stream=other)
+    plan(**args)
+    plan(**args, stream=other)
+    gpu.current[0] = Stream(33, gpu.log)
+    plan(**args)
+    plan(**args)
+    assert gpu.log == [("keep for", 22), ("run", 22), ("run", 11), ("run", 22), ("keep for", 33), ("run", 33), ("run", 33)]
+
+
+def test_scratch_of_a_plan_made_under_capture_or_given(gpu):
+    gpu.capturing = True                       # (a capture may not be waited for, and orders its own work)
+    plan, args = rules(gpu)
+    plan(**args)
+    assert gpu.log == [("fill", 11), ("run", 11)]
+    gpu.capturing = False
+    del gpu.log[:]
+    block = Tensor((1 << 20,), torch.uint8, gpu.log)
+    plan, args = rules(gpu, workspace=block)
+    plan(**args, stream=Stream(44, gpu.log))
+    assert gpu.log == [("run", 44)]            # the program's own block
