@@ -327,11 +327,14 @@ asr_status asr_set_encoder_streams(asr_ctx* ctx, int32_t n);
 
 /* Decode steps replayed from HIP graphs (on = 1, the default) or launched
  * kernel by kernel (on = 0).  With graphs, the decode kernels of each shape
- * (row count, logits wanted) are captured once -- at that shape's second
- * step, on a stream the context owns -- and every later step of the shape
- * replays them on the bound stream after uploading its rows.  Results are
- * the same either way; steps with per-launch timing selected always launch
- * directly. */
+ * (row count, logits wanted; with hypotheses or rules also the families, their
+ * rows and largest size, and the candidates) are captured once -- at that shape's
+ * second step, on a stream the context owns -- and every later step of the shape
+ * replays them on the bound stream after uploading its rows.  Of the shapes with
+ * hypotheses or rules 128 graphs are kept; a new one takes the place of one that
+ * no step of the last 512 used, and while there is none its steps are launched
+ * directly.  Results are the same either way; steps with per-launch timing
+ * selected always launch directly. */
 asr_status asr_set_decode_graphs(asr_ctx* ctx, int32_t on);
 
 /* classes is a bit mask over the asr_kernel_class values: bit k selects class

@@ -8,6 +8,7 @@
 #include <mutex>
 #include <string>
 #include <unordered_map>
+#include <unordered_set>
 #include <vector>
 
 #include "../../include/asr.h"
@@ -104,6 +105,19 @@ struct StepShape {
   }
 };
 
+// A captured step, and the context's step that replayed it last.
+struct StepGraph {
+  hipGraphExec_t exec = nullptr;
+  bool plain = false;      // neither families nor rules
+  int64_t used = 0;
+};
+// Plain shapes are 2 * 128 at most and all kept.  Of the others, which families of
+// any sizes make by the thousand, so many are; one gives way to a new shape when no
+// step of the last kGraphIdle was its own (a walk over more shapes than are kept
+// would capture at every step otherwise), and until then the new one is launched
+// kernel by kernel.  So many shapes are remembered as seen once.
+constexpr int kOtherGraphs = 128, kGraphIdle = 4 * kOtherGraphs, kShapesSeen = 1024;
+
 struct EncLayer {
   size_t ln1_g, ln1_b, qkv_w, qkv_b, o_w, o_b, ln2_g, ln2_b, fc1_w, fc1_b, fc2_w, fc2_b;
 };
@@ -182,8 +196,9 @@ struct asr_ctx {
   // captured on a private stream at the second step of that shape
   bool decode_graphs = true;
   hipStream_t cap_stream = nullptr;
-  std::unordered_map<int64_t, hipGraphExec_t> dgraph;
-  std::unordered_map<int64_t, int32_t> dshape_seen;
+  std::unordered_map<int64_t, StepGraph> dgraph;
+  std::unordered_set<int64_t> dshape_seen;
+  int64_t dsteps = 0;
   Layout L;
   bool bound = false, loaded = false;
   char* base = nullptr;
@@ -1132,6 +1147,29 @@ void leave_family(asr_ctx* c, int slot) {
 
 bool in_family(const asr_ctx* c, int slot) { return c->family[slot].root >= 0 || c->family[slot].kids > 0; }
 
+void drop_graphs(asr_ctx* c) {
+  for (auto& kv : c->dgraph) (void)hipGraphExecDestroy(kv.second.exec);
+  c->dgraph.clear();
+  c->dshape_seen.clear();
+}
+
+// Room for the graph of a shape that is not plain, see kOtherGraphs.  (Steps are
+// waited for, so none is in flight here.)
+bool room_for_graph(asr_ctx* c) {
+  int others = 0;
+  auto oldest = c->dgraph.end();
+  for (auto it = c->dgraph.begin(); it != c->dgraph.end(); ++it) {
+    if (it->second.plain) continue;
+    ++others;
+    if (oldest == c->dgraph.end() || it->second.used < oldest->second.used) oldest = it;
+  }
+  if (others < kOtherGraphs) return true;
+  if (c->dsteps - oldest->second.used < kGraphIdle) return false;
+  (void)hipGraphExecDestroy(oldest->second.exec);
+  c->dgraph.erase(oldest);
+  return true;
+}
+
 // A slot that is filled anew starts with the default rules.
 asr_status start_rules(asr_ctx* c, int slot) {
   c->rules[slot] = c->default_rules;
@@ -1211,7 +1249,7 @@ asr_status asr_destroy(asr_ctx* c) {
       if (c->estream[i]) (void)hipStreamDestroy(c->estream[i]);
     }
     if (c->ev_efork) (void)hipEventDestroy(c->ev_efork);
-    for (auto& kv : c->dgraph) (void)hipGraphExecDestroy(kv.second);
+    drop_graphs(c);
     if (c->cap_stream) (void)hipStreamDestroy(c->cap_stream);
   }
   delete c;
@@ -1230,9 +1268,7 @@ asr_status asr_bind(asr_ctx* c, void* dev_block, size_t bytes, void* stream) {
   if (!dev_block || ((uintptr_t)dev_block & 255)) return fail(ASR_EINVAL, "block must be 256-byte aligned");
   if (bytes < c->L.total) return fail(ASR_ENOMEM, "bound block smaller than asr_workspace_size");
   HIPCHK(hipSetDevice(c->device));
-  for (auto& kv : c->dgraph) (void)hipGraphExecDestroy(kv.second);
-  c->dgraph.clear();
-  c->dshape_seen.clear();
+  drop_graphs(c);
   c->hyp = Hypotheses();
   c->family.assign(c->slots.size(), Family());
   c->rules.assign(c->slots.size(), Rules());
@@ -1459,7 +1495,8 @@ asr_status run_prefill(asr_ctx* c, const std::vector<const Request*>& reqs,
 // and tokens are read from device memory -- so one graph serves every step of
 // a shape.  A shape's first step runs directly (it also performs the
 // kernels' one-time attribute set-up); the second is captured on a private
-// stream and replayed from then on.  Per-launch timing always runs directly.
+// stream and replayed from then on (while there is room: kOtherGraphs).  Per-launch
+// timing always runs directly.
 asr_status decode_launch(asr_ctx* c, const StepShape& sh, const std::vector<int32_t>& pos, bool want_logits) {
   auto direct = [&]() {
     return c->bf16() ? decode_rows<bf16_t>(c, sh, pos, want_logits)
@@ -1469,9 +1506,16 @@ asr_status decode_launch(asr_ctx* c, const StepShape& sh, const std::vector<int3
   const bool per_launch_timing = (c->timing & ~((1 << ASR_K_PREFILL) | (1 << ASR_K_DECODE) |
                                                 (1 << ASR_K_ENCODE))) != 0;
   if (!c->decode_graphs || per_launch_timing) return direct();
+  ++c->dsteps;
   auto it = c->dgraph.find(key);
   if (it == c->dgraph.end()) {
-    if (c->dshape_seen[key]++ == 0) return direct();
+    const bool plain = sh.shared == 0 && sh.k == 0;
+    if (!c->dshape_seen.count(key)) {
+      if (c->dshape_seen.size() >= kShapesSeen) c->dshape_seen.clear();
+      c->dshape_seen.insert(key);
+      return direct();
+    }
+    if (!plain && !room_for_graph(c)) return direct();
     if (!c->cap_stream) HIPCHK(hipStreamCreateWithFlags(&c->cap_stream, hipStreamNonBlocking));
     hipStream_t bound = c->stream;
     c->stream = c->cap_stream;
@@ -1489,9 +1533,10 @@ asr_status decode_launch(asr_ctx* c, const StepShape& sh, const std::vector<int3
     const hipError_t e2 = hipGraphInstantiate(&ex, g, nullptr, nullptr, 0);
     (void)hipGraphDestroy(g);
     if (e2 != hipSuccess) return fail(ASR_EDEVICE, std::string("hipGraphInstantiate: ") + hipGetErrorString(e2));
-    it = c->dgraph.emplace(key, ex).first;
+    it = c->dgraph.emplace(key, StepGraph{ex, plain, 0}).first;
   }
-  HIPCHK(hipGraphLaunch(it->second, c->stream));
+  it->second.used = c->dsteps;
+  HIPCHK(hipGraphLaunch(it->second.exec, c->stream));
   return ASR_OK;
 }
 
@@ -1788,9 +1833,7 @@ asr_status asr_bind_hypotheses(asr_ctx* c, int32_t max_bias, int32_t n_masks, vo
   HIPCHK(hipSetDevice(c->device));
   // (steps captured without the block, or with another, are of no use)
   HIPCHK(hipStreamSynchronize(c->stream));
-  for (auto& kv : c->dgraph) (void)hipGraphExecDestroy(kv.second);
-  c->dgraph.clear();
-  c->dshape_seen.clear();
+  drop_graphs(c);
   c->hyp = plan_hypotheses(c, max_bias, n_masks);
   c->hyp.base = (char*)dev_block;
   c->rules.assign(c->slots.size(), Rules());

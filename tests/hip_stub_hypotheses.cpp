@@ -17,6 +17,7 @@ namespace {
 std::function<void(void* src, size_t n, int number)> results;
 int copies = 0;
 int graphs = 0;          // that are kept
+int replays = 0;
 constexpr int kToHost = 2;
 }  // namespace
 
@@ -48,7 +49,7 @@ int hipStreamEndCapture(void*, void** g) { *g = malloc(1); return 0; }
 int hipGraphDestroy(void* g) { free(g); return 0; }
 int hipGraphInstantiate(void** ex, void*, void*, char*, size_t) { *ex = malloc(1); ++graphs; return 0; }
 int hipGraphExecDestroy(void* ex) { free(ex); --graphs; return 0; }
-int hipGraphLaunch(void*, void*) { return 0; }
+int hipGraphLaunch(void*, void*) { ++replays; return 0; }
 }
 
 #define OK(x)                                                                       \
@@ -203,6 +204,64 @@ int beside() {
   return 0;
 }
 
+// Steps of 256 shapes with rules, of 16 without, and a change of the shapes in use: the graphs
+// kept are bounded, every shape without rules keeps its own, and new shapes come to theirs.
+int shapes() {
+  Context x;
+  if (x.make(0, 16, 40, 0, 1)) return 1;
+  const int most = 128;
+  int32_t slots[16], tokens[16] = {}, argmax[16], done[16], best[256], left = 448;
+  int64_t id = -1;
+  float logprob[256];
+  std::vector<float> E(1500 * 64);
+  for (int i = 0; i < 16; ++i) slots[i] = i;
+  auto renew = [&](int i) { return asr_debug_set_encoder_out(x.c, slots + i, &id, &left, 1, E.data(), 0); };
+  int steps = 0;
+  auto step = [&](int rows, int k) -> asr_status {
+    if (steps++ % 440 == 0)                            // positions end at 448
+      for (int i = 0; i < 16; ++i)
+        if (asr_status st = renew(i)) return st;
+    asr_step_in in{0, nullptr, rows, slots, tokens, nullptr};
+    asr_step_out out{nullptr, argmax, done};
+    return k ? asr_step_topk(x.c, &in, &out, k, best, logprob) : asr_step(x.c, &in, &out);
+  };
+  for (int round = 0; round < 3; ++round)
+    for (int rows = 1; rows <= 16; ++rows)
+      for (int k = 1; k <= 16; ++k) {
+        OK(step(rows, k));
+        CHECK(graphs <= most);
+      }
+  CHECK(graphs == most && replays == 2 * most);        // the first to come keep theirs
+  for (int round = 0; round < 3; ++round)
+    for (int rows = 1; rows <= 16; ++rows) OK(step(rows, 0));
+  CHECK(graphs == most + 16);
+  int before = replays;
+  OK(step(16, 16));
+  CHECK(replays == before);                            // no room yet
+  for (int i = 0; i < 600; ++i) OK(step(1 + i % 16, 0));
+  before = replays;
+  for (int i = 0; i < 3; ++i) OK(step(16, 16));
+  CHECK(replays == before + 3 && graphs == most + 16);
+  for (int i = 0; i < 16; ++i) OK(renew(i));
+  steps = 1;
+  for (int round = 0; round < 3; ++round)              // families: forks one after the other
+    for (int rows = 2; rows <= 8; ++rows) {
+      for (int i = 1; i < rows; ++i) {
+        OK(asr_release_slot(x.c, i));
+        OK(asr_fork_slot(x.c, 0, i));
+      }
+      for (int k = 0; k <= 16; ++k) OK(step(rows, k));
+      for (int i = 1; i < rows; ++i) OK(asr_release_slot(x.c, i));
+      for (int i = 1; i < rows; ++i) OK(renew(i));
+      CHECK(graphs <= most + 16);
+    }
+  before = replays;
+  for (int rows = 1; rows <= 16; ++rows) OK(step(rows, 0));
+  CHECK(replays == before + 16);
+  printf("shapes: ok\n");
+  return 0;
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -212,6 +271,7 @@ int main(int argc, char** argv) {
     copies = 0;
     const int bad = name == "serve"    ? serve()
                     : name == "beside" ? beside()
+                    : name == "shapes" ? shapes()
                                        : (printf("no scenario %s\n", argv[i]), 1);
     if (bad) return bad;
   }

@@ -42,6 +42,11 @@ def test_a_row_without_rules_beside_one_with_rules(stub):
     stub("beside")
 
 
+def test_graphs_of_many_shapes_are_bounded(stub):
+    """A search goes through more shapes of a step than graphs are kept of."""
+    stub("shapes")
+
+
 class FakeLibrary:
     """The entry points of a step: `status`, and what they write where they get so far."""
 
