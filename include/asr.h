@@ -564,7 +564,7 @@ asr_status asr_attend_shared(const asr_attention* a, void* ws, size_t ws_bytes, 
  * logprob = z - L, L = log sum_v e^z in float32 (so off by half a step of L).  A
  * token with z = -inf is never given: where the others run out, token = -1 and
  * logprob = -inf (a row whose mask allows nothing has only these).
- *   vocab at most 1048576, rows at most 65535. */
+ *   vocab at most 1048576, rows at most 65535, history_ld and bias_ld at most 2^30. */
 typedef struct {
   int32_t dtype;       /* asr_dtype of the logits */
   int32_t rows, vocab, sets, masks, k;

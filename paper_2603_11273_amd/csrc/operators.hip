@@ -176,10 +176,12 @@ asr_status plan_rules(const asr_rules* r, RulesLaunch* s, size_t* bytes) {
   if (r->vocab < 1 || r->vocab > kRulesMaxVocab) return fail(ASR_EINVAL, "vocab out of [1, 1048576]");
   if (r->k < 0 || r->k > kRulesMaxK) return fail(ASR_EINVAL, "k out of [0, 16]");
   if (r->sets < 0 || r->masks < 0) return fail(ASR_EINVAL, "negative size");
-  if (r->history && (r->history_ld < 0 || r->history_ld > INT32_MAX || !r->history_len))
-    return fail(ASR_EINVAL, "history needs history_len and a row length");
-  if (r->bias_token && (r->bias_ld < 0 || r->bias_ld > INT32_MAX || !r->bias_value || !r->bias_len))
-    return fail(ASR_EINVAL, "bias_token needs bias_value, bias_len and a row length");
+  // (the kernels step past a list's end with 32 bits)
+  constexpr int64_t kMostEntries = 1 << 30;
+  if (r->history && (r->history_ld < 0 || r->history_ld > kMostEntries || !r->history_len))
+    return fail(ASR_EINVAL, "history needs history_len and a row length of at most 2^30");
+  if (r->bias_token && (r->bias_ld < 0 || r->bias_ld > kMostEntries || !r->bias_value || !r->bias_len))
+    return fail(ASR_EINVAL, "bias_token needs bias_value, bias_len and a row length of at most 2^30");
   if (r->mask && r->mask_ld < (r->vocab + 31) / 32) return fail(ASR_EINVAL, "mask_ld shorter than the vocabulary");
   *s = {r->logits, r->ld, r->rows, r->vocab, r->sets, r->set, r->history, r->history_ld, r->history_len, r->prompt_len,
         r->repetition, r->frequency, r->presence, r->bias_token, r->bias_value, r->bias_ld, r->bias_len, r->mask,

@@ -118,3 +118,13 @@ def test_plans_refuse_host_memory():
         keys = zeros(1, 2, 8, 64)
         asr.SharedAttention(keys, keys, n_head=2, rows=1, groups=1, max_group=1,
                             group_start=zeros(2, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("name", ["history_ld", "bias_ld"])
+def test_lists_that_32_bits_would_not_step_through(name):
+    """The kernels read a list 8192 entries at a time with 32-bit places; past 2^31 - 8192 entries the
+    last of them would wrap round to places before the list."""
+    assert size(asr.lib.asr_logit_rules_size, rules(**{name: 1 << 30}))[0] == asr.ASR_OK
+    for n in ((1 << 30) + 1, (1 << 31) - 1):
+        assert size(asr.lib.asr_logit_rules_size, rules(**{name: n}))[0] == asr.ASR_EINVAL
+        assert asr.lib.asr_logit_rules(C.byref(rules(**{name: n})), A, 1 << 30, None) == asr.ASR_EINVAL
