@@ -65,11 +65,13 @@ struct Logits<bf16_t> {
 };
 
 // x / d of N values, correctly rounded, one divisor for all.  With r the rounded
-// 1 / d, q = x r is off by 2 steps at most, one correction q += r (x - q d) makes
+// 1 / d, q = x r is off by 2 steps at most, one correction q -= r (q d - x) makes
 // it one of the two floats around x / d, and a second one, by Markstein's theorem,
 // the nearest: 5 instructions where a division by itself takes 11.  The theorem
-// wants x - q d exact, hence no quotient or residual near the ends of the range;
-// a wave with such values (infinities among them) divides.
+// wants q d - x exact, hence no quotient or residual near the ends of the range;
+// a wave with such values (infinities among them) divides.  A residual of 0 is +0
+// for x = 0 and x = -0, and q - r 0 is q: a quotient keeps the sign of its zero
+// (with the residual x - q d it would not).
 template <int N>
 __device__ __forceinline__ void divide(const float* x, float d, float r, float* y) {
   float hi = 0.f;
@@ -87,8 +89,8 @@ __device__ __forceinline__ void divide(const float* x, float d, float r, float* 
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     float q = x[i] * r;
-    q = fmaf(fmaf(-q, d, x[i]), r, q);
-    y[i] = fmaf(fmaf(-q, d, x[i]), r, q);
+    q = fmaf(-fmaf(q, d, -x[i]), r, q);
+    y[i] = fmaf(-fmaf(q, d, -x[i]), r, q);
   }
 }
 
@@ -249,6 +251,7 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
   const bool ruled = set >= 0 && set < a.sets;
   if (!ruled) set = 0;
   const bool some = ruled && a.sets > 0;
+  const bool biased = some && a.bias_token;
   // ... and of its lists what fits, before their lengths are known (rows are as long as they say)
   const int32_t* hist = a.history + (int64_t)set * a.history_ld;
   int said[RU_FIRST] = {};
@@ -261,13 +264,13 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
   const float* bv = a.bias_value + (int64_t)set * a.bias_ld;
   int bias_tok = -1;
   float bias_val = 0.f;
-  if (some && a.bias_token && lane < a.bias_ld) {
+  if (biased && lane < a.bias_ld) {
     bias_tok = bt[lane];
     bias_val = bv[lane];
   }
   const int hist_len = some && a.history ? a.history_len[set] : 0;
   const int prompt = some && a.history && a.prompt_len ? a.prompt_len[set] : 0;
-  const int bias_len = some && a.bias_token ? a.bias_len[set] : 0;
+  const int bias_len = biased ? a.bias_len[set] : 0;
   const int mask_row = some && a.mask ? (a.mask_of ? a.mask_of[set] : set) : -1;
   const float rep = some && a.repetition ? a.repetition[set] : 1.f;
   const float freq = some && a.frequency ? a.frequency[set] : 0.f;
@@ -310,10 +313,11 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
       }
     }
   }
-  if (bias_n > 0) {
+  if (biased) {
     // the biases in the order of their list, so that a token given twice has one
     // sum: each wave adds up those of its own tokens, in their places of the table
-    // (which no other wave reads any more)
+    // (which no other wave reads any more).  A token without biases has the sum 0,
+    // which makes a 0 of a -0
     float* sums = (float*)own;
     const auto place = [&](int i) { return i * 4 / VEC * RU_NT * VEC + tid * VEC + i * 4 % VEC; };
     bool some_hit = false;
@@ -335,7 +339,7 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
         if (lane == 0) sums[ul] += vl;
       }
     };
-    add(lane < bias_n ? bias_tok : -1, bias_val);
+    if (bias_n > 0) add(lane < bias_n ? bias_tok : -1, bias_val);
     for (int j0 = 64; j0 < bias_n; j0 += 256) {
       int tok[4];
       float val[4];
@@ -358,6 +362,9 @@ __device__ __forceinline__ bool rules_block(const RulesLaunch& a, int chunks) {
         z[4 * i + 2] = z[4 * i + 2] + x.z;
         z[4 * i + 3] = z[4 * i + 3] + x.w;
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < RU_E; ++i) z[i] = z[i] + 0.f;
     }
   }
   if (temp > 0.f && temp != 1.f) divide<RU_E>(z, temp, 1.f / temp, z);
