@@ -561,7 +561,7 @@ asr_status asr_attend_shared(const asr_attention* a, void* ws, size_t ws_bytes, 
  *   out (may be NULL): z, float32; it may be the logits themselves (float32,
  * out_ld = ld).  k in [0, 16] best tokens per row, larger z first, the lower
  * token of equal ones, a NaN before everything: token and logprob [rows][k],
- * logprob = z - L, L = log sum_v e^z in float32 (so off by half a step of L).  A
+ * logprob = (z - M) - log sum_v e^{z - M}, M the largest z, in float32.  A
  * token with z = -inf is never given: where the others run out, token = -1 and
  * logprob = -inf (a row whose mask allows nothing has only these).
  *   vocab at most 1048576, rows at most 65535, history_ld and bias_ld at most 2^30. */

@@ -548,17 +548,15 @@ __device__ __forceinline__ void join_row(const RulesLaunch& a, int chunks, int r
 #pragma unroll
   for (int i = 0; i < LISTS; ++i)
     S += m[i] == M ? s[i] : s[i] * __builtin_amdgcn_exp2f((m[i] - M) * 1.4426950408889634f);
-  // logprob = z - L with L = log sum_v e^z in float32, as the definition's steps
-  // round it; where a step of L is above 2^-12 (logits of the type's lowest value
-  // among others) (z - M) - log sum_v e^{z - M}, which L's size does not enter
-  const float log_sum = logf(wave_sum_lanes(S)), L = M + log_sum;
-  const bool near = fabsf(M) < 4096.f;
+  // logprob = (z - M) - log sum_v e^{z - M}: with M in it (z minus M + log sum) the
+  // result would be off by half a step of M, all there is of a near-certain token's
+  const float log_sum = logf(wave_sum_lanes(S));
   wave_lds_done();
   auto put = [&](int place, uint64_t x) {
     const uint32_t r = (uint32_t)(x >> 32);
     const float z = r == 0xffffffffu ? NAN : from_ordered_u32(r);
     a.token[(int64_t)row * a.k + place] = x ? (int)~(uint32_t)x : -1;
-    a.logprob[(int64_t)row * a.k + place] = x ? (near ? z - L : (z - M) - log_sum) : -INFINITY;
+    a.logprob[(int64_t)row * a.k + place] = x ? (z - M) - log_sum : -INFINITY;
   };
   uint64_t* cand = rules_lds + n;
   const uint32_t least = rank_floor(largest, a.k);
