@@ -448,7 +448,9 @@ asr_status asr_fork_slot(asr_ctx* ctx, int32_t src, int32_t dst);
  * the prompt (tokens behind a cache set by asr_debug_set_self_kv are unknown and
  * not counted).  repetition > 0 (1: off), frequency and presence 0: off,
  * temperature > 0, mask: a row of the mask table, -1: none; bias_token and
- * bias_value are host arrays of n_bias <= max_bias entries. */
+ * bias_value are host arrays of n_bias <= max_bias entries (values finite, or
+ * -INFINITY for a token that is never to come: +INFINITY would leave no
+ * probabilities). */
 typedef struct {
   float repetition, frequency, presence, temperature;
   int32_t n_prompt;

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <mutex>
@@ -1923,8 +1924,8 @@ asr_status asr_set_slot_rules(asr_ctx* c, int32_t slot, const asr_slot_rules* r)
     if (r->n_bias < 0 || r->n_bias > h.max_bias) return fail(ASR_EINVAL, "n_bias out of [0, max_bias]");
     if (r->n_bias > 0 && (!r->bias_token || !r->bias_value)) return fail(ASR_EINVAL, "NULL biases");
     for (int i = 0; i < r->n_bias; ++i)
-      if (r->bias_token[i] < 0 || r->bias_token[i] >= c->cfg.vocab || std::isnan(r->bias_value[i]))
-        return fail(ASR_EINVAL, "bias token out of the vocabulary, or its value a NaN");
+      if (r->bias_token[i] < 0 || r->bias_token[i] >= c->cfg.vocab || !(r->bias_value[i] <= FLT_MAX))
+        return fail(ASR_EINVAL, "bias token out of the vocabulary, or its value a NaN or +infinite");
     x = {true, r->repetition, r->frequency, r->presence, r->temperature, r->n_prompt, r->mask, r->n_bias};
     if (r->n_bias > 0) {
       HIPCHK(hipSetDevice(c->device));

@@ -262,6 +262,31 @@ int shapes() {
   return 0;
 }
 
+// Biases that would leave a row no probabilities are refused when they are given.
+int biases() {
+  Context x;
+  if (x.make(0, 2, 40, 3, 0)) return 1;
+  int32_t slot = 0, left = 9, token[3] = {1, 2, 1};
+  int64_t id = -1;
+  std::vector<float> E(1500 * 64);
+  OK(asr_debug_set_encoder_out(x.c, &slot, &id, &left, 1, E.data(), 0));
+  float value[3] = {-INFINITY, 3.4e38f, -3.4e38f};
+  asr_slot_rules rules{1.f, 0.f, 0.f, 1.f, 0, -1, 3, token, value};
+  for (int to = -1; to <= 0; ++to) {
+    OK(asr_set_slot_rules(x.c, to, &rules));
+    for (float bad : {INFINITY, NAN, -NAN}) {
+      value[1] = bad;
+      CHECK(asr_set_slot_rules(x.c, to, &rules) == ASR_EINVAL);
+      value[1] = 0.f;
+    }
+    token[2] = 40;
+    CHECK(asr_set_slot_rules(x.c, to, &rules) == ASR_EINVAL);
+    token[2] = 1;
+  }
+  printf("biases: ok\n");
+  return 0;
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -272,6 +297,7 @@ int main(int argc, char** argv) {
     const int bad = name == "serve"    ? serve()
                     : name == "beside" ? beside()
                     : name == "shapes" ? shapes()
+                    : name == "biases" ? biases()
                                        : (printf("no scenario %s\n", argv[i]), 1);
     if (bad) return bad;
   }

@@ -47,6 +47,10 @@ def test_graphs_of_many_shapes_are_bounded(stub):
     stub("shapes")
 
 
+def test_biases_without_probabilities_are_refused(stub):
+    stub("biases")
+
+
 class FakeLibrary:
     """The entry points of a step: `status`, and what they write where they get so far."""
 
