@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 
 import numpy as np
 
@@ -249,7 +250,10 @@ class _Operator:
     them may change between calls.  A workspace given to a plan starts as zeros; plans may share
     one if their calls never overlap.  A plan's own may be used on any stream as soon as the plan is
     made (under capture: in that graph alone), and stays until the calls are done; calls held by a
-    captured graph need the plan kept."""
+    captured graph need the plan kept.
+
+    A plan is for one call at a time.  Threads that call one take turns; calls on several streams,
+    which share its scratch, are ordered by the program, or made through a plan for each stream."""
 
     def __init__(self, device, workspace, size, run, args):
         import torch
@@ -257,6 +261,7 @@ class _Operator:
                                       or not workspace.is_contiguous()):
             raise TypeError(f"workspace must be contiguous bytes (torch.uint8) on {device}")
         self._dev, self._run, self._args = device, run, args
+        self._turn = threading.Lock()          # from a call's pointers in args to the library's return
         # the current stream's handle without a Stream object around it (1.8 us of a 10-us call)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -314,8 +319,8 @@ class SharedAttention(_Operator):
     prefix_slot / prefix_first / prefix_len [groups] and own_slot / own_first / own_len [rows] are
     read at every call.  max_prefix, max_own bound the lengths (default: the positions).
     plan(q, out): q float32 [rows][n_head * 64], out [rows][n_head * 64] in the cache's type, on
-    `stream` (default: torch's current stream).  Plans whose calls may overlap need a
-    workspace each (default: one of the plan's own)."""
+    `stream` (default: torch's current stream).  One call at a time: calls that may overlap on the
+    GPU need plans with a workspace each (default: one of the plan's own)."""
 
     def __init__(self, prefix_k=None, prefix_v=None, own_k=None, own_v=None, *, n_head, rows,
                  groups, max_group, group_start, row_of=None, prefix_slot=None, prefix_first=None,
@@ -359,10 +364,11 @@ class SharedAttention(_Operator):
     def __call__(self, q, out, stream=None):
         import torch
         a = self._args
-        a.q = self._need(q, "q", torch.float32, self._shape, self._dev, ld=True)
-        a.out = self._need(out, "out", self._dtype, self._shape, self._dev, ld=True)
-        a.q_ld, a.out_ld = self._ld(q), self._ld(out)
-        self._launch(stream)
+        with self._turn:
+            a.q = self._need(q, "q", torch.float32, self._shape, self._dev, ld=True)
+            a.out = self._need(out, "out", self._dtype, self._shape, self._dev, ld=True)
+            a.q_ld, a.out_ld = self._ld(q), self._ld(out)
+            self._launch(stream)
         return out
 
 
@@ -375,7 +381,8 @@ class LogitRules(_Operator):
     bias_len int32 [sets]; mask int32 [masks][words] (bit v % 32 of word v / 32 set = allowed) with
     mask_of int32 [sets].  plan(logits, out, token, logprob): logits [rows][vocab] of `dtype`
     (float32 or bfloat16), out float32 [rows][vocab] or None (may be the logits themselves), token
-    int32 and logprob float32 [rows][k]."""
+    int32 and logprob float32 [rows][k].  One call at a time: calls that may overlap on the GPU
+    need plans with a workspace each (default: one of the plan's own)."""
 
     def __init__(self, rows, vocab, dtype, *, k=0, sets=None, set=None, history=None,
                  history_len=None, prompt_len=None, repetition=None, frequency=None,
@@ -416,13 +423,14 @@ class LogitRules(_Operator):
     def __call__(self, logits, out=None, token=None, logprob=None, stream=None):
         import torch
         a = self._args
-        a.logits = self._need(logits, "logits", self._dtype, self._shape, self._dev, ld=True)
-        a.ld = self._ld(logits)
-        a.out = self._need(out, "out", torch.float32, self._shape, self._dev, ld=True)
-        a.out_ld = 0 if out is None else self._ld(out)
-        a.token = self._need(token, "token", torch.int32, self._best, self._dev)
-        a.logprob = self._need(logprob, "logprob", torch.float32, self._best, self._dev)
-        self._launch(stream)
+        with self._turn:
+            a.logits = self._need(logits, "logits", self._dtype, self._shape, self._dev, ld=True)
+            a.ld = self._ld(logits)
+            a.out = self._need(out, "out", torch.float32, self._shape, self._dev, ld=True)
+            a.out_ld = 0 if out is None else self._ld(out)
+            a.token = self._need(token, "token", torch.int32, self._best, self._dev)
+            a.logprob = self._need(logprob, "logprob", torch.float32, self._best, self._dev)
+            self._launch(stream)
 
 
 def model_cfg(shape, max_slots=8, max_prefill=1, max_decode=8, max_queue=4096) -> ModelCfg:

@@ -91,3 +91,44 @@ def test_scratch_of_a_plan_made_under_capture_or_given(gpu):
     plan, args = rules(gpu, workspace=block)
     plan(**args, stream=Stream(44, gpu.log))
     assert gpu.log == [("run", 44)]            # the program's own block
+
+
+def test_threads_take_turns(gpu):
+    """Two threads with one plan: the library sees each call's own tensors from its start to its end."""
+    import threading
+    import time
+    plan, _ = rules(gpu)
+    mine, wrong = threading.local(), []
+
+    def run(ref, ws, n, stream):
+        for _ in range(3):
+            if (ref._obj.logits, ref._obj.token) != mine.args:
+                wrong.append((ref._obj.logits, mine.args))
+            time.sleep(0.0005)                 # (the interpreter lock is free, as in a library call)
+        return asr.ASR_OK
+    plan._run = run
+
+    def caller():
+        for _ in range(20):
+            x, token, logprob = Tensor((2, 100), torch.float32), Tensor((2, 1), torch.int32), Tensor((2, 1), torch.float32)
+            mine.args = (x.at, token.at)
+            plan(x, token=token, logprob=logprob)
+    threads = [threading.Thread(target=caller) for _ in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
+def test_a_refused_call_leaves_the_plan_to_others(gpu):
+    plan, args = rules(gpu)
+    with pytest.raises(TypeError):
+        plan(Tensor((2, 99), torch.float32))
+    plan._run, run = lambda *a: asr.ASR_EINVAL, plan._run
+    with pytest.raises(asr.AsrError):
+        plan(**args)
+    plan._run = run
+    del gpu.log[:]
+    plan(**args)
+    assert gpu.log == [("run", 11)]
