@@ -340,12 +340,14 @@ class SharedAttention(_Operator):
                 raise TypeError(f"{name}: k and v must be [slots][kv heads][positions][64]")
             if any(t.device != dev or t.dtype != some.dtype for t in (k, v)):
                 raise TypeError(f"{name}: k and v must be {some.dtype} on {dev}")
-            if k.stride() != v.stride() or k.stride(3) != 1:
+            # (of a dimension of one element torch may say anything)
+            step, v_step = ([t.stride(i) if t.shape[i] > 1 else one for i, one in enumerate((0, 0, 64, 1))]
+                            for t in (k, v))
+            if step != v_step or step[3] != 1:
                 raise TypeError(f"{name}: k and v must have the same strides, dims contiguous")
             idx = [self._need(t, f"{name}_{n}", i32, (entries,), dev)
                    for t, n in ((slot, "slot"), (first, "first"), (length, "len"))]
-            return Keys(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
-                        k.shape[0], k.shape[2], *idx)
+            return Keys(k.data_ptr(), v.data_ptr(), *step[:3], k.shape[0], k.shape[2], *idx)
 
         self._keep = (prefix_k, prefix_v, own_k, own_v, group_start, row_of, prefix_slot,
                       prefix_first, prefix_len, own_slot, own_first, own_len)

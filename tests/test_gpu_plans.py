@@ -67,3 +67,25 @@ def test_scratch_outlives_a_dropped_plan():
     torch.cuda.synchronize()
     assert torch.equal(token.long(), want) and pending and np.isfinite(logprob.cpu().numpy()).all()
     del x
+
+
+@pytest.mark.parametrize("slots,heads,positions", [(1, 2, 40), (3, 1, 40), (3, 2, 1), (1, 1, 1)])
+def test_caches_with_dimensions_of_one_element(slots, heads, positions):
+    """torch gives the stride of a dimension of one element as it likes, and k and v different ones."""
+    from paper_2603_11273_amd import asr
+    g = torch.Generator(device="cuda").manual_seed(slots + heads + positions)
+    k, v = (torch.randn((slots, heads, positions, 64), generator=g, device="cuda") for _ in range(2))
+    q = torch.randn((slots, heads * 64), generator=g, device="cuda")
+    odd = [k.as_strided(k.shape, [s if n > 1 else one for n, s, one in zip(k.shape, k.stride(), (7, 5, 3, 1))])] + \
+          [v.as_strided(v.shape, [s if n > 1 else one for n, s, one in zip(v.shape, v.stride(), (1, 9, 64, 1))])]
+    start = torch.arange(slots + 1, dtype=torch.int32, device="cuda")
+    got = []
+    for kk, vv in ((k, v), odd):
+        plan = asr.SharedAttention(kk, vv, n_head=heads, rows=slots, groups=slots, max_group=1, group_start=start)
+        got.append(plan(q, torch.empty_like(q)))
+    assert torch.equal(*got)
+    q64, k64, v64 = q.cpu().double().view(slots, heads, 64), k.cpu().double(), v.cpu().double()
+    p = torch.softmax((q64[:, :, None] * k64).sum(-1) / 8, -1)
+    want = (p[..., None] * v64).sum(2).reshape(slots, -1)
+    # (scores of a few units: 66 steps of 2^-24 of sum |q k| below 100, twice that on the weights)
+    assert (got[0].cpu().double() - want).abs().max() <= 4 * 66 * 2.0 ** -24 * 100 * v64.abs().max()
