@@ -601,6 +601,7 @@ class Context:
     def set_slot_rules(self, slot, repetition=1.0, frequency=0.0, presence=0.0, temperature=1.0,
                        n_prompt=0, mask=-1, bias=()):
         """Rules of a slot (-1: of every slot filled from now on); bias: (token, value) pairs."""
+        bias = list(bias)
         tok, p_tok = _i32([t for t, _ in bias] or [0])
         val = np.ascontiguousarray([v for _, v in bias] or [0.0], dtype=np.float32)
         r = SlotRules(repetition, frequency, presence, temperature, n_prompt, mask, len(bias),

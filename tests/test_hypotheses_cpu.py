@@ -117,3 +117,24 @@ def test_a_dead_row_does_not_take_the_others_results(context):
             assert e.value.results is None and e.value.status == status
     ctx = context(asr.ASR_OK)
     assert list(ctx.step(slots=[2], tokens=[1])["argmax"]) == [-1] and ctx.serve_step(1)["policy"] == 2
+
+
+def test_biases_of_any_iterable(monkeypatch):
+    """(token, value) pairs from a list, a dict's items, a zip or a generator."""
+    got = []
+
+    class Library:
+        def asr_set_slot_rules(self, h, slot, r):
+            r = r._obj
+            got.append([(r.bias_token[i], r.bias_value[i]) for i in range(r.n_bias)])
+            return asr.ASR_OK
+    monkeypatch.setattr(asr, "lib", Library())
+    ctx = asr.Context.__new__(asr.Context)
+    ctx.h = None
+    pairs = [(7, 2.5), (11, -1.0), (7, 0.5)]
+    for bias in (pairs, zip([7, 11, 7], [2.5, -1.0, 0.5]), (p for p in pairs), tuple(pairs)):
+        ctx.set_slot_rules(0, bias=bias)
+    assert got == [pairs] * 4
+    ctx.set_slot_rules(0, bias={3: 1.0}.items())
+    ctx.set_slot_rules(0)
+    assert got[4:] == [[(3, 1.0)], []]
