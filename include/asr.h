@@ -182,7 +182,8 @@ typedef struct {
  * the same call.  Errors: ESTATE, ENODEV, EINVAL (bad id/slot/token,
  * duplicate slot, position at 448), EFULL (no free slot), EDEVICE (a HIP
  * error; or, with all arrays filled and every slot a step further, a row whose
- * logits hold a NaN or whose rules allow no token: argmax -1). */
+ * logits hold a NaN, whose rules allow no token (argmax -1) or whose best logit
+ * under rules is +infinite). */
 asr_status asr_step(asr_ctx* ctx, const asr_step_in* in, asr_step_out* out);
 
 /* Frees a slot for reuse. */
@@ -282,7 +283,7 @@ asr_status asr_serve_config(asr_ctx* ctx, const asr_serve_cfg* cfg);
  * every running request, commit.  Synchronises on the bound stream.  A request
  * whose rules (asr_set_slot_rules) allow no next token finishes with those it
  * has; its token in this step is -1.  So does one whose logits hold a NaN (or,
- * under rules, whose best logit is infinite), and the step then returns EDEVICE
+ * under rules, whose best logit is +infinite), and the step then returns EDEVICE
  * with `out` filled and every other request one token on. */
 asr_status asr_serve_step(asr_ctx* ctx, int64_t now_us, asr_serve_out* out);
 /* The same schedule without running the model (tokens -1), for queue-only
