@@ -597,6 +597,178 @@ typedef struct {
 asr_status asr_logit_rules_size(const asr_rules* r, size_t* bytes);
 asr_status asr_logit_rules(const asr_rules* r, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- a cache in pages of 8 bits, and tokens drawn by chance ----------------
+ * Stateless calls like the two above (device pointers, caller's scratch and
+ * stream, no allocation, no synchronisation, capturable); where a call takes no
+ * ws it needs none.
+ *
+ * A pool of pages holds keys and values of `page` positions each as e4m3 codes
+ * (OCP: 1 sign, 4 exponent, 3 mantissa bits, largest 448, no infinities, NaN =
+ * 0x7f and 0xff) with one float32 scale per head and block of 64 positions: a
+ * value is its code times the scale of its block.  Of page p
+ *   codes  + p * page_stride  (bytes):    [2][kv_heads][page / 64][64][64]
+ *   scales + p * scale_stride (elements): [2][kv_heads][page / 64]
+ * keys first, [position][dim] in a block, then values, [dim][position] in a block.
+ * Pages may lie further apart than their size (other layers' parts of the same
+ * page between them: one table then serves all layers).  codes 16-byte aligned,
+ * page_stride a multiple of 16; page a multiple of 64, at most 4096.
+ *   Position i of sequence s is position i % page of page table[s][i / page].  An
+ * entry outside [0, pages) is no page: its positions cannot be written and are
+ * not there to attend to. */
+typedef struct {
+  int32_t kv_heads, page, pages;
+  uint8_t* codes;
+  int64_t page_stride;
+  float* scales;
+  int64_t scale_stride;
+  const int32_t* table;      /* [sequences][columns], rows table_ld apart */
+  int64_t table_ld;
+  int32_t sequences, columns;
+} asr_pages;
+
+/* New keys and values into pages.  Sequence s holds length[s] positions; tokens
+ * token_start[s] <= i < token_start[s + 1] (NULL: token s alone), at most max_new
+ * of them, go to positions length[s], length[s] + 1, ..  In each block of 64
+ * positions that gets tokens, per head and for keys and values apart:
+ *   need   = the smallest power of two of at least 2^-120 that is >= max |x| / 448,
+ *            x the block's new values (those that are not finite do not count);
+ *   scale' = the larger of need and, where the block holds earlier positions, its scale;
+ *   code   = x / scale' rounded to nearest even; NaN where x is not finite;
+ * and where the scale grew the earlier positions' codes become (code scale /
+ * scale') rounded to nearest even.  (A block's scale that is not a power of two
+ * in [2^-120, 2^120], as a caller's own might be, is first rounded up to one, one
+ * that is not positive to 2^-120; codes past 448 become 448.)  Nothing else is
+ * written: positions behind the new ones stay as they were.  A negative length
+ * writes nothing, nor do positions past the table.  The sequences of a call must
+ * not share the pages that it writes.
+ *   k, v: [tokens][kv_heads * 64] float32 or bf16, rows ld elements apart, 16-byte
+ * aligned, ld a multiple of 16 bytes. */
+typedef struct {
+  asr_pages cache;
+  int32_t dtype;                 /* asr_dtype of k and v */
+  int32_t tokens, max_new;
+  const void* k;
+  const void* v;
+  int64_t ld;
+  const int32_t* token_start;    /* [sequences + 1] or NULL */
+  const int32_t* length;         /* [sequences] */
+} asr_page_write;
+asr_status asr_write_pages(const asr_page_write* w, void* stream);
+
+/* Attention of new tokens over the pages of their sequence:
+ *   out[r][h] = softmax over j of (scale q[r][h] . k_j) . v_j,
+ * j from first[r] (NULL: 0) to length[r] - 1 of the row's sequence, on cache head
+ * h / (n_head / n_kv_head).  Rows row_start[s] <= r < row_start[s + 1] (NULL: row s
+ * alone), at most max_rows of them, are of sequence s; row starts do not fall, rows
+ * of no sequence are left as they were.  One row a sequence is a decode step;
+ * several with one length are hypotheses of one clip, with rising ones a prompt or
+ * drafts under a causal mask.  Keys are read once for up to 64 queries of a
+ * sequence and cache head.  A negative first counts as 0, a length past max_keys
+ * or the table ends there; a row without any key gives zeros.  What a row does not
+ * see does not touch it, NaN codes included; what it sees makes it NaN as the
+ * formula does.  Sums are float32; a row's bits depend neither on the other rows nor
+ * on its place (with part_keys given; 0 lets the library split by the size of the
+ * call).
+ *   q: float32 [rows][n_head * 64], rows q_ld apart; out of type dtype, rows
+ * out_ld apart (both 16-byte aligned, q_ld and out_ld multiples of 4). */
+typedef struct {
+  asr_pages cache;
+  int32_t dtype;             /* asr_dtype of out */
+  int32_t n_head;
+  int32_t rows, max_rows;
+  int32_t max_keys;
+  int32_t part_keys;         /* keys per part of the work: 0, or a multiple of 256 up to 16384 */
+  float scale;
+  const float* q;
+  int64_t q_ld;
+  void* out;
+  int64_t out_ld;
+  const int32_t* row_start;  /* [sequences + 1] or NULL */
+  const int32_t* first;      /* [rows] or NULL */
+  const int32_t* length;     /* [rows] */
+} asr_paged_attention;
+asr_status asr_attend_pages_size(const asr_paged_attention* a, size_t* bytes);
+asr_status asr_attend_pages(const asr_paged_attention* a, void* ws, size_t ws_bytes, void* stream);
+
+/* The page tables of a next step.  Sequence s goes on from parent[s] (NULL: itself):
+ * itself, another one (a fork; any number may share a parent), or none (outside
+ * [0, sequences): it ends, or starts empty).  It keeps the parent's length and the
+ * pages that this covers, and gets pages until it holds want[s] positions (NULL: no
+ * more).  Pages that no sequence keeps are free.
+ *   Full pages are shared.  A last page that is partly filled will be written, so one
+ * sequence only keeps it: a page that some sequence keeps as a full one is left to
+ * those, otherwise the lowest s keeps it; every other gets a copy in a page of its own.
+ * Pages are given out in the order of sequences and, in a sequence, of positions, the
+ * lowest free number first; when none are left, the entries are -1.
+ *   compact != 0: the n pages then in use are numbers 0 to n - 1.  Kept pages from n
+ * on move, in order, to the lowest free numbers, and the pages given out come from
+ * those behind.
+ *   new_table, new_length: may be table and length themselves; otherwise they must
+ * not overlap.  Entries behind a sequence's pages are -1; table entries outside
+ * [0, pages) stay no page (-1).  room[s]: positions that the pages from the first on
+ * hold without a gap.  info: pages in use, pages that were missing, pages copied,
+ * pages moved.  Lengths are cut to [0, columns * page], want alike.
+ *   codes, scales: page p's code_bytes at codes + p * code_stride and scale_bytes at
+ * scales + p * scale_stride are copied when p is (all multiples of 4 bytes, codes and
+ * scales 4-byte aligned; NULL: the program copies its data itself).  sequences * columns at most 2^26,
+ * pages at most 2^22. */
+typedef struct {
+  int32_t sequences, columns, page, pages, compact;
+  const int32_t* table;
+  int64_t table_ld;
+  const int32_t* length;
+  const int32_t* parent;       /* [sequences] or NULL */
+  const int32_t* want;         /* [sequences] or NULL */
+  int32_t* new_table;
+  int64_t new_ld;
+  int32_t* new_length;
+  int32_t* room;               /* [sequences] or NULL */
+  int32_t* info;               /* [4] or NULL */
+  void* codes;
+  int64_t code_stride, code_bytes;
+  void* scales;
+  int64_t scale_stride, scale_bytes;
+} asr_page_tables;
+asr_status asr_next_tables_size(const asr_page_tables* t, size_t* bytes);
+asr_status asr_next_tables(const asr_page_tables* t, void* ws, size_t ws_bytes, void* stream);
+
+/* Tokens drawn from logits by given random numbers.  Row r follows parameter set
+ * s = set[r] (NULL: s = r; outside [0, sets): none).  With M the row's largest logit
+ * and T = temperature[s] (NULL: 1), w_v = e^{(l_v - M) / T}; a token whose logit is
+ * -inf has no weight and is never kept.  In the order of falling logits, equal ones by
+ * token, the row keeps the tokens
+ *   among the first top_k[s] (NULL or below 1: all),
+ *   before which the weights sum to less than top_p[s] of the sum over those first
+ *     top_k (NULL, NaN, 1 and above: all),
+ *   whose weight is at least min_p[s] (NULL, NaN: all);
+ * the first is always kept.  A temperature that is not above 0 keeps only the first, and
+ * T counts as 1.  Draw d of the row is the first kept token v, by number, at which the kept
+ * weights up to v sum to more than u[r][d] times their whole sum (u below 0 or NaN counts
+ * as 0, 1 and above as the float32 below 1).  Sums are of weights rounded to multiples of
+ * 2^(n - 62), 2^n the power of two not below the vocabulary, in whole numbers, so
+ * neither the work's split nor its order can change a token.
+ *   token [rows][draws]; logprob [rows][draws] or NULL: (l - M) / T - log sum over all v of
+ * w_v, in float32; kept [rows] or NULL: tokens kept.  A row whose logits hold a NaN or
+ * +inf, or only -inf, gives token -1, kept 0 and logprob NaN (only -inf: -inf).
+ *   vocab at most 1048576, rows at most 65535, draws at most 64. */
+typedef struct {
+  int32_t dtype;               /* asr_dtype of the logits */
+  int32_t rows, vocab, sets, draws;
+  const void* logits;
+  int64_t ld;
+  const float* u;              /* [rows][draws] */
+  const int32_t* set;          /* [rows] or NULL */
+  const float* temperature;    /* [sets] or NULL, each */
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* token;
+  float* logprob;
+  int32_t* kept;
+} asr_sampling;
+asr_status asr_sample_size(const asr_sampling* a, size_t* bytes);
+asr_status asr_sample(const asr_sampling* a, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

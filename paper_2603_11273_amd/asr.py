@@ -39,6 +39,8 @@ EXPORTED = [
     "asr_serve_plan",
     "asr_serve_tokens", "asr_serve_simulate", "asr_serve_stats",
     "asr_attend_shared_size", "asr_attend_shared", "asr_logit_rules_size", "asr_logit_rules",
+    "asr_write_pages", "asr_attend_pages_size", "asr_attend_pages", "asr_next_tables_size",
+    "asr_next_tables", "asr_sample_size", "asr_sample",
     "asr_hypotheses_size", "asr_bind_hypotheses", "asr_fork_slot", "asr_set_masks",
     "asr_set_slot_rules", "asr_set_slot_mask", "asr_step_topk",
 ]
@@ -107,6 +109,42 @@ class Rules(C.Structure):
         ("bias_len", C.c_void_p), ("mask", C.c_void_p), ("mask_ld", C.c_int64),
         ("mask_of", C.c_void_p), ("temperature", C.c_void_p), ("out", C.c_void_p),
         ("out_ld", C.c_int64), ("token", C.c_void_p), ("logprob", C.c_void_p)]
+
+
+class Pages(C.Structure):
+    _fields_ = [("kv_heads", C.c_int32), ("page", C.c_int32), ("pages", C.c_int32), ("codes", C.c_void_p),
+                ("page_stride", C.c_int64), ("scales", C.c_void_p), ("scale_stride", C.c_int64),
+                ("table", C.c_void_p), ("table_ld", C.c_int64), ("sequences", C.c_int32),
+                ("columns", C.c_int32)]
+
+
+class PageTokens(C.Structure):
+    _fields_ = [("cache", Pages), ("dtype", C.c_int32), ("tokens", C.c_int32), ("max_new", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("ld", C.c_int64), ("token_start", C.c_void_p),
+                ("length", C.c_void_p)]
+
+
+class PageQueries(C.Structure):
+    _fields_ = [("cache", Pages)] + [(n, C.c_int32) for n in (
+        "dtype", "n_head", "rows", "max_rows", "max_keys", "part_keys")] + [
+        ("scale", C.c_float), ("q", C.c_void_p), ("q_ld", C.c_int64), ("out", C.c_void_p),
+        ("out_ld", C.c_int64), ("row_start", C.c_void_p), ("first", C.c_void_p), ("length", C.c_void_p)]
+
+
+class NextTables(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("sequences", "columns", "page", "pages", "compact")] + [
+        ("table", C.c_void_p), ("table_ld", C.c_int64), ("length", C.c_void_p), ("parent", C.c_void_p),
+        ("want", C.c_void_p), ("new_table", C.c_void_p), ("new_ld", C.c_int64),
+        ("new_length", C.c_void_p), ("room", C.c_void_p), ("info", C.c_void_p), ("codes", C.c_void_p),
+        ("code_stride", C.c_int64), ("code_bytes", C.c_int64), ("scales", C.c_void_p),
+        ("scale_stride", C.c_int64), ("scale_bytes", C.c_int64)]
+
+
+class Sampling(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "rows", "vocab", "sets", "draws")] + [
+        ("logits", C.c_void_p), ("ld", C.c_int64), ("u", C.c_void_p), ("set", C.c_void_p),
+        ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+        ("token", C.c_void_p), ("logprob", C.c_void_p), ("kept", C.c_void_p)]
 
 
 class SlotRules(C.Structure):
@@ -180,6 +218,13 @@ def _load():
         "asr_attend_shared": [P(Attention), vp, C.c_size_t, vp],
         "asr_logit_rules_size": [P(Rules), P(C.c_size_t)],
         "asr_logit_rules": [P(Rules), vp, C.c_size_t, vp],
+        "asr_write_pages": [P(PageTokens), vp],
+        "asr_attend_pages_size": [P(PageQueries), P(C.c_size_t)],
+        "asr_attend_pages": [P(PageQueries), vp, C.c_size_t, vp],
+        "asr_next_tables_size": [P(NextTables), P(C.c_size_t)],
+        "asr_next_tables": [P(NextTables), vp, C.c_size_t, vp],
+        "asr_sample_size": [P(Sampling), P(C.c_size_t)],
+        "asr_sample": [P(Sampling), vp, C.c_size_t, vp],
         "asr_hypotheses_size": [vp, i32, i32, P(C.c_size_t)],
         "asr_bind_hypotheses": [vp, i32, i32, vp, C.c_size_t],
         "asr_fork_slot": [vp, i32, i32],
@@ -432,6 +477,219 @@ class LogitRules(_Operator):
             a.out_ld = 0 if out is None else self._ld(out)
             a.token = self._need(token, "token", torch.int32, self._best, self._dev)
             a.logprob = self._need(logprob, "logprob", torch.float32, self._best, self._dev)
+            self._launch(stream)
+
+
+def _no_scratch(args, bytes):
+    """The _size call of an operator without scratch."""
+    return ASR_OK
+
+
+class _Paged(_Operator):
+    """What the plans over a pool of pages share: the pool and its tables.
+
+    codes uint8 [pages][2][kv heads][page / 64][64][64] and scales float32
+    [pages][2][kv heads][page / 64], on the GPU, everything inside a page contiguous (pages may
+    lie further apart: codes[:, layer] of a pool of several layers); keys [position][dim] in a
+    block, values [dim][position].  table int32 [sequences][columns]."""
+
+    def _pages(self, codes, scales, table):
+        import torch
+        if not (codes.is_cuda and codes.dtype in (torch.uint8, torch.float8_e4m3fn) and codes.dim() == 6
+                and codes.shape[1] == 2 and tuple(codes.shape[4:]) == (64, 64)):
+            raise TypeError("codes must be device bytes of shape [pages][2][kv heads][page / 64][64][64]")
+        dev, n = codes.device, codes.shape[0]
+        if scales.device != dev or scales.dtype != torch.float32 or scales.shape != codes.shape[:4]:
+            raise TypeError(f"scales must be float32 of shape {tuple(codes.shape[:4])} on {dev}")
+        if n and not (codes[0].is_contiguous() and scales[0].is_contiguous()):
+            raise TypeError("codes and scales must be contiguous inside a page")
+        if table.dim() != 2:
+            raise TypeError("table must be [sequences][columns]")
+        self._need(table, "table", torch.int32, table.shape, dev, ld=True)
+        stride = codes.stride(0) if n > 1 else max(codes[0].numel() if n else 0, 0)
+        scale_stride = scales.stride(0) if n > 1 else scales[0].numel() if n else 0
+        self._keep = [codes, scales, table]
+        return dev, Pages(codes.shape[2], codes.shape[3] * 64, n, codes.data_ptr(), stride,
+                          scales.data_ptr(), scale_stride, table.data_ptr(), self._ld(table),
+                          table.shape[0], table.shape[1])
+
+
+class PageWrite(_Paged):
+    """asr_write_pages as a plan: pool, tables and lengths once, then plan(k, v) per step.
+
+    codes, scales, table: a pool of pages (see _Paged).  Sequence s holds length[s] positions
+    and gets tokens token_start[s] .. token_start[s + 1] - 1 behind them (None: token s alone), at
+    most max_new.  The int32 device tensors table, length [sequences] and token_start
+    [sequences + 1] are read at every call.  plan(k, v): [tokens][kv heads * 64] of `dtype`
+    (float32 or bfloat16), rows the same distance apart, on `stream` (default: torch's current
+    stream)."""
+
+    def __init__(self, codes, scales, table, length, *, tokens, dtype, token_start=None, max_new=1):
+        import torch
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("keys and values must be float32 or bfloat16")
+        dev, pages = self._pages(codes, scales, table)
+        n = table.shape[0]
+        args = PageTokens(pages, BF16 if dtype == torch.bfloat16 else F32, tokens, max_new, None, None, 0,
+                          self._need(token_start, "token_start", torch.int32, (n + 1,), dev),
+                          self._need(length, "length", torch.int32, (n,), dev))
+        if length is None:
+            raise TypeError("length must be given")
+        self._keep += [length, token_start]
+        self._dtype, self._shape = dtype, (tokens, codes.shape[2] * 64)
+        run = lambda ref, ws, n, stream: lib.asr_write_pages(ref, stream)  # noqa: E731
+        super().__init__(dev, torch.empty(0, dtype=torch.uint8, device=dev), _no_scratch, run, args)
+
+    def __call__(self, k, v, stream=None):
+        a = self._args
+        with self._turn:
+            a.k = self._need(k, "k", self._dtype, self._shape, self._dev, ld=True)
+            a.v = self._need(v, "v", self._dtype, self._shape, self._dev, ld=True)
+            if a.k is None or a.v is None or self._ld(k) != self._ld(v):
+                raise TypeError("k and v must be given, their rows the same distance apart")
+            a.ld = self._ld(k)
+            self._launch(stream)
+
+
+class PagedAttention(_Paged):
+    """asr_attend_pages as a plan: pool, tables and rows once, then plan(q, out) per step.
+
+    codes, scales, table: a pool of pages (see _Paged).  Rows row_start[s] .. row_start[s + 1] - 1
+    are of sequence s (None: row s alone), at most max_rows of them; row r attends to positions
+    first[r] (None: 0) .. length[r] - 1.  The int32 device tensors table, row_start
+    [sequences + 1], first and length [rows] are read at every call.  max_keys bounds the lengths
+    (default: what the table holds).  plan(q, out): q float32 [rows][n_head * 64], out
+    [rows][n_head * 64] of `dtype` (float32 or bfloat16), on `stream` (default: torch's current
+    stream).  One call at a time: calls that may overlap on the GPU need plans with a workspace
+    each (default: one of the plan's own)."""
+
+    def __init__(self, codes, scales, table, length, *, n_head, rows, row_start=None, max_rows=1,
+                 first=None, max_keys=None, scale=0.125, dtype=None, part_keys=0, workspace=None):
+        import torch
+        dtype = torch.bfloat16 if dtype is None else dtype
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("out must be float32 or bfloat16")
+        dev, pages = self._pages(codes, scales, table)
+        if length is None:
+            raise TypeError("length must be given")
+        one = lambda t, name, n: self._need(t, name, torch.int32, (n,), dev)  # noqa: E731
+        most = min(pages.columns * pages.page, (1 << 31) - 1) if max_keys is None else max_keys
+        args = PageQueries(pages, BF16 if dtype == torch.bfloat16 else F32, n_head, rows, max_rows, most,
+                           part_keys, scale, None, 0, None, 0, one(row_start, "row_start", pages.sequences + 1),
+                           one(first, "first", rows), one(length, "length", rows))
+        self._keep += [length, row_start, first]
+        self._dtype, self._shape = dtype, (rows, n_head * 64)
+        super().__init__(dev, workspace, lib.asr_attend_pages_size, lib.asr_attend_pages, args)
+
+    def __call__(self, q, out, stream=None):
+        import torch
+        a = self._args
+        with self._turn:
+            a.q = self._need(q, "q", torch.float32, self._shape, self._dev, ld=True)
+            a.out = self._need(out, "out", self._dtype, self._shape, self._dev, ld=True)
+            if a.q is None or a.out is None:
+                raise TypeError("q and out must be given")
+            a.q_ld, a.out_ld = self._ld(q), self._ld(out)
+            self._launch(stream)
+        return out
+
+
+class PageTables(_Operator):
+    """asr_next_tables as a plan: the tables of a next step from those of this one.
+
+    codes and scales: a pool, pages first, everything inside a page contiguous (all layers of a
+    model in a page, or one), or None (the program copies its data itself; then pages and page say what
+    the pool is).  table int32 [sequences][columns] and length [sequences] are those before the call;
+    new_table and new_length those after it, or None: in place.  parent [sequences]: the
+    sequence that each goes on from (None: itself; outside the range: none); want: the positions
+    that each must have room for.  room [sequences] and info [4] (pages in use, missing, copied,
+    moved) may be None.  Device tensors of int32, read at every call.  plan(compact=False): with
+    compact the pages in use end up as the first of the pool.  One call at a time: calls that may
+    overlap on the GPU need plans with a workspace each (default: one of the plan's own)."""
+
+    def __init__(self, codes, scales, table, length, *, parent=None, want=None, new_table=None,
+                 new_length=None, room=None, info=None, page=None, pages=None, workspace=None):
+        import torch
+        i32 = torch.int32
+        if table is None or not table.is_cuda or table.dim() != 2 or length is None:
+            raise TypeError("table must be a device tensor of [sequences][columns], with its lengths")
+        dev, (n, columns) = table.device, table.shape
+        if codes is not None:
+            if codes.dim() < 3 or codes.dtype not in (torch.uint8, torch.float8_e4m3fn):
+                raise TypeError("codes must be bytes, pages first")
+            page = codes.shape[-3] * 64 if page is None else page
+            pages = codes.shape[0] if pages is None else pages
+        if page is None or pages is None:
+            raise TypeError("without codes, page and pages must be given")
+
+        def pool(t, name):
+            if t is None:
+                return None, 0, 0
+            if t.device != dev or t.shape[0] < pages or (pages and not t[0].is_contiguous()):
+                raise TypeError(f"{name} must be {pages} pages on {dev}, contiguous inside a page")
+            size = t[0].numel() * t.element_size() if pages else 0
+            return t.data_ptr(), t.stride(0) * t.element_size() if pages > 1 else size, size
+
+        new_table = table if new_table is None else new_table
+        new_length = length if new_length is None else new_length
+        one = lambda t, name: self._need(t, name, i32, (n,), dev)  # noqa: E731
+        args = NextTables(n, columns, page, pages, 0, self._need(table, "table", i32, (n, columns), dev, ld=True),
+                          self._ld(table), one(length, "length"), one(parent, "parent"), one(want, "want"),
+                          self._need(new_table, "new_table", i32, (n, columns), dev, ld=True),
+                          self._ld(new_table), one(new_length, "new_length"), one(room, "room"),
+                          self._need(info, "info", i32, (4,), dev), *pool(codes, "codes"), *pool(scales, "scales"))
+        self._keep = (codes, scales, table, length, parent, want, new_table, new_length, room, info)
+        super().__init__(dev, workspace, lib.asr_next_tables_size, lib.asr_next_tables, args)
+
+    def __call__(self, compact=False, stream=None):
+        with self._turn:
+            self._args.compact = int(bool(compact))
+            self._launch(stream)
+
+
+class Sampler(_Operator):
+    """asr_sample as a plan: parameter sets once, then plan(logits, u, token, ...) per step.
+
+    Row r follows parameter set set[r] (None: r).  Device tensors, read at every call: set int32
+    [rows]; temperature, top_p, min_p float32 and top_k int32 [sets].  plan(logits, u, token,
+    logprob, kept): logits [rows][vocab] of `dtype` (float32 or bfloat16), u float32
+    [rows][draws] in [0, 1), token int32 and logprob float32 [rows][draws], kept int32 [rows]
+    (logprob and kept may be None).  One call at a time: calls that may overlap on the GPU need
+    plans with a workspace each (default: one of the plan's own)."""
+
+    def __init__(self, rows, vocab, dtype, *, draws=1, sets=None, set=None, temperature=None, top_k=None,
+                 top_p=None, min_p=None, device=None, workspace=None):
+        import torch
+        i32, f32 = torch.int32, torch.float32
+        if dtype not in (f32, torch.bfloat16):
+            raise TypeError("logits must be float32 or bfloat16")
+        given = [t for t in (set, temperature, top_k, top_p, min_p) if t is not None]
+        dev = torch.device(device if device is not None else
+                           given[0].device if given else torch.cuda.current_device())
+        if dev.type != "cuda":
+            raise TypeError(f"tokens are drawn on a GPU, not on {dev}")
+        if dev.index is None:
+            dev = torch.device(dev.type, torch.cuda.current_device())
+        n = rows if sets is None else sets
+        one = lambda t, name, kind: self._need(t, name, kind, (n,), dev)  # noqa: E731
+        args = Sampling(BF16 if dtype == torch.bfloat16 else F32, rows, vocab, n, draws, None, 0, None,
+                        self._need(set, "set", i32, (rows,), dev), one(temperature, "temperature", f32),
+                        one(top_k, "top_k", i32), one(top_p, "top_p", f32), one(min_p, "min_p", f32),
+                        None, None, None)
+        self._keep = (set, temperature, top_k, top_p, min_p)
+        self._dtype, self._shape, self._drawn = dtype, (rows, vocab), (rows, draws)
+        super().__init__(dev, workspace, lib.asr_sample_size, lib.asr_sample, args)
+
+    def __call__(self, logits, u, token, logprob=None, kept=None, stream=None):
+        import torch
+        a = self._args
+        with self._turn:
+            a.logits = self._need(logits, "logits", self._dtype, self._shape, self._dev, ld=True)
+            a.ld = self._ld(logits)
+            a.u = self._need(u, "u", torch.float32, self._drawn, self._dev)
+            a.token = self._need(token, "token", torch.int32, self._drawn, self._dev)
+            a.logprob = self._need(logprob, "logprob", torch.float32, self._drawn, self._dev)
+            a.kept = self._need(kept, "kept", torch.int32, self._shape[:1], self._dev)
             self._launch(stream)
 
 

@@ -21,7 +21,7 @@ SYNTH_LIB = os.path.join(HERE, "libasr_synth.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 HIP_SOURCES = ["k_misc.hip", "k_gemm.hip", "k_attn.hip", "k_rows.hip", "k_share.hip", "k_rules.hip",
-               "operators.hip", "runtime.hip"]
+               "k_pages.hip", "k_paged.hip", "k_sample.hip", "operators.hip", "runtime.hip"]
 CPP_SOURCES = ["queue.cpp", "serve.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed fp32 instructions are disabled: hipcc emits them from plain float

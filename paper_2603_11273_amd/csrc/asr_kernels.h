@@ -237,6 +237,79 @@ struct RulesLaunch {
 size_t rules_ws_bytes(int rows, int vocab, int k);
 void logit_rules(const RulesLaunch& a, bool bf16, hipStream_t s);
 
+// A pool of pages of e4m3 codes and the tables of its sequences (asr_pages): one
+// scale per head and kPageBlock positions.
+constexpr int kPageBlock = 64;
+struct Pages {
+  uint8_t* codes;
+  float* scales;
+  int64_t page_stride, scale_stride;              // bytes, elements
+  const int32_t* table;
+  int64_t table_ld;
+  int32_t kv_heads, page, pages, sequences, columns;
+};
+// New keys and values into pages (asr_write_pages).
+struct PageWriteLaunch {
+  Pages c;
+  const void *k, *v;
+  int64_t ld;
+  const int32_t *token_start, *length;
+  int32_t tokens, max_new;
+};
+void write_pages(const PageWriteLaunch& a, bool bf16, hipStream_t s);
+
+// Attention over pages (asr_attend_pages), in parts of at most `part` keys, `parts`
+// of them at most (more than one: a record of each in `rec`, 66 floats per row, head
+// and part).
+struct PagedLaunch {
+  Pages c;
+  const float* q;
+  int64_t q_ld;
+  void* out;
+  int64_t out_ld;
+  float qmul;                                     // scale * log2(e)
+  const int32_t *row_start, *first, *length;
+  int32_t n_head, rows, max_rows, max_keys, part, parts;
+  float* rec;
+};
+hipError_t attend_pages(const PagedLaunch& a, bool bf16, hipStream_t s);
+
+// The page tables of a next step (asr_next_tables).
+struct TablesLaunch {
+  int32_t sequences, columns, page, pages;
+  bool compact;
+  const int32_t* table;
+  int64_t table_ld;
+  const int32_t *length, *parent, *want;
+  int32_t* new_table;
+  int64_t new_ld;
+  int32_t *new_length, *room, *info;
+  void* codes;
+  int64_t code_stride, code_bytes;
+  void* scales;
+  int64_t scale_stride, scale_bytes;
+  int32_t* ws;                                    // tables_ws_words
+};
+int64_t tables_ws_words(int sequences, int columns, int pages);
+void next_tables(const TablesLaunch& a, hipStream_t s);
+
+// Tokens drawn from logits (asr_sample).
+constexpr int kSampleMaxDraws = 64;
+struct SampleLaunch {
+  const void* logits;
+  int64_t ld;
+  int32_t rows, vocab, sets, draws;
+  const float* u;
+  const int32_t* set;
+  const float* temperature;
+  const int32_t* top_k;
+  const float *top_p, *min_p;
+  int32_t* token;
+  float* logprob;
+  int32_t* kept;
+};
+hipError_t sample(const SampleLaunch& a, bool bf16, hipStream_t s);
+
 // What a decode step knows of its rows into the per-slot arrays that the rules
 // read: the token at the row's position, the history's length, the scalars of
 // the slot's rules (row arrays, D apart, in the order of the members).

@@ -1,5 +1,5 @@
-// Entry points of the stateless decode operators: argument checks, the split of
-// the work, and the launches.
+// Entry points of the stateless operators: argument checks, the split of the work,
+// and the launches.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -197,6 +197,92 @@ asr_status check_ws(const void* ws, size_t have, size_t need) {
   return ASR_OK;
 }
 
+// ---------------------------------------------------------------------------
+// Pages of 8 bits
+// ---------------------------------------------------------------------------
+asr_status check_pages(const asr_pages& c, Pages* p) {
+  if (c.kv_heads <= 0 || c.kv_heads > 65536) return fail(ASR_EINVAL, "kv_heads out of [1, 65536]");
+  if (c.page < kPageBlock || c.page > 4096 || c.page % kPageBlock) return fail(ASR_EINVAL, "page must be a multiple of 64, at most 4096");
+  if (c.pages < 1 || c.sequences < 0 || c.columns < 1) return fail(ASR_EINVAL, "pages and columns must be positive, sequences not negative");
+  if ((int64_t)c.columns * c.page > (1 << 30)) return fail(ASR_EINVAL, "more than 2^30 positions in a sequence");
+  const int64_t blocks = 2 * (int64_t)c.kv_heads * (c.page / kPageBlock);
+  if (c.page_stride < blocks * kPageBlock * kHeadDim || c.page_stride % 16 || c.scale_stride < blocks)
+    return fail(ASR_EINVAL, "page_stride must be a multiple of 16 bytes, and the strides at least a page's size");
+  if (c.table_ld < c.columns) return fail(ASR_EINVAL, "table_ld below columns");
+  if (!c.codes || !aligned(c.codes, 16) || !c.scales || !aligned(c.scales, 4)) return fail(ASR_EINVAL, "codes must be 16-byte aligned, scales 4-byte, neither NULL");
+  if (!c.table) return fail(ASR_EINVAL, "NULL table");
+  *p = {c.codes, c.scales, c.page_stride, c.scale_stride, c.table, c.table_ld, c.kv_heads, c.page, c.pages, c.sequences, c.columns};
+  return ASR_OK;
+}
+
+asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* bytes) {
+  if (!a) return fail(ASR_EINVAL, "NULL argument");
+  if (a->dtype != ASR_F32 && a->dtype != ASR_BF16) return fail(ASR_EINVAL, "dtype");
+  const asr_status st = check_pages(a->cache, &s->c);
+  if (st != ASR_OK) return st;
+  if (a->n_head <= 0 || a->n_head % a->cache.kv_heads || a->n_head > 65536)
+    return fail(ASR_EINVAL, "kv_heads must divide n_head (at most 65536)");
+  if (a->rows < 0 || a->max_keys < 0) return fail(ASR_EINVAL, "negative size");
+  if (a->rows > 0 && (a->max_rows < 1 || a->max_rows > a->rows)) return fail(ASR_EINVAL, "max_rows out of [1, rows]");
+  if (!a->row_start && a->rows > a->cache.sequences) return fail(ASR_EINVAL, "more rows than sequences, and no row_start");
+  if (a->part_keys != 0 && (a->part_keys < 256 || a->part_keys > 16384 || a->part_keys % 256))
+    return fail(ASR_EINVAL, "part_keys must be 0 or a multiple of 256, at most 16384");
+  if (!std::isfinite(a->scale)) return fail(ASR_EINVAL, "scale");
+  const int64_t most = std::min<int64_t>(a->max_keys, (int64_t)a->cache.columns * a->cache.page);
+  if ((double)a->rows * a->n_head >= 67108864.0) return fail(ASR_EINVAL, "too much work for one call");
+  s->q = a->q;
+  s->q_ld = a->q_ld;
+  s->out = a->out;
+  s->out_ld = a->out_ld;
+  s->qmul = a->scale * 1.4426950408889634f;
+  s->row_start = a->row_start;
+  s->first = a->first;
+  s->length = a->length;
+  s->n_head = a->n_head;
+  s->rows = a->rows;
+  s->max_rows = a->row_start ? a->max_rows : 1;
+  s->max_keys = (int32_t)most;
+  *bytes = 0;
+  return ASR_OK;
+}
+
+asr_status plan_tables(const asr_page_tables* t, TablesLaunch* s, size_t* bytes) {
+  if (!t) return fail(ASR_EINVAL, "NULL argument");
+  if (t->sequences < 0 || t->columns < 1 || t->page < 1 || t->pages < 1) return fail(ASR_EINVAL, "sizes must be positive");
+  if (t->pages > (1 << 22) || (int64_t)t->sequences * t->columns > (1 << 26) || (int64_t)t->columns * t->page > (1 << 30))
+    return fail(ASR_EINVAL, "more than 2^22 pages, 2^26 table entries or 2^30 positions in a sequence");
+  if (t->table_ld < t->columns || t->new_ld < t->columns) return fail(ASR_EINVAL, "table_ld or new_ld below columns");
+  if (t->codes && (t->code_bytes < 0 || t->code_bytes % 4 || t->code_stride < t->code_bytes || t->code_stride % 4 || !aligned(t->codes, 4)))
+    return fail(ASR_EINVAL, "codes: sizes and addresses must be multiples of 4 bytes, the stride at least the size");
+  if (t->scales && (t->scale_bytes < 0 || t->scale_bytes % 4 || t->scale_stride < t->scale_bytes || t->scale_stride % 4 || !aligned(t->scales, 4)))
+    return fail(ASR_EINVAL, "scales: sizes and addresses must be multiples of 4 bytes, the stride at least the size");
+  *s = {t->sequences, t->columns, t->page, t->pages, t->compact != 0, t->table, t->table_ld, t->length, t->parent, t->want,
+        t->new_table, t->new_ld, t->new_length, t->room, t->info, t->codes, t->code_stride, t->codes ? t->code_bytes : 0,
+        t->scales, t->scale_stride, t->scales ? t->scale_bytes : 0, nullptr};
+  *bytes = 4 * (kCounters + (size_t)tables_ws_words(t->sequences, t->columns, t->pages));
+  return ASR_OK;
+}
+
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  return (uintptr_t)a < (uintptr_t)b + (uint64_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uint64_t)a_bytes;
+}
+
+// ---------------------------------------------------------------------------
+// Sampling
+// ---------------------------------------------------------------------------
+asr_status plan_sample(const asr_sampling* a, SampleLaunch* s, size_t* bytes) {
+  if (!a) return fail(ASR_EINVAL, "NULL argument");
+  if (a->dtype != ASR_F32 && a->dtype != ASR_BF16) return fail(ASR_EINVAL, "dtype");
+  if (a->rows < 0 || a->rows > 65535) return fail(ASR_EINVAL, "rows out of [0, 65535]");
+  if (a->vocab < 1 || a->vocab > kRulesMaxVocab) return fail(ASR_EINVAL, "vocab out of [1, 1048576]");
+  if (a->draws < 1 || a->draws > kSampleMaxDraws) return fail(ASR_EINVAL, "draws out of [1, 64]");
+  if (a->sets < 0) return fail(ASR_EINVAL, "negative size");
+  *s = {a->logits, a->ld, a->rows, a->vocab, a->sets, a->draws, a->u, a->set, a->temperature, a->top_k, a->top_p, a->min_p,
+        a->token, a->logprob, a->kept};
+  *bytes = 0;
+  return ASR_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -260,6 +346,118 @@ asr_status asr_logit_rules(const asr_rules* r, void* ws, size_t ws_bytes, void* 
     s.counters = r->k > 0 && blocks <= cu_count() ? (uint32_t*)ws : nullptr;
     logit_rules(s, r->dtype == ASR_BF16, (hipStream_t)stream);
     return launched(hipSuccess);
+  });
+}
+
+asr_status asr_write_pages(const asr_page_write* w, void* stream) {
+  return guarded([&]() -> asr_status {
+    if (!w) return fail(ASR_EINVAL, "NULL argument");
+    if (w->dtype != ASR_F32 && w->dtype != ASR_BF16) return fail(ASR_EINVAL, "dtype");
+    PageWriteLaunch s{};
+    const asr_status st = check_pages(w->cache, &s.c);
+    if (st != ASR_OK) return st;
+    if (w->tokens < 0 || w->max_new < 0) return fail(ASR_EINVAL, "negative size");
+    if (!w->token_start && w->tokens < w->cache.sequences) return fail(ASR_EINVAL, "fewer tokens than sequences, and no token_start");
+    if (w->cache.sequences == 0 || w->tokens == 0 || w->max_new == 0) return ASR_OK;
+    if (!w->k || !w->v || !w->length) return fail(ASR_EINVAL, "NULL k, v or length");
+    const int64_t unit = w->dtype == ASR_BF16 ? 8 : 4;
+    if (!aligned(w->k, 16) || !aligned(w->v, 16) || w->ld < (int64_t)w->cache.kv_heads * kHeadDim || w->ld % unit)
+      return fail(ASR_EINVAL, "k and v must be 16-byte aligned, ld a multiple of 16 bytes and at least kv_heads * 64");
+    s.k = w->k;
+    s.v = w->v;
+    s.ld = w->ld;
+    s.token_start = w->token_start;
+    s.length = w->length;
+    s.tokens = w->tokens;
+    s.max_new = w->token_start ? std::min(w->max_new, w->tokens) : 1;
+    // (a launch has fewer than 2^32 threads)
+    if ((double)w->cache.sequences * w->cache.kv_heads * 2 * ((double)s.max_new / kPageBlock + 2) >= 16777216.0)
+      return fail(ASR_EINVAL, "too much work for one call");
+    write_pages(s, w->dtype == ASR_BF16, (hipStream_t)stream);
+    return launched(hipSuccess);
+  });
+}
+
+asr_status asr_attend_pages_size(const asr_paged_attention* a, size_t* bytes) {
+  return guarded([&]() -> asr_status {
+    if (!bytes) return fail(ASR_EINVAL, "NULL argument");
+    PagedLaunch s{};
+    return plan_paged(a, &s, bytes);
+  });
+}
+
+asr_status asr_attend_pages(const asr_paged_attention* a, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> asr_status {
+    PagedLaunch s{};
+    size_t need = 0;
+    asr_status st = plan_paged(a, &s, &need);
+    if (st != ASR_OK) return st;
+    if (a->rows == 0 || a->cache.sequences == 0) return ASR_OK;
+    if (!a->q || !a->out || !a->length) return fail(ASR_EINVAL, "NULL q, out or length");
+    const int64_t width = (int64_t)a->n_head * kHeadDim;
+    if (a->q_ld < width || a->out_ld < width || a->q_ld % 4 || a->out_ld % 4)
+      return fail(ASR_EINVAL, "q_ld and out_ld must be multiples of 4, at least n_head * 64");
+    if (!aligned(a->q, 16) || !aligned(a->out, 16)) return fail(ASR_EINVAL, "q and out must be 16-byte aligned");
+    st = check_ws(ws, ws_bytes, need);
+    if (st != ASR_OK) return st;
+    s.rec = need ? (float*)ws + kCounters : nullptr;
+    return launched(attend_pages(s, a->dtype == ASR_BF16, (hipStream_t)stream));
+  });
+}
+
+asr_status asr_next_tables_size(const asr_page_tables* t, size_t* bytes) {
+  return guarded([&]() -> asr_status {
+    if (!bytes) return fail(ASR_EINVAL, "NULL argument");
+    TablesLaunch s{};
+    return plan_tables(t, &s, bytes);
+  });
+}
+
+asr_status asr_next_tables(const asr_page_tables* t, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> asr_status {
+    TablesLaunch s{};
+    size_t need = 0;
+    asr_status st = plan_tables(t, &s, &need);
+    if (st != ASR_OK) return st;
+    if (t->sequences > 0) {
+      if (!t->table || !t->length || !t->new_table || !t->new_length) return fail(ASR_EINVAL, "NULL table or length");
+      const bool same = (const void*)t->table == t->new_table, same_length = (const void*)t->length == t->new_length;
+      if (same != same_length || (same && t->table_ld != t->new_ld))
+        return fail(ASR_EINVAL, "in place are both the table and the lengths, with one stride");
+      const int64_t n = t->sequences;
+      if (!same && (overlap(t->table, ((n - 1) * t->table_ld + t->columns) * 4, t->new_table, ((n - 1) * t->new_ld + t->columns) * 4) ||
+                    overlap(t->length, n * 4, t->new_length, n * 4)))
+        return fail(ASR_EINVAL, "the new table or lengths overlap the old ones");
+    }
+    st = check_ws(ws, ws_bytes, need);
+    if (st != ASR_OK) return st;
+    s.ws = (int32_t*)ws + kCounters;
+    next_tables(s, (hipStream_t)stream);
+    return launched(hipSuccess);
+  });
+}
+
+asr_status asr_sample_size(const asr_sampling* a, size_t* bytes) {
+  return guarded([&]() -> asr_status {
+    if (!bytes) return fail(ASR_EINVAL, "NULL argument");
+    SampleLaunch s{};
+    return plan_sample(a, &s, bytes);
+  });
+}
+
+asr_status asr_sample(const asr_sampling* a, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> asr_status {
+    SampleLaunch s{};
+    size_t need = 0;
+    asr_status st = plan_sample(a, &s, &need);
+    if (st != ASR_OK) return st;
+    if (a->rows == 0) return ASR_OK;
+    if (!a->logits || a->ld < a->vocab) return fail(ASR_EINVAL, "logits: NULL, or ld below the vocabulary");
+    if (!aligned(a->logits, a->dtype == ASR_BF16 ? 2 : 4)) return fail(ASR_EINVAL, "logits must be aligned to their type");
+    if (!a->u || !a->token) return fail(ASR_EINVAL, "NULL u or token");
+    st = check_ws(ws, ws_bytes, need);
+    if (st != ASR_OK) return st;
+    return launched(sample(s, a->dtype == ASR_BF16, (hipStream_t)stream));
   });
 }
 
