@@ -272,7 +272,9 @@ struct PagedLaunch {
   int32_t n_head, rows, max_rows, max_keys, part, parts;
   float* rec;
 };
-hipError_t attend_pages(const PagedLaunch& a, bool bf16, hipStream_t s);
+void attend_pages(const PagedLaunch& a, bool bf16, hipStream_t s);
+// 16-column query tiles that a block holds, of `cols` queries of a sequence and cache head
+int paged_query_tiles(int cols);
 
 // The page tables of a next step (asr_next_tables).
 struct TablesLaunch {
@@ -308,7 +310,7 @@ struct SampleLaunch {
   float* logprob;
   int32_t* kept;
 };
-hipError_t sample(const SampleLaunch& a, bool bf16, hipStream_t s);
+void sample(const SampleLaunch& a, bool bf16, hipStream_t s);
 
 // What a decode step knows of its rows into the per-slot arrays that the rules
 // read: the token at the row's position, the history's length, the scalars of

@@ -258,14 +258,13 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit_log2)
 
 }  // namespace
 
-hipError_t sample(const SampleLaunch& a, bool bf16, hipStream_t s) {
+void sample(const SampleLaunch& a, bool bf16, hipStream_t s) {
   int log2 = 0;
   while ((1 << log2) < a.vocab) ++log2;
   if (bf16)
     k_sample<bf16_t><<<dim3((unsigned)a.rows), SM_NT, 0, s>>>(a, 62 - log2);
   else
     k_sample<float><<<dim3((unsigned)a.rows), SM_NT, 0, s>>>(a, 62 - log2);
-  return hipSuccess;
 }
 
 }  // namespace asr

@@ -215,6 +215,10 @@ asr_status check_pages(const asr_pages& c, Pages* p) {
   return ASR_OK;
 }
 
+// A part is a block of 64 keys for each of four waves at least; a lane knows the page
+// of each of its wave's blocks.
+constexpr int kPartStep = 4 * kPageBlock, kMostPart = 64 * kPartStep;
+
 asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* bytes) {
   if (!a) return fail(ASR_EINVAL, "NULL argument");
   if (a->dtype != ASR_F32 && a->dtype != ASR_BF16) return fail(ASR_EINVAL, "dtype");
@@ -229,7 +233,23 @@ asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* byte
     return fail(ASR_EINVAL, "part_keys must be 0 or a multiple of 256, at most 16384");
   if (!std::isfinite(a->scale)) return fail(ASR_EINVAL, "scale");
   const int64_t most = std::min<int64_t>(a->max_keys, (int64_t)a->cache.columns * a->cache.page);
-  if ((double)a->rows * a->n_head >= 67108864.0) return fail(ASR_EINVAL, "too much work for one call");
+  const int64_t per = a->n_head / a->cache.kv_heads, cols = (a->row_start ? a->max_rows : 1) * per;
+  if (cols > INT32_MAX) return fail(ASR_EINVAL, "too many queries in a sequence");
+  const int64_t tile = 16 * paged_query_tiles((int)cols), tiles = (cols + tile - 1) / tile;
+  const int64_t units = (int64_t)a->cache.sequences * a->cache.kv_heads * tiles;
+  if (a->part_keys) {
+    s->part = a->part_keys;
+  } else {
+    const int fixed = (int)(200 + 10 * std::min<int64_t>(cols, 64)) * 2;
+    const bool ragged = a->cache.sequences > 1;
+    s->part = part_keys(std::max<int64_t>(units, 1), most, ragged, fixed, kPartStep);
+    if (ragged) s->part = part_keys_ragged(units, most, s->part, fixed, 20, kPartStep);
+    s->part = std::min(s->part, kMostPart);
+  }
+  s->parts = std::max(parts_of((int)most, s->part), 1);
+  const double blocks = ((double)units * s->parts + 8.0 * tiles);
+  // (a launch has fewer than 2^32 threads: 256 a block, 64 a row and head)
+  if (blocks >= 16777216.0 || (double)a->rows * a->n_head >= 67108864.0) return fail(ASR_EINVAL, "too much work for one call");
   s->q = a->q;
   s->q_ld = a->q_ld;
   s->out = a->out;
@@ -242,7 +262,7 @@ asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* byte
   s->rows = a->rows;
   s->max_rows = a->row_start ? a->max_rows : 1;
   s->max_keys = (int32_t)most;
-  *bytes = 0;
+  *bytes = s->parts > 1 ? kCounters * 4 + (size_t)a->rows * a->n_head * s->parts * (kHeadDim + 2) * 4 : 0;
   return ASR_OK;
 }
 
@@ -401,7 +421,8 @@ asr_status asr_attend_pages(const asr_paged_attention* a, void* ws, size_t ws_by
     st = check_ws(ws, ws_bytes, need);
     if (st != ASR_OK) return st;
     s.rec = need ? (float*)ws + kCounters : nullptr;
-    return launched(attend_pages(s, a->dtype == ASR_BF16, (hipStream_t)stream));
+    attend_pages(s, a->dtype == ASR_BF16, (hipStream_t)stream);
+    return launched(hipSuccess);
   });
 }
 
@@ -457,7 +478,8 @@ asr_status asr_sample(const asr_sampling* a, void* ws, size_t ws_bytes, void* st
     if (!a->u || !a->token) return fail(ASR_EINVAL, "NULL u or token");
     st = check_ws(ws, ws_bytes, need);
     if (st != ASR_OK) return st;
-    return launched(sample(s, a->dtype == ASR_BF16, (hipStream_t)stream));
+    sample(s, a->dtype == ASR_BF16, (hipStream_t)stream);
+    return launched(hipSuccess);
   });
 }
 
