@@ -310,7 +310,7 @@ struct SampleLaunch {
   float* logprob;
   int32_t* kept;
 };
-void sample(const SampleLaunch& a, bool bf16, hipStream_t s);
+hipError_t sample(const SampleLaunch& a, bool bf16, hipStream_t s);
 
 // What a decode step knows of its rows into the per-slot arrays that the rules
 // read: the token at the row's position, the history's length, the scalars of

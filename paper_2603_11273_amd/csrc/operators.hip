@@ -478,8 +478,7 @@ asr_status asr_sample(const asr_sampling* a, void* ws, size_t ws_bytes, void* st
     if (!a->u || !a->token) return fail(ASR_EINVAL, "NULL u or token");
     st = check_ws(ws, ws_bytes, need);
     if (st != ASR_OK) return st;
-    sample(s, a->dtype == ASR_BF16, (hipStream_t)stream);
-    return launched(hipSuccess);
+    return launched(sample(s, a->dtype == ASR_BF16, (hipStream_t)stream));
   });
 }
 
