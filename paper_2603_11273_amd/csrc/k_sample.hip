@@ -1,183 +1,266 @@
 // Tokens drawn from logits under temperature, top-k, top-p and min-p by given
 // random numbers (asr_sample).
 //
-// The kept tokens are a prefix of the falling order, so they are those above a cut:
-// a logit and, among the tokens that have it, how many of the first.  Nothing is
-// sorted.  A block of 1024 threads takes a row, which stays in its XCD's L2 between
-// passes:
+// The kept tokens are a prefix of the falling order, so they are those up to a cut: a
+// logit and, among the tokens that have it, the last that is kept.  Nothing is sorted.
+// A block of 1024 threads takes a row, each wave a sixteenth of it, which comes from L2
+// again at each pass:
 //   1. the largest logit M, and each thread's;
-//   2. a bin that the cut cannot lie behind: bins are the leading bits of M - l (32 to an
-//      octave), filled with counts for top-k (few wanted tokens: from the threads'
-//      largest alone) or with weights for top-p;
-//   3. the tokens up to that bin, in the order of tokens, into a list in LDS: the
-//      cuts by the digits of the list's logits, the draws by its sums.
-// Where the list would be longer than 4096 the cuts are found by digits over the row
-// again, and draws by sums of 64 lanes' tokens.
+//   2. a bin that the cut cannot lie behind: bins are the leading bits of M - l (256 to an
+//      octave), filled with counts for top-k (up to 768 wanted tokens: of the threads'
+//      largest alone) or, for top-p, with the float32 weights of the threads' largest and
+//      of every fourth or eighth other token.  The latter is a guess that 3. checks;
+//   3. the tokens up to that bin, in the order of tokens, into lists of the waves in LDS,
+//      and the weights of all; the cuts are found by finer bins of the lists, the draws
+//      by the lists' sums.
+// Where a wave's list would be longer than 512 tokens, counts or weights of the whole
+// row are filled into bins for each cut in turn, only the cut's own bin is listed, and
+// draws go by sums over 256 lanes' loads.
 //
 // Weights are whole numbers, so sums do not depend on an order: 2^(i / 512) from a table
-// times a polynomial, in 64 bits.
+// times a polynomial, in 64 bits.  The kernel is bound by its instructions: a weight
+// takes about 24 of them, a bin 7, against half a cycle a token for its bytes.
 #include "asr_device.h"
 
 namespace asr {
 namespace {
 
 constexpr int SM_NT = 1024, SM_NW = SM_NT / 64;
-constexpr int SM_BINS = 8192, SM_LIST = 4096, SM_TAB = 512;
-constexpr int SM_FEW = 768;              // wanted tokens that the threads' largest may bound
+constexpr int SM_BINS = 8192, SM_FINE = 2048, SM_TAB = 512;
+constexpr int SM_LIST = 512, SM_NARROW = 256;      // of a wave: all tokens up to a bin, those of one bin
+constexpr int SM_U = 4;                            // loads under way, and in a segment
+constexpr int SM_FEW = 768;                        // wanted tokens that the threads' largest may bound
+constexpr int SM_MEMBERS = 64;
+
+#define SM_INLINE __attribute__((always_inline))
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint16_t u16x8u __attribute__((ext_vector_type(8), aligned(2)));
 
-// A lane's tokens of one step: 16 bytes.
+// A lane's tokens of one load: 16 bytes.
 template <typename T>
 constexpr int kPer = 16 / sizeof(T);
 
+// A wave's part of a row: `steps` times 64 lanes' loads from token `first` on.
 template <typename T>
 struct RowOf {
   static constexpr int E = kPer<T>;
   const T* p;
-  int V;
-  // tokens base .. base + E - 1; -inf past the end
-  __device__ __forceinline__ void load(int base, float* x) const {
+  int V, steps, first;
+
+  __device__ __forceinline__ uint4 fetch(int base) const {
     if (base + E <= V) {
-      if constexpr (sizeof(T) == 4) {
-        const f32x4u a = *(const f32x4u*)(p + base);
+      if constexpr (sizeof(T) == 4)
+        return __builtin_bit_cast(uint4, *(const f32x4u*)(p + base));
+      else
+        return __builtin_bit_cast(uint4, *(const u16x8u*)(p + base));
+    }
+    uint4 u;                                               // -inf past the end
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = a[i] + 0.f;      // (zeros of either sign are one logit)
-      } else {
-        const u16x8u a = *(const u16x8u*)(p + base);
-#pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = bf2f(a[i]) + 0.f;
-      }
+      for (int i = 0; i < 4; ++i) ((float*)&u)[i] = base + i < V ? p[base + i] : -INFINITY;
     } else {
 #pragma unroll
-      for (int i = 0; i < E; ++i) x[i] = base + i < V ? St<T>::ld(p, base + i) + 0.f : -INFINITY;
+      for (int i = 0; i < 8; ++i) ((uint16_t*)&u)[i] = base + i < V ? p[base + i] : (uint16_t)0xff80u;
+    }
+    return u;
+  }
+  static __device__ __forceinline__ void floats(const uint4& u, float* x) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        x[i] = __uint_as_float(w[i]);
+      } else {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
     }
   }
-  // f(segment, first token, x) over the row; a segment is 64 lanes' tokens of a step
-  template <class F>
-  __device__ __forceinline__ void each(F&& f) const {
-    constexpr int U = sizeof(T) == 4 ? 4 : 2, STEP = SM_NT * E;
-    const int wave = threadIdx.x >> 6;
-    for (int b0 = 0; b0 < V; b0 += U * STEP) {
-      float x[U][E];
+  __device__ __forceinline__ int base(int step) const { return first + (step * 64 + (int)(threadIdx.x & 63)) * E; }
+  // f(first token, x) over the wave's part; after(segment) behind each SM_U steps
+  template <class F, class G>
+  __device__ SM_INLINE void each(F&& f, G&& after) const {
+#pragma unroll 1
+    for (int i = 0; i < steps; i += SM_U) {
+      uint4 u[SM_U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) load(b0 + u * STEP + (int)threadIdx.x * E, x[u]);
+      for (int j = 0; j < SM_U; ++j) u[j] = fetch(base(i + j));
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (b0 + u * STEP < V) f((b0 / STEP + u) * SM_NW + wave, b0 + u * STEP + (int)threadIdx.x * E, x[u]);
+      for (int j = 0; j < SM_U; ++j)
+        if (i + j < steps) {
+          float x[E];
+          floats(u[j], x);
+          f(base(i + j), x);
+        }
+      after((int)(threadIdx.x >> 6) * ((steps + SM_U - 1) / SM_U) + i / SM_U);
     }
+  }
+  template <class F>
+  __device__ SM_INLINE void each(F&& f) const {
+    each(f, [](int) SM_INLINE {});
+  }
+  __device__ __forceinline__ int segments() const { return SM_NW * ((steps + SM_U - 1) / SM_U); }
+  // the first token of a segment's step for this lane; steps of the segment
+  __device__ __forceinline__ int segment_steps(int seg) const {
+    return min(steps - seg % ((steps + SM_U - 1) / SM_U) * SM_U, SM_U);
+  }
+  __device__ __forceinline__ int segment_base(int seg, int step) const {
+    const int per = (steps + SM_U - 1) / SM_U;
+    return ((seg / per * steps + seg % per * SM_U + step) * 64 + (int)(threadIdx.x & 63)) * E;
   }
 };
 
-// e^{(l - M) / T} and its whole number of units of 2^-unit.
+// e^{(l - M) / T} in whole units of 2^-unit.
 struct Weights {
-  const double* tab;       // 2^(i / 512)
+  const double* tab;       // 2^(unit + i / 512)
   double top, c;           // 512 log2(e) / T
-  int unit;
-  __device__ __forceinline__ double scaled(float l, int by) const {
-    const double y = ((double)l - top) * c;
-    if (!(y > -512.0 * 1080)) return 0.0;                  // (nothing in 64 bits; -inf; 0 times -inf)
+  double least;            // of what weighs less than an eighth of a unit
+  __device__ __forceinline__ double place(float l) const { return ((double)l - top) * c; }
+  __device__ __forceinline__ uint64_t whole(float l) const {
+    const double y = fmax(place(l), least);                // (0 times -inf, too)
     constexpr double kMagic = 6755399441055744.0;          // 1.5 * 2^52: the nearest whole number is in the low bits
     const double t = y + kMagic;
     const int k = __double2loint(t);
     const double r = y - (t - kMagic);
     constexpr double a1 = 6.93147180559945286e-01 / 512, a2 = a1 * a1 / 2, a3 = a1 * a1 * a1 / 6;   // (the next term: 9e-15)
-    const double e = fma(fma(fma(a3, r, a2), r, a1), r, 1.0);
-    return ldexp(tab[k & (SM_TAB - 1)] * e, (k >> 9) + by);
-  }
-  __device__ __forceinline__ double value(float l) const { return scaled(l, 0); }
-  __device__ __forceinline__ uint64_t whole(float l) const {
-    return (uint64_t)__double_as_longlong(scaled(l, unit) + 4503599627370496.0) & 0xfffffffffffffull;   // + 2^52
+    const double e = tab[k & (SM_TAB - 1)];
+    const double v = fma(fma(fma(a3, r, a2), r, a1), r * e, e);
+    // times 2^(k / 512), in the exponent; 2^52 leaves the whole number in the low bits
+    const double z = __hiloint2double(__double2hiint(v) + (int)((uint32_t)(k & ~(SM_TAB - 1)) << 11), __double2loint(v));
+    return (uint64_t)__double_as_longlong(z + 4503599627370496.0) & 0xfffffffffffffull;
   }
 };
 
-// Tokens whose falling key is below `key`, and of those at it the first `ties`.
+// Kept: logits above `l`, and of those at it tokens up to `last`.
 struct Cut {
-  uint32_t key, ties;
+  float l;
+  int last;
+  __device__ __forceinline__ bool keeps(float x, int token) const { return x > l || (x == l && token <= last); }
 };
-__device__ __forceinline__ uint32_t falling(float l) { return ~ordered_u32(l); }
+// Rises as logits fall; zeros of either sign are one logit.
+__device__ __forceinline__ uint32_t falling(float l) { return ~ordered_u32(l + 0.f); }
 __device__ __forceinline__ float of_falling(uint32_t k) { return from_ordered_u32(~k); }
+
+// Bins of M - l: 0 below 2^-12, 256 to each octave, the last from 2^20 on.
+constexpr int SM_SHIFT = 15, SM_BIN0 = (127 - 12) << (23 - SM_SHIFT);
+static_assert(SM_BINS == 32 << (23 - SM_SHIFT), "32 octaves");
+__device__ __forceinline__ uint32_t depth(float top, float l) { return __float_as_uint(top - l); }
+__device__ __forceinline__ int bin_of(uint32_t depth) { return min(max((int)(depth >> SM_SHIFT) - SM_BIN0, 0), SM_BINS - 1); }
+__device__ __forceinline__ uint32_t bin_begin(int b) { return b <= 0 ? 0u : (uint32_t)(b + SM_BIN0) << SM_SHIFT; }
+__device__ __forceinline__ uint32_t bin_end(int b) { return b >= SM_BINS - 1 ? 0xffffffffu : (uint32_t)(b + 1 + SM_BIN0) << SM_SHIFT; }
 
 struct Lds {
   double tab[SM_TAB];
   union {
     uint64_t bins[SM_BINS];
     struct {
-      float logit[SM_LIST];
-      int32_t token[SM_LIST];
-      uint64_t digits[256];
+      float logit[SM_NW][SM_LIST];
+      int32_t token[SM_NW][SM_LIST];
     } list;
   };
-  uint64_t seg[kRulesMaxVocab / 256];
-  uint64_t sums[SM_NW];
-  uint64_t found_before, found_in;
-  uint32_t found;
-  float tops[SM_NW];
-  int32_t first, bad;
+  union {
+    uint32_t counts[SM_BINS];
+    uint64_t fine[SM_FINE];
+    uint64_t seg[SM_NT];
+  };
+  struct {
+    float logit[SM_NW][SM_NARROW];
+    int32_t token[SM_NW][SM_NARROW];
+  } narrow;
+  uint64_t sums[2][SM_NW];
+  uint64_t found_before, found_in, found_other;
+  uint32_t found, members;
+  float tops[SM_NW], lows[SM_NW];
+  float member_logit[SM_MEMBERS];
+  int32_t member_token[SM_MEMBERS];
+  int32_t first, bad, token;
 };
+static_assert(kRulesMaxVocab <= SM_NT * SM_U * 64 * 4, "a segment a thread");
 
-__device__ __forceinline__ uint64_t wave_add(uint64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor((unsigned long long)v, o, 64);
+// Inclusive sum over the lanes before (data-parallel moves: rows of 16, then their ends).
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
+#define SM_STEP(ctrl, rows)                                                                          \
+  do {                                                                                               \
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, ctrl, rows, 0xf, false);          \
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), ctrl, rows, 0xf, false);  \
+    v += (uint64_t)hi << 32 | lo;                                                                    \
+  } while (0)
+  SM_STEP(0x111, 0xf);                     // row_shr 1, 2, 4, 8
+  SM_STEP(0x112, 0xf);
+  SM_STEP(0x114, 0xf);
+  SM_STEP(0x118, 0xf);
+  SM_STEP(0x142, 0xa);                     // row_bcast 15 to rows 1 and 3, 31 to rows 2 and 3
+  SM_STEP(0x143, 0xc);
+#undef SM_STEP
   return v;
 }
-__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {    // inclusive
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+// Exclusive sums over the threads of two values; their sums over all in *va and *vb.
+__device__ __forceinline__ void block_scan2(uint64_t a, uint64_t b, Lds& s, uint64_t* before_a, uint64_t* va, uint64_t* before_b,
+                                            uint64_t* vb) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t x = wave_scan(a), y = wave_scan(b);
+  __syncthreads();
+  if (lane == 63) s.sums[0][wave] = x, s.sums[1][wave] = y;
+  __syncthreads();
+  uint64_t pa = 0, pb = 0, ta = 0, tb = 0;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t y = __shfl_up((unsigned long long)v, o, 64);
-    if (lane >= o) v += y;
+  for (int i = 0; i < SM_NW; ++i) {
+    const uint64_t u = s.sums[0][i], v = s.sums[1][i];
+    pa += i < wave ? u : 0;
+    pb += i < wave ? v : 0;
+    ta += u;
+    tb += v;
   }
-  return v;
+  *before_a = pa + x - a;
+  *before_b = pb + y - b;
+  *va = ta;
+  *vb = tb;
 }
-// Exclusive sum over the threads; the sum of all in *total.
-__device__ uint64_t block_scan(uint64_t v, Lds& s, uint64_t* total) {
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, Lds& s, uint64_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t x = wave_scan(v);
   __syncthreads();
-  if (lane == 63) s.sums[wave] = x;
+  if (lane == 63) s.sums[0][wave] = x;
   __syncthreads();
   uint64_t before = 0, all = 0;
 #pragma unroll
   for (int i = 0; i < SM_NW; ++i) {
-    const uint64_t y = s.sums[i];
+    const uint64_t y = s.sums[0][i];
     before += i < wave ? y : 0;
     all += y;
   }
   *total = all;
   return before + x - v;
 }
-__device__ uint64_t block_add(uint64_t v, Lds& s) {
-  const uint64_t x = wave_add(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s.sums[threadIdx.x >> 6] = x;
-  __syncthreads();
-  uint64_t all = 0;
-#pragma unroll
-  for (int i = 0; i < SM_NW; ++i) all += s.sums[i];
+__device__ __forceinline__ uint64_t block_add(uint64_t v, Lds& s) {
+  uint64_t all;
+  block_scan(v, s, &all);
   return all;
 }
 
-template <int N>
-__device__ __forceinline__ void clear_bins(uint64_t* bins) {
-  for (int i = threadIdx.x; i < N; i += SM_NT) bins[i] = 0;
-  __syncthreads();
+template <int BYTES>
+__device__ __forceinline__ void clear(void* p) {
+  static_assert(BYTES % (16 * SM_NT) == 0, "");
+#pragma unroll
+  for (int i = 0; i < BYTES / (16 * SM_NT); ++i) ((uint4*)p)[i * SM_NT + threadIdx.x] = uint4{0, 0, 0, 0};
 }
-// The bin at which the running sum reaches `goal`, what is before it and in it; false
-// where all bins sum to less.
-template <int N>
-__device__ bool find_bin(const uint64_t* bins, uint64_t goal, Lds& s, uint64_t* total) {
-  constexpr int P = (N + SM_NT - 1) / SM_NT;
+// The bin at which the running sum reaches goal(sum of all), into found, found_before and
+// found_in; the sum of all.  The bins are complete behind this function's first barrier.
+template <int N, class X, class G>
+__device__ __forceinline__ uint64_t find_bin(const X* bins, Lds& s, G&& goal_of) {
+  constexpr int P = N / SM_NT;
   const int b = threadIdx.x * P;
-  uint64_t x[P], sum = 0;
+  uint64_t x[P], sum = 0, total;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    x[i] = b + i < N ? bins[b + i] : 0;
-    sum += x[i];
-  }
-  uint64_t before = block_scan(sum, s, total);
+  for (int i = 0; i < P; ++i) sum += x[i] = bins[b + i];
+  uint64_t before = block_scan(sum, s, &total);
+  const uint64_t goal = goal_of(total);
   if (before < goal && goal <= before + sum) {
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -186,38 +269,129 @@ __device__ bool find_bin(const uint64_t* bins, uint64_t goal, Lds& s, uint64_t* 
     }
   }
   __syncthreads();
-  return goal <= *total;
+  return total;
 }
 
-// Leading bits of M - l, rising as logits fall.
-__device__ __forceinline__ int bin_of(float top, float l) { return (int)(__float_as_uint(top - l) >> 18); }
+// A wave's list, in the order of tokens.
+struct List {
+  const float* logit;
+  const int32_t* token;
+  int n;
+};
+
+// The last token, in falling order, of those listed and kept by `in` up to which their count or
+// their weights reach `goal` (at least 1, at most the whole).
+__device__ SM_INLINE Cut cut_list(const List& e, Cut in, bool by_count, uint64_t goal, const Weights& w, Lds& s) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float hi = -INFINITY, lo = INFINITY;
+  for (int i = lane; i < e.n; i += 64) {
+    const float x = e.logit[i];
+    if (in.keeps(x, e.token[i])) hi = fmaxf(hi, x), lo = fminf(lo, x);
+  }
+  hi = wave_max_lanes(hi);
+  lo = -wave_max_lanes(-lo);
+  __syncthreads();
+  clear<sizeof(s.fine)>(s.fine);
+  if (lane == 0) s.tops[wave] = hi, s.lows[wave] = lo;
+  if (threadIdx.x == 0) s.members = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < SM_NW; ++i) hi = fmaxf(hi, s.tops[i]), lo = fminf(lo, s.lows[i]);
+  // bins of one width over their range: most often the cut's holds a few tokens
+  const float range = hi - lo, by = range > 1e-30f && range < 1e30f ? (SM_FINE - 1) / range : 0.f;
+  auto bin = [&](float x) SM_INLINE { return min((int)((hi - x) * by), SM_FINE - 1); };
+  for (int i = lane; i < e.n; i += 64) {
+    const float x = e.logit[i];
+    if (in.keeps(x, e.token[i])) atomicAdd((unsigned long long*)&s.fine[bin(x)], by_count ? 1ull : (unsigned long long)w.whole(x));
+  }
+  find_bin<SM_FINE>(s.fine, s, [&](uint64_t) SM_INLINE { return goal; });
+  const int found = s.found;
+  uint64_t rest = goal - s.found_before;
+  for (int i = lane; i < e.n; i += 64) {
+    const float x = e.logit[i];
+    if (in.keeps(x, e.token[i]) && bin(x) == found) {
+      const uint32_t at = atomicAdd(&s.members, 1u);
+      if (at < SM_MEMBERS) s.member_logit[at] = x, s.member_token[at] = e.token[i];
+    }
+  }
+  __syncthreads();
+  const int m = s.members;
+  if (m <= SM_MEMBERS) {                   // (every wave for itself)
+    const float x = lane < m ? s.member_logit[lane] : -INFINITY;
+    const int token = lane < m ? s.member_token[lane] : INT32_MAX;
+    const uint64_t y = lane >= m ? 0 : by_count ? 1 : w.whole(x);
+    uint64_t before = 0;
+    for (int j = 0; j < m; ++j) {
+      const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), j));
+      const int t = __builtin_amdgcn_readlane(token, j);
+      before += o > x || (o == x && t < token) ? lane_value(y, j) : 0;
+    }
+    const int at = __ffsll((unsigned long long)__ballot(before < rest && rest <= before + y)) - 1;
+    return {__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at)), __builtin_amdgcn_readlane(token, at)};
+  }
+  // many in one bin (equal ones, as a rule): by the digits of their logits
+  uint32_t prefix = 0;
+#pragma unroll 1
+  for (int level = 0; level < 3; ++level) {
+    const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
+    __syncthreads();
+    clear<sizeof(s.fine)>(s.fine);
+    __syncthreads();
+    for (int i = lane; i < e.n; i += 64) {
+      const float x = e.logit[i];
+      const uint32_t k = falling(x);
+      if (in.keeps(x, e.token[i]) && bin(x) == found && (level == 0 || !((k ^ prefix) >> (shift + bits))))
+        atomicAdd((unsigned long long*)&s.fine[k >> shift & ((1 << bits) - 1)], by_count ? 1ull : (unsigned long long)w.whole(x));
+    }
+    find_bin<SM_FINE>(s.fine, s, [&](uint64_t) SM_INLINE { return rest; });
+    prefix |= s.found << shift;
+    rest -= s.found_before;
+  }
+  // the first of those at the cut's logit
+  const float l = of_falling(prefix);
+  const uint64_t each = by_count ? 1 : max(w.whole(l), (uint64_t)1), ties = (rest + each - 1) / each;
+  const int per = (e.n + 63) / 64, begin = min(lane * per, e.n), end = min(begin + per, e.n);
+  uint64_t n = 0, t;
+  for (int i = begin; i < end; ++i) n += e.logit[i] == l && in.keeps(l, e.token[i]);
+  uint64_t at = block_scan(n, s, &t);
+  for (int i = begin; i < end; ++i)
+    if (e.logit[i] == l && in.keeps(l, e.token[i]) && ++at == ties) s.token = e.token[i];
+  __syncthreads();
+  return {l, s.token};
+}
 
 template <typename T>
 __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   extern __shared__ __attribute__((aligned(16))) char sample_lds[];
   Lds& s = *(Lds*)sample_lds;
   constexpr int E = kPer<T>;
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const RowOf<T> x_of = {(const T*)a.logits + row * a.ld, a.vocab};
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  RowOf<T> r;
+  r.p = (const T*)a.logits + row * a.ld;
+  r.V = a.vocab;
+  r.steps = (a.vocab + SM_NT * E - 1) / (SM_NT * E);
+  r.first = wave * r.steps * 64 * E;
   const int set = a.set ? a.set[row] : row;
   const bool has = set >= 0 && set < a.sets;
   const float temperature = has && a.temperature ? a.temperature[set] : 1.f;
   const bool greedy = !(temperature > 0.f);
-  const int32_t top_k = has && a.top_k ? a.top_k[set] : 0;
-  const float top_p = has && a.top_p ? a.top_p[set] : 1.f, min_p_given = has && a.min_p ? a.min_p[set] : 0.f;
+  int32_t top_k = has && a.top_k ? a.top_k[set] : 0;
+  const float top_p = has && a.top_p ? a.top_p[set] : 1.f, min_p = has && a.min_p ? a.min_p[set] : 0.f;
 
   // the largest logit
+  if (tid < SM_TAB) s.tab[tid] = ldexp(exp2((double)tid / SM_TAB), unit);
+  if (tid == 0) s.bad = 0, s.first = INT32_MAX;
+  clear<sizeof(s.bins)>(s.bins);
+  clear<sizeof(s.counts)>(s.counts);
   float mine = -INFINITY;
   bool nan = false;
-  x_of.each([&](int, int, const float* x) {
+  r.each([&](int, const float* x) SM_INLINE {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      mine = fmaxf(mine, x[i]);
-      nan |= x[i] != x[i];
+    for (int i = 0; i < E; i += 2) {
+      mine = fmaxf(mine, fmaxf(x[i], x[i + 1]));
+      nan |= __builtin_isunordered(x[i], x[i + 1]);
     }
   });
-  for (int i = tid; i < SM_TAB; i += SM_NT) s.tab[i] = exp2((double)i / SM_TAB);
-  if (tid == 0) s.bad = 0, s.first = a.vocab;
   float top = wave_max_lanes(mine);
   if (lane == 0) s.tops[wave] = top;
   __syncthreads();
@@ -235,427 +409,383 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     if (tid == 0 && a.kept) a.kept[row] = 0;
     return;
   }
-  const Weights w = {s.tab, (double)top, 512.0 * 1.4426950408889634074 / (greedy ? 1.0 : (double)temperature), unit};
-  const double inv_unit = ldexp(1.0, -unit);
-  uint64_t all = 0;                        // of all weights
-  auto answer = [&](int d, int token, float l) {
+  constexpr double kScale = 512.0 * 1.4426950408889634074;
+  const Weights w = {s.tab, (double)top, kScale / (greedy ? 1.0 : (double)temperature), -512.0 * (unit + 3)};
+  uint64_t all = 0;                        // of all weights, once `have_all`
+  auto answer = [&](int d, int token, float l) SM_INLINE {
     token_out[d] = token;
-    if (logprob_out)
-      logprob_out[d] = (float)(((double)l - w.top) * (w.c / (512.0 * 1.4426950408889634074)) - log((double)all * inv_unit));
+    if (logprob_out) logprob_out[d] = (float)(w.place(l) / kScale - log(ldexp((double)all, -unit)));
+  };
+  auto goal_of = [&](int d, uint64_t mass) SM_INLINE {
+    const float u = a.u[(int64_t)row * a.draws + d];
+    return min((uint64_t)((u > 0.f ? fmin((double)u, 1.0 - 0x1p-24) : 0.0) * (double)mass), mass - 1);
   };
 
   if (greedy) {
-    int at = a.vocab;
-    x_of.each([&](int, int base, const float* x) {
+    int at = INT32_MAX;
+    r.each([&](int base, const float* x) SM_INLINE {
 #pragma unroll
       for (int i = E - 1; i >= 0; --i) {
-        all += w.whole(x[i]);
+        if (logprob_out) all += w.whole(x[i]);
         if (x[i] == top) at = min(at, base + i);
       }
     });
-    if (at < a.vocab) atomicMin(&s.first, at);
+    if (at < INT32_MAX) atomicMin(&s.first, at);
     all = block_add(all, s);
     if (tid < a.draws) answer(tid, s.first, top);
     if (tid == 0 && a.kept) a.kept[row] = 1;
     return;
   }
-  const double min_p = min_p_given > 0.f ? (double)min_p_given : 0.0;
+  if (min_p > 1.f) top_k = 1;              // (the first is kept all the same)
   bool k_on = top_k > 0 && top_k < a.vocab;
   const bool p_on = top_p < 1.f;
-  auto p_goal = [&](uint64_t mass) {       // the least whole sum that is not below top_p of the mass
+  auto p_goal = [&](uint64_t mass) SM_INLINE {       // the least whole sum that is not below top_p of the mass
     const double part = (double)top_p * (double)mass;
     return part > 0.0 ? max((uint64_t)ceil(part), (uint64_t)1) : (uint64_t)1;
   };
-
-  // a bin that the cut is not behind
-  int last = -1;
-  uint64_t before = 0, total;
-  bool have_all = false, exact_bin = false;
-  if (k_on && top_k <= SM_FEW) {
-    clear_bins<SM_BINS>(s.bins);
-    if (mine > -INFINITY) atomicAdd((unsigned long long*)&s.bins[bin_of(top, mine)], 1ull);
-    if (find_bin<SM_BINS>(s.bins, top_k, s, &total)) last = s.found;
+  auto k_goal = [&](uint64_t) SM_INLINE { return (uint64_t)top_k; };
+  Cut cut = {-INFINITY, -1};
+  // min-p as a cut: the least logit whose weight is at least min_p
+  Cut least = cut;
+  if (min_p > 0.f && min_p <= 1.f) {
+    const double bound = 512.0 * log2((double)min_p);
+    auto passes = [&](uint32_t k) SM_INLINE { return w.place(of_falling(k)) >= bound; };
+    const uint32_t first = falling(top), end = falling(-INFINITY);
+    const uint32_t near = falling((float)fmax(fmin(w.top + bound / w.c, w.top), -3e38));
+    uint32_t in = near - first < 16 ? first : near - 16, out = end - near < 16 ? end : near + 16;   // (keys, falling logits)
+    if (!passes(in)) in = first;
+    if (passes(out)) out = end;
+    while (out - in > 1) {
+      const uint32_t mid = in + (out - in) / 2;
+      if (passes(mid)) in = mid; else out = mid;
+    }
+    least = {of_falling(in), INT32_MAX};
   }
-  auto count_bins = [&] {
-    __syncthreads();
-    clear_bins<SM_BINS>(s.bins);
-    x_of.each([&](int, int, const float* x) {
+  auto tighter = [&](Cut x) SM_INLINE { return least.l > x.l ? least : x; };
+
+  // ---- a bin that the cut is not behind: `last`; tokens before it
+  int last = -1;
+  uint64_t before = 0;
+  bool counted = false, have_all = false;
+  auto count_bins = [&]() SM_INLINE {                // the bin of top-k's cut; false where there are no more tokens than that
+    r.each([&](int, const float* x) SM_INLINE {
 #pragma unroll
       for (int i = 0; i < E; ++i)
-        if (x[i] > -INFINITY) atomicAdd((unsigned long long*)&s.bins[bin_of(top, x[i])], 1ull);
+        if (x[i] > -INFINITY) atomicAdd(&s.counts[bin_of(depth(top, x[i]))], 1u);
     });
-    if (find_bin<SM_BINS>(s.bins, top_k, s, &total) && (uint64_t)top_k < total) {
-      last = s.found, before = s.found_before, exact_bin = true;
-    } else {
-      k_on = false, last = -1;
-    }
+    counted = true;
+    if (find_bin<SM_BINS>(s.counts, s, k_goal) <= (uint64_t)top_k) return false;
+    last = s.found, before = s.found_before;
+    return true;
   };
-  if (k_on && last < 0) count_bins();
-  if (!k_on && p_on) {
-    // what weighs less than (1 - p) / V cannot be where the sum passes p of it: those
-    // tokens sum to less than 1 - p of the largest weight alone
-    const uint64_t least = (uint64_t)((1.0 - (double)top_p) / a.vocab * ldexp(1.0, unit));
-    __syncthreads();
-    clear_bins<SM_BINS>(s.bins);
-    uint64_t rest = 0;
-    x_of.each([&](int, int, const float* x) {
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const uint64_t y = w.whole(x[i]);
-        if (y > least)
-          atomicAdd((unsigned long long*)&s.bins[bin_of(top, x[i])], (unsigned long long)y);
-        else
-          rest += y;
+  bool few = true;                         // the tokens up to it may fit the lists
+  if (r.steps * 64 * E <= SM_LIST) {
+    last = SM_BINS - 1;
+  } else if (k_on) {
+    if (top_k <= SM_FEW) {
+      if (mine > -INFINITY) atomicAdd(&s.counts[bin_of(depth(top, mine))], 1u);
+      if (find_bin<SM_BINS>(s.counts, s, k_goal) >= (uint64_t)top_k) {
+        last = s.found;
+      } else {
+        clear<sizeof(s.counts)>(s.counts);
+        __syncthreads();
       }
+    }
+    if (last < 0) {
+      k_on = count_bins();
+      few = k_on && before + s.found_in <= SM_NW * SM_LIST * 3 / 4;
+    }
+  }
+  if (last < 0 && p_on) {
+    // counts above 43 bits of weights, in units of 2^-22
+    constexpr uint64_t kOne = 1ull << 43;
+    const float c = (float)fmin(w.c / 512.0, 3e38);
+    auto note = [&](float x, int times) SM_INLINE {
+      const uint32_t n = (uint32_t)(__builtin_amdgcn_exp2f((x - top) * c) * 0x1p22f + 0.5f);
+      if (n) atomicAdd((unsigned long long*)&s.bins[bin_of(depth(top, x))], (unsigned long long)((kOne + n) * times));
+    };
+    if (mine > -INFINITY) note(mine, 1);
+    r.each([&](int, const float* x) SM_INLINE {
+      if (x[0] != mine && x[0] > -INFINITY) note(x[0], E);
     });
-    all = block_add(rest, s);
-    find_bin<SM_BINS>(s.bins, 0, s, &total);
-    all += total;
-    have_all = true;
-    find_bin<SM_BINS>(s.bins, min(p_goal(all), total), s, &total);
-    last = s.found, before = s.found_before, exact_bin = true;
+    __syncthreads();
+    constexpr int P = SM_BINS / SM_NT;
+    uint64_t x[P], weights = 0, n = 0, w_before, n_before, w_all, n_all;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      x[i] = s.bins[tid * P + i];
+      weights += x[i] & (kOne - 1);
+      n += x[i] >> 43;
+    }
+    if (tid == 0) s.found = SM_BINS - 1, s.found_other = ~0ull;
+    block_scan2(weights, n, s, &w_before, &w_all, &n_before, &n_all);
+    const uint64_t goal = (uint64_t)((double)w_all * fmax(0.2 + 0.8 * (double)top_p, 0.2));
+    if (w_before < goal && goal <= w_before + weights) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const uint64_t y = x[i] & (kOne - 1);
+        n_before += x[i] >> 43;
+        if (w_before < goal && goal <= w_before + y) s.found = tid * P + i, s.found_other = n_before;
+        w_before += y;
+      }
+    }
+    __syncthreads();
+    last = s.found;
+    few = s.found_other <= SM_NW * SM_LIST * 3 / 4;
+  } else if (last < 0 && least.l > -INFINITY) {
+    last = bin_of(depth(top, least.l));
   }
 
-  const int segments = (a.vocab + 64 * E - 1) / (64 * E), rounded = (segments + SM_NW - 1) / SM_NW * SM_NW;
-  uint64_t listed = SM_LIST + 1;
-  if (last >= 0) {
+  // The tokens of bins `from` to `to` that `cut` keeps into the waves' lists of `room`; whether
+  // they fit.  f(token, bin's depth) besides.
+  List e;
+  uint64_t listed_all;
+  auto list_bins = [&](int from, int to, float* logit, int32_t* token, int room, bool sum_all) SM_INLINE {
+    const uint32_t lo = bin_begin(from), width = bin_end(to) - lo;
+    int n = 0;
     uint64_t sum = 0;
     __syncthreads();
-    x_of.each([&](int seg, int, const float* x) {
-      int n = 0;
+    r.each([&](int base, const float* x) SM_INLINE {
+      uint64_t is[E], any = 0;
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        n += __popcll(__ballot(bin_of(top, x[i]) <= last && x[i] > -INFINITY));
-        if (!have_all) sum += w.whole(x[i]);
-      }
-      if (lane == 0) s.seg[seg] = n;
-    });
-    if (!have_all) all = block_add(sum, s), have_all = true;
-    __syncthreads();
-    uint64_t n[4], mine4 = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      n[i] = 4 * tid + i < rounded ? s.seg[4 * tid + i] : 0;
-      mine4 += n[i];
-    }
-    uint64_t at = block_scan(mine4, s, &listed);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (4 * tid + i < rounded) s.seg[4 * tid + i] = at;
-      at += n[i];
-    }
-    __syncthreads();
-  }
-
-  if (listed <= SM_LIST) {
-    const int count = (int)listed;
-    x_of.each([&](int seg, int base, const float* x) {
-      bool in[E];
-      int at = (int)s.seg[seg];
-      uint64_t any = 0;
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        in[i] = bin_of(top, x[i]) <= last && x[i] > -INFINITY;
-        const uint64_t is = __ballot(in[i]);
-        at += __popcll(is & ((1ull << lane) - 1));
-        any |= is;
+        is[i] = __ballot(depth(top, x[i]) - lo < width);
+        any |= is[i];
+        if (sum_all) sum += w.whole(x[i]);
       }
       if (any) {
+        bool in[E];
+        uint32_t at = n;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          in[i] = (is[i] >> lane & 1) && cut.keeps(x[i], base + i);
+          is[i] = __ballot(in[i]);
+          at = __builtin_amdgcn_mbcnt_hi((uint32_t)(is[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)is[i], at));
+          n += __popcll(is[i]);
+        }
 #pragma unroll
         for (int i = 0; i < E; ++i)
           if (in[i]) {
-            s.list.logit[at] = x[i];
-            s.list.token[at] = base + i;
+            if (at < (uint32_t)room) logit[at] = x[i], token[at] = base + i;
             ++at;
           }
       }
     });
-    __syncthreads();
-    constexpr int L = SM_LIST / SM_NT;
-    float x[L];
-    uint32_t key[L];
-    uint64_t y[L];
-    const uint32_t best = falling(top);
-    uint32_t widest = 0;
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const int at = L * tid + i;
-      const bool in = at < count;
-      x[i] = in ? s.list.logit[at] : -INFINITY;
-      y[i] = in ? w.whole(x[i]) : 0;
-      key[i] = in ? falling(x[i]) - best : 0xffffffffu;
-      if (in) widest = max(widest, key[i]);
-    }
-    widest = wave_max_u32(widest);
-    if (lane == 0) s.tops[wave] = __uint_as_float(widest);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < SM_NW; ++i) widest = max(widest, __float_as_uint(s.tops[i]));
-    const int digits = widest ? (39 - __clz(widest)) / 8 : 1;
+    e = {logit, token, n};
+    uint64_t t0, sum_of, over;
+    block_scan2(sum, lane == 0 ? (n > room ? 1ull << 32 : 0) + (uint64_t)n : 0, s, &t0, &sum_of, &t0, &over);
+    if (sum_all) all = sum_of, have_all = true;
+    listed_all = over & 0xffffffffu;
+    return over >> 32 == 0;
+  };
 
-    bool kept[L];
-#pragma unroll
-    for (int i = 0; i < L; ++i) kept[i] = L * tid + i < count;
-    // keeps what is before the cut at `goal` of counts or weights of what is kept now
-    auto cut_list = [&](bool by_count, uint64_t goal) {
-      uint32_t prefix = 0;
-      uint64_t sum = 0;
-      for (int d = digits - 1; d >= 0; --d) {
-        for (int i = tid; i < 256; i += SM_NT) s.list.digits[i] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < L; ++i)
-          if (kept[i] && (d == 3 || key[i] >> (8 * d + 8) == prefix >> (8 * d + 8)))
-            atomicAdd((unsigned long long*)&s.list.digits[key[i] >> (8 * d) & 255], by_count ? 1ull : (unsigned long long)y[i]);
-        uint64_t t;
-        find_bin<256>(s.list.digits, goal - sum, s, &t);
-        prefix |= s.found << (8 * d);
-        sum += s.found_before;
-        __syncthreads();
-      }
-      // the first of those at the cut's logit
-      const uint64_t each = by_count ? 1 : max(w.whole(of_falling(prefix + best)), (uint64_t)1);
-      const uint64_t ties = (goal - sum + each - 1) / each;
-      uint64_t at = 0, t;
-#pragma unroll
-      for (int i = 0; i < L; ++i) at += kept[i] && key[i] == prefix;
-      at = block_scan(at, s, &t);
-#pragma unroll
-      for (int i = 0; i < L; ++i) {
-        if (kept[i] && key[i] == prefix) {
-          kept[i] = at < ties;
-          ++at;
-        } else {
-          kept[i] = kept[i] && key[i] < prefix;
-        }
-      }
-    };
-    if (k_on) cut_list(true, top_k);
+  if (last >= 0 && few && list_bins(0, last, s.list.logit[wave], s.list.token[wave], SM_LIST, logprob_out || (p_on && !k_on))) {
+    const int per = (e.n + 63) / 64, begin = min(lane * per, e.n), end = min(begin + per, e.n);
+    bool fine = true;
+    if (k_on && listed_all > (uint64_t)top_k) cut = cut_list(e, cut, true, top_k, w, s);
     if (p_on) {
-      uint64_t mass = all;
-      if (k_on) {
-        mass = 0;
-#pragma unroll
-        for (int i = 0; i < L; ++i) mass += kept[i] ? y[i] : 0;
-        mass = block_add(mass, s);
-      }
-      cut_list(false, p_goal(mass));
+      uint64_t mass = 0;
+      for (int i = begin; i < end; ++i) mass += cut.keeps(e.logit[i], e.token[i]) ? w.whole(e.logit[i]) : 0;
+      mass = block_add(mass, s);
+      const uint64_t goal = p_goal(k_on ? mass : all);
+      fine = goal <= mass;                 // the guess was far enough
+      if (fine) cut = cut_list(e, cut, false, goal, w, s);
     }
-    if (min_p > 0.0) {
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (kept[i] && key[i] == 0) atomicMin(&s.first, L * tid + i);
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < L; ++i) kept[i] = kept[i] && (L * tid + i == s.first || w.value(x[i]) >= min_p);
-    }
-    uint64_t sum = 0, mass, n = 0;
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      if (!kept[i]) y[i] = 0;
-      sum += y[i];
-      n += kept[i];
-    }
-    n = block_add(n, s);
-    if (tid == 0 && a.kept) a.kept[row] = (int32_t)n;
-    const uint64_t from = block_scan(sum, s, &mass);
-    for (int d = 0; d < a.draws; ++d) {
-      const float u = a.u[(int64_t)row * a.draws + d];
-      const uint64_t goal = min((uint64_t)((u > 0.f ? fmin((double)u, 1.0 - 0x1p-24) : 0.0) * (double)mass), mass - 1);
-      if (from <= goal && goal < from + sum) {
+    if (fine) {
+      cut = tighter(cut);
+      uint64_t sum = 0, n = 0, mass, from, n_before, n_all;
+      for (int i = begin; i < end; ++i)
+        if (cut.keeps(e.logit[i], e.token[i])) sum += w.whole(e.logit[i]), ++n;
+      block_scan2(sum, n, s, &from, &mass, &n_before, &n_all);
+      if (tid == 0 && a.kept) a.kept[row] = (int32_t)n_all;
+      for (int d = 0; d < a.draws; ++d) {
+        const uint64_t goal = goal_of(d, mass);
+        if (goal < from || goal >= from + sum) continue;
         uint64_t c = from;
-#pragma unroll
-        for (int i = 0; i < L; ++i) {
-          if (c <= goal && goal < c + y[i]) answer(d, s.list.token[L * tid + i], x[i]);
-          c += y[i];
+        for (int i = begin; i < end; ++i) {
+          const float l = e.logit[i];
+          const uint64_t y = cut.keeps(l, e.token[i]) ? w.whole(l) : 0;
+          if (c <= goal && goal < c + y) answer(d, e.token[i], l);
+          c += y;
         }
       }
+      return;
     }
-    return;
   }
 
-  // ---- many tokens: cuts by digits over the row
-  Cut cut = {falling(-INFINITY), 0};
-  bool tied = false;                       // only some of the tokens at the cut's logit
-  // the cut at which the counts or weights of what `cut` leaves, before + those of
-  // bin `last`, reach goal
-  auto cut_row = [&](bool by_count, uint64_t goal) {
+  // ---- many tokens: each cut's bin, then its list
+  auto narrow = [&](bool sum_all) SM_INLINE {
+    return list_bins(last, last, s.narrow.logit[wave], s.narrow.token[wave], SM_NARROW, sum_all);
+  };
+  // (a bin too full for the lists: digits over the row)
+  auto cut_row = [&](bool by_count, uint64_t rest) SM_INLINE {
     const Cut in = cut;
+    const uint32_t lo = bin_begin(last), width = bin_end(last) - lo;
     uint32_t prefix = 0;
-    uint64_t sum = before, here = 0;
 #pragma unroll 1
     for (int level = 0; level < 3; ++level) {
       const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
       __syncthreads();
-      clear_bins<2048>(s.bins);
-      x_of.each([&](int, int, const float* x) {
+      clear<sizeof(s.fine)>(s.fine);
+      __syncthreads();
+      r.each([&](int base, const float* x) SM_INLINE {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           const uint32_t k = falling(x[i]);
-          if (bin_of(top, x[i]) != last || !(x[i] > -INFINITY) || (level > 0 && (k ^ prefix) >> (shift + bits))) continue;
-          if (by_count)
-            atomicAdd((unsigned long long*)&s.bins[k >> shift & ((1 << bits) - 1)], 1ull);
-          else if (k < in.key)
-            atomicAdd((unsigned long long*)&s.bins[k >> shift & ((1 << bits) - 1)], (unsigned long long)w.whole(x[i]));
+          if (depth(top, x[i]) - lo < width && in.keeps(x[i], base + i) && (level == 0 || !((k ^ prefix) >> (shift + bits))))
+            atomicAdd((unsigned long long*)&s.fine[k >> shift & ((1 << bits) - 1)], by_count ? 1ull : (unsigned long long)w.whole(x[i]));
         }
       });
-      __syncthreads();
-      const float l = of_falling(in.key);
-      if (!by_count && in.ties && tid == 0 && bin_of(top, l) == last && !(level > 0 && (in.key ^ prefix) >> (shift + bits)))
-        s.bins[in.key >> shift & ((1 << bits) - 1)] += in.ties * w.whole(l);
-      uint64_t t;
-      find_bin<2048>(s.bins, goal - sum, s, &t);
+      find_bin<SM_FINE>(s.fine, s, [&](uint64_t) SM_INLINE { return rest; });
       prefix |= s.found << shift;
-      sum += s.found_before;
-      here = s.found_in;
+      rest -= s.found_before;
     }
-    const uint64_t each = by_count ? 1 : max(w.whole(of_falling(prefix)), (uint64_t)1);
-    const uint64_t ties = (goal - sum + each - 1) / each;
-    tied = ties * each < here || (prefix == in.key && tied);
-    cut = {prefix, (uint32_t)ties};
-  };
-  if (k_on) {
-    if (!exact_bin) count_bins();
-    if (k_on) cut_row(true, top_k);
-  }
-  if (p_on) {
-    if (k_on) {
-      // weights of what top-k leaves
-      __syncthreads();
-      clear_bins<SM_BINS>(s.bins);
-      x_of.each([&](int, int, const float* x) {
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-          if (falling(x[i]) < cut.key) atomicAdd((unsigned long long*)&s.bins[bin_of(top, x[i])], (unsigned long long)w.whole(x[i]));
-      });
-      __syncthreads();
-      const float l = of_falling(cut.key);
-      if (tid == 0) s.bins[bin_of(top, l)] += cut.ties * w.whole(l);
-      find_bin<SM_BINS>(s.bins, 0, s, &total);
-      find_bin<SM_BINS>(s.bins, p_goal(total), s, &total);
-      last = s.found, before = s.found_before;
-      cut_row(false, p_goal(total));
-    } else {
-      cut_row(false, min(p_goal(all), total));
-    }
-  }
-  // the last token at the cut's logit that is kept
-  int last_tie = cut.ties ? a.vocab : -1;
-  if (tied) {
+    const float l = of_falling(prefix);
+    const uint64_t each = by_count ? 1 : max(w.whole(l), (uint64_t)1), ties = (rest + each - 1) / each;
+    // the last of the kept ones at the cut's logit: its segment, then its step
     __syncthreads();
-    x_of.each([&](int seg, int, const float* x) {
-      int n = 0;
+    uint64_t n = 0, t;
+    r.each(
+        [&](int base, const float* x) SM_INLINE {
 #pragma unroll
-      for (int i = 0; i < E; ++i) n += __popcll(__ballot(falling(x[i]) == cut.key));
-      if (lane == 0) s.seg[seg] = n;
-    });
+          for (int i = 0; i < E; ++i) n += __popcll(__ballot(x[i] == l && in.keeps(l, base + i)));
+        },
+        [&](int seg) SM_INLINE {
+          if (lane == 0) s.seg[seg] = n;
+          n = 0;
+        });
     __syncthreads();
-    uint64_t n[4], mine4 = 0, t;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      n[i] = 4 * tid + i < rounded ? s.seg[4 * tid + i] : 0;
-      mine4 += n[i];
-    }
-    uint64_t at = block_scan(mine4, s, &t);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (at < cut.ties && cut.ties <= at + n[i]) s.found = 4 * tid + i, s.found_before = at;
-      at += n[i];
-    }
+    const uint64_t own = tid < r.segments() ? s.seg[tid] : 0, at = block_scan(own, s, &t);
+    if (at < ties && ties <= at + own) s.found = tid, s.found_before = at;
     __syncthreads();
     if (wave == 0) {
-      float x[E];
-      const int base = (int)s.found * 64 * E + lane * E;
-      x_of.load(base, x);
-      uint32_t c = (uint32_t)s.found_before;
+      uint64_t c = s.found_before;
+      const int steps = r.segment_steps(s.found);
+      for (int j = 0; j < steps; ++j) {
+        float x[E];
+        const int base = r.segment_base(s.found, j);
+        r.floats(r.fetch(base), x);
+        uint32_t mine_at = 0, of_step = 0;
 #pragma unroll
-      for (int i = 0; i < E; ++i) c += __popcll(__ballot(falling(x[i]) == cut.key) & ((1ull << lane) - 1));
+        for (int i = 0; i < E; ++i) {
+          const uint64_t is = __ballot(x[i] == l && in.keeps(l, base + i));
+          mine_at = __builtin_amdgcn_mbcnt_hi((uint32_t)(is >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)is, mine_at));
+          of_step += __popcll(is);
+        }
 #pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (falling(x[i]) == cut.key && ++c == cut.ties) s.first = base + i;
+        for (int i = 0; i < E; ++i)
+          if (x[i] == l && in.keeps(l, base + i) && c + ++mine_at == ties) s.token = base + i;
+        c += of_step;
+      }
     }
     __syncthreads();
-    last_tie = s.first;
-    __syncthreads();
-    if (tid == 0) s.first = a.vocab;
-  }
-  if (min_p > 0.0) {
-    int at = a.vocab;
-    __syncthreads();
-    x_of.each([&](int, int base, const float* x) {
-#pragma unroll
-      for (int i = E - 1; i >= 0; --i)
-        if (x[i] == top) at = min(at, base + i);
-    });
-    if (at < a.vocab) atomicMin(&s.first, at);
-    __syncthreads();
-  }
-  const int first_best = s.first;
-  const bool bare = !k_on && !p_on;
-  auto keeps = [&](float l, int token) {
-    if (!(l > -INFINITY)) return false;
-    const uint32_t k = falling(l);
-    if (!bare && (k > cut.key || (k == cut.key && token > last_tie))) return false;
-    return !(min_p > 0.0) || token == first_best || w.value(l) >= min_p;
+    return Cut{l, s.token};
   };
-  uint64_t sum = 0, n = 0;
-  __syncthreads();
-  x_of.each([&](int seg, int base, const float* x) {
-    uint64_t part = 0;
-    bool some = false;
+  // weights of what `cut` keeps of bins `from` to `to` into the bins; those of all
+  auto weigh = [&](int from, int to, bool sum_all) SM_INLINE {
+    const uint32_t lo = bin_begin(from), width = bin_end(to) - lo;
+    uint64_t sum = 0;
+    r.each([&](int base, const float* x) SM_INLINE {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const bool in = keeps(x[i], base + i);
-      some |= in;
-      n += in;
-      const uint64_t y = !have_all || in ? w.whole(x[i]) : 0;
-      sum += y;
-      part += in ? y : 0;
+      for (int i = 0; i < E; ++i) {
+        const uint32_t at = depth(top, x[i]);
+        const bool in = at - lo < width && cut.keeps(x[i], base + i);
+        if (!sum_all && !__any(in)) continue;
+        const uint64_t y = w.whole(x[i]);
+        if (sum_all) sum += y;
+        if (in && y) atomicAdd((unsigned long long*)&s.bins[bin_of(at)], (unsigned long long)y);
+      }
+    });
+    if (sum_all) all = block_add(sum, s), have_all = true;
+  };
+  if (k_on || p_on) {
+    __syncthreads();
+    clear<sizeof(s.bins)>(s.bins);
+    if (k_on && !counted) {
+      clear<sizeof(s.counts)>(s.counts);
+      __syncthreads();
+      k_on = count_bins();
     }
-    part = __any(some) ? wave_add(part) : 0;
-    if (lane == 0) s.seg[seg] = part;
-  });
-  if (!have_all) all = block_add(sum, s);
-  n = block_add(n, s);
-  if (tid == 0 && a.kept) a.kept[row] = (int32_t)n;
+    __syncthreads();
+  }
+  if (k_on) {
+    const int bin = last;
+    const bool fits = narrow(false);
+    cut = fits ? cut_list(e, cut, true, top_k - before, w, s) : cut_row(true, top_k - before);
+    if (p_on) weigh(0, bin, logprob_out && !have_all);
+  } else if (p_on) {
+    weigh(0, SM_BINS - 1, !have_all);
+  }
+  if (p_on) {
+    uint64_t goal = 0;
+    find_bin<SM_BINS>(s.bins, s, [&](uint64_t mass) SM_INLINE { return goal = p_goal(mass); });
+    last = s.found, before = s.found_before;
+    const bool fits = narrow(false);
+    cut = fits ? cut_list(e, cut, false, goal - before, w, s) : cut_row(false, goal - before);
+  }
+  cut = tighter(cut);
+  uint64_t sum = 0, n = 0, part = 0;
+  const bool sum_all = logprob_out && !have_all;
   __syncthreads();
-  uint64_t y[4], mine4 = 0, mass;
+  r.each(
+      [&](int base, const float* x) SM_INLINE {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[i] = 4 * tid + i < rounded ? s.seg[4 * tid + i] : 0;
-    mine4 += y[i];
-  }
-  uint64_t at = block_scan(mine4, s, &mass);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    at += y[i];
-    if (4 * tid + i < rounded) s.seg[4 * tid + i] = at;        // up to and with it
-  }
+        for (int i = 0; i < E; ++i) {
+          const bool in = cut.keeps(x[i], base + i);
+          if (!sum_all && !__any(in)) continue;
+          const uint64_t y = w.whole(x[i]);
+          n += in;
+          sum += y;
+          part += in ? y : 0;
+        }
+      },
+      [&](int seg) SM_INLINE {
+        if (__any(part != 0)) part = lane_value(wave_scan(part), 63);
+        if (lane == 0) s.seg[seg] = part;
+        part = 0;
+      });
+  uint64_t t0, t1, n_all, mass;
+  block_scan2(sum, n, s, &t0, &t1, &t0, &n_all);
+  if (sum_all) all = t1;
+  if (tid == 0 && a.kept) a.kept[row] = (int32_t)n_all;
+  const int segments = r.segments();
+  const uint64_t own = tid < segments ? s.seg[tid] : 0, upto = block_scan(own, s, &mass) + own;
+  if (tid < segments) s.seg[tid] = upto;
   __syncthreads();
   for (int d = wave; d < a.draws; d += SM_NW) {
-    const float u = a.u[(int64_t)row * a.draws + d];
-    const uint64_t goal = min((uint64_t)((u > 0.f ? fmin((double)u, 1.0 - 0x1p-24) : 0.0) * (double)mass), mass - 1);
-    int lo = 0, hi = rounded - 1;                              // the first segment whose sum is above goal
+    const uint64_t goal = goal_of(d, mass);
+    int lo = 0, hi = segments - 1;                             // the first segment whose sum is above goal
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (s.seg[mid] > goal) hi = mid; else lo = mid + 1;
     }
-    float x[E];
-    uint64_t z[E], own = 0;
-    const int base = lo * 64 * E + lane * E;
-    x_of.load(base, x);
+    uint64_t c = lo ? s.seg[lo - 1] : 0;
+    const int steps = r.segment_steps(lo);
+    for (int j = 0; j < steps; ++j) {
+      float x[E];
+      uint64_t z[E], of_lane = 0;
+      const int base = r.segment_base(lo, j);
+      r.floats(r.fetch(base), x);
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      z[i] = keeps(x[i], base + i) ? w.whole(x[i]) : 0;
-      own += z[i];
-    }
-    uint64_t c = (lo ? s.seg[lo - 1] : 0) + wave_scan(own) - own;
+      for (int i = 0; i < E; ++i) of_lane += z[i] = cut.keeps(x[i], base + i) ? w.whole(x[i]) : 0;
+      const uint64_t scanned = wave_scan(of_lane);
+      uint64_t at = c + scanned - of_lane;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      if (c <= goal && goal < c + z[i]) answer(d, base + i, x[i]);
-      c += z[i];
+      for (int i = 0; i < E; ++i) {
+        if (at <= goal && goal < at + z[i]) answer(d, base + i, x[i]);
+        at += z[i];
+      }
+      c += lane_value(scanned, 63);
     }
   }
+}
+
+template <typename T>
+hipError_t launch(const SampleLaunch& a, int unit, hipStream_t s) {
+  const hipError_t e = hipFuncSetAttribute((const void*)k_sample<T>, hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(Lds));
+  if (e != hipSuccess) return e;
+  k_sample<T><<<dim3((unsigned)a.rows), SM_NT, sizeof(Lds), s>>>(a, unit);
+  return hipSuccess;
 }
 
 }  // namespace
@@ -664,14 +794,7 @@ hipError_t sample(const SampleLaunch& a, bool bf16, hipStream_t s) {
   int log2 = 0;
   while ((1 << log2) < a.vocab) ++log2;
   const int unit = log2 < 12 ? 50 : 62 - log2;
-  const void* k = bf16 ? (const void*)k_sample<bf16_t> : (const void*)k_sample<float>;
-  const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(Lds));
-  if (e != hipSuccess) return e;
-  if (bf16)
-    k_sample<bf16_t><<<dim3((unsigned)a.rows), SM_NT, sizeof(Lds), s>>>(a, unit);
-  else
-    k_sample<float><<<dim3((unsigned)a.rows), SM_NT, sizeof(Lds), s>>>(a, unit);
-  return hipSuccess;
+  return bf16 ? launch<bf16_t>(a, unit, s) : launch<float>(a, unit, s);
 }
 
 }  // namespace asr
