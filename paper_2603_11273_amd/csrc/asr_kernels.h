@@ -293,7 +293,7 @@ struct TablesLaunch {
   int32_t* ws;                                    // tables_ws_words
 };
 int64_t tables_ws_words(int sequences, int columns, int pages);
-void next_tables(const TablesLaunch& a, hipStream_t s);
+hipError_t next_tables(const TablesLaunch& a, hipStream_t s);
 
 // Tokens drawn from logits (asr_sample).
 constexpr int kSampleMaxDraws = 64;

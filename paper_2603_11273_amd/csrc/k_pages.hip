@@ -1,5 +1,7 @@
 // A cache in pages of e4m3 codes: new keys and values into it (asr_write_pages)
 // and the page tables of a next step (asr_next_tables).
+#include <algorithm>
+
 #include "asr_device.h"
 
 namespace asr {
@@ -154,51 +156,60 @@ done:
 // ---------------------------------------------------------------------------
 // Page tables
 // ---------------------------------------------------------------------------
+// One block finds the new tables, many copy the pages.  The first is a chain of steps
+// between barriers, so everything that fits stays in LDS: the pages' two bits (kept by
+// some sequence, kept as a full page by some), what is known of each sequence, the old
+// table, the free pages that are given out.  Free pages are counted by the bits, a
+// word's 32 at once.  Who keeps a partly filled page is settled in a word per page of
+// the workspace, which only the sequences' last pages touch.
 constexpr int32_t kNobody = 0x7fffffff;
+constexpr int TB_NT = 1024, TB_WORDS = 8192, TB_SPOTS = 4096, TB_SEQS = 1024, TB_ENTRIES = 8192;
+constexpr int TB_CHUNK = 16384;            // bytes of a page that a block copies at a time
 
-struct TablesWork {          // words of the workspace
-  int32_t* owner;            // [pages] 0: read by some, s + 1: written by s
-  int32_t* to;               // [pages] where a page moves, itself otherwise
-  int32_t* spots;            // [pages] free pages, in order
-  int32_t* first_ask;        // [sequences + 1] asks before a sequence's
-  int32_t* copy_from;        // [sequences] page that a sequence has a copy of, or -1
-  int32_t* copy_to;
-  int32_t* counts;           // moves
-  int32_t* old_table;        // [sequences][columns], [sequences]
-  int32_t* old_length;
+struct SeqArrays {             // of each sequence
+  int32_t *parent, *length;    // it goes on from (or -1), positions it keeps
+  int32_t *full, *kept, *want; // pages: full ones, all kept, wanted
+  int32_t *first_ask, *from;   // asks before its own; the page that it gets a copy of, or -1
+  int32_t *gap;                // the first entry without a page
+};
+__host__ __device__ inline SeqArrays seq_arrays(int32_t* p, int n) {
+  return {p, p + n, p + 2 * (int64_t)n, p + 3 * (int64_t)n, p + 4 * (int64_t)n, p + 5 * (int64_t)n, p + 6 * (int64_t)n, p + 7 * (int64_t)n};
+}
+struct TablesWork {            // words of the workspace
+  int32_t* counts;             // pages to copy
+  int32_t* pairs;              // [pages + sequences][2] from, to
+  int32_t* owner;              // [pages] of a last page: s + 1
+  int32_t* to;                 // [pages] where a page moves
+  int32_t* spots;              // [pages] free pages, in order
+  uint32_t *used, *full;       // a bit per page
+  SeqArrays seq;
+  int32_t* old_table;          // [sequences][columns]
 };
 __host__ __device__ inline TablesWork tables_work(int32_t* ws, int sequences, int columns, int pages) {
   TablesWork w;
-  w.owner = ws;
+  const int words = (pages + 31) / 32;
+  w.counts = ws;
+  w.pairs = w.counts + 16;
+  w.owner = w.pairs + 2 * ((int64_t)pages + sequences);
   w.to = w.owner + pages;
   w.spots = w.to + pages;
-  w.first_ask = w.spots + pages;
-  w.copy_from = w.first_ask + sequences + 1;
-  w.copy_to = w.copy_from + sequences;
-  w.counts = w.copy_to + sequences;
-  w.old_length = w.counts + 16;
-  w.old_table = w.old_length + sequences;
+  w.used = (uint32_t*)w.spots + pages;
+  w.full = w.used + words;
+  int32_t* p = (int32_t*)w.full + words;
+  w.seq = seq_arrays(p, sequences);
+  w.old_table = p + 8 * (int64_t)sequences;
   return w;
 }
 
-struct NextSeq {
-  int parent, length, full, kept, want;      // pages: full ones, all kept, wanted
+struct TablesLds {
+  uint32_t used[TB_WORDS], full[TB_WORDS];
+  int32_t spots[TB_SPOTS], seq[8 * TB_SEQS], table[TB_ENTRIES];
+  int sums[16];
+  int copies;
 };
-__device__ __forceinline__ NextSeq next_seq(const TablesLaunch& a, const int32_t* lengths, int s) {
-  NextSeq n;
-  n.parent = a.parent ? a.parent[s] : s;
-  const int most = a.columns * a.page;
-  n.length = n.parent >= 0 && n.parent < a.sequences ? min(max(lengths[n.parent], 0), most) : 0;
-  n.full = n.length / a.page;
-  n.kept = (n.length + a.page - 1) / a.page;
-  const int want = a.want ? min(max(a.want[s], 0), most) : 0;
-  n.want = max(n.kept, (want + a.page - 1) / a.page);
-  return n;
-}
 
 // Exclusive sum over the block's 1024 threads; *total gets the sum of all.
-__device__ __forceinline__ int block_scan(int v, int* total) {
-  __shared__ int sums[16];
+__device__ __forceinline__ int block_scan(int v, int* sums, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int x = v;
 #pragma unroll
@@ -210,6 +221,7 @@ __device__ __forceinline__ int block_scan(int v, int* total) {
   if (lane == 63) sums[wave] = x;
   __syncthreads();
   int before = 0, all = 0;
+#pragma unroll
   for (int i = 0; i < 16; ++i) {
     if (i < wave) before += sums[i];
     all += sums[i];
@@ -218,131 +230,175 @@ __device__ __forceinline__ int block_scan(int v, int* total) {
   return before + x - v;
 }
 
-// One block: claims, asks, free pages, tables.
-__global__ __launch_bounds__(1024) void k_next_tables(TablesLaunch a, bool in_place) {
+// IN: the bits and what is known of the sequences fit in LDS.
+template <bool IN>
+__global__ __launch_bounds__(TB_NT) void k_next_tables(TablesLaunch a, bool in_place) {
+  extern __shared__ __attribute__((aligned(16))) char tables_lds[];
+  TablesLds& l = *(TablesLds*)tables_lds;
   const TablesWork w = tables_work(a.ws, a.sequences, a.columns, a.pages);
-  const int tid = threadIdx.x;
-  const int32_t *table = a.table, *lengths = a.length;
+  const int tid = threadIdx.x, n = a.sequences, words = (a.pages + 31) / 32;
+  const SeqArrays q = IN ? seq_arrays(l.seq, TB_SEQS) : w.seq;
+  uint32_t *used = IN ? l.used : w.used, *full = IN ? l.full : w.full;
+  const auto clear_word = [&](uint32_t* p) {
+    if constexpr (IN) *p = 0; else store_agent(p, 0u);
+  };
+  const auto word_of = [&](const uint32_t* p) -> uint32_t {
+    if constexpr (IN) return *p; else return load_agent(p);
+  };
+  const auto is_page = [&](int p) { return p >= 0 && p < a.pages; };
+
+  // the old table, where its entries are read twice from near or would be overwritten
+  const int64_t entries = (int64_t)n * a.columns;
+  const bool near = entries <= TB_ENTRIES;
+  const int32_t* table = a.table;
   int64_t ld = a.table_ld;
-  if (in_place) {
-    for (int64_t i = tid; i < (int64_t)a.sequences * a.columns; i += 1024) w.old_table[i] = a.table[i / a.columns * a.table_ld + i % a.columns];
-    for (int i = tid; i < a.sequences; i += 1024) w.old_length[i] = a.length[i];
-    table = w.old_table, lengths = w.old_length, ld = a.columns;
+  if (near || in_place) {
+    int32_t* copy = near ? l.table : w.old_table;
+    for (int64_t i = tid; i < entries; i += TB_NT) copy[i] = a.table[i / a.columns * a.table_ld + i % a.columns];
+    table = copy, ld = a.columns;
   }
-  for (int i = tid; i < a.pages; i += 1024) store_agent(&w.owner[i], kNobody);
-  __threadfence_block();
-  __syncthreads();
-  const int wave = tid >> 6, lane = tid & 63;
-  for (int s = wave; s < a.sequences; s += 16) {
-    const NextSeq n = next_seq(a, lengths, s);
-    for (int j = lane; j < n.kept; j += 64) {
-      const int p = table[n.parent * ld + j];
-      if (p >= 0 && p < a.pages) atomicMin(&w.owner[p], j < n.full ? 0 : s + 1);
+  for (int i = tid; i < words; i += TB_NT) clear_word(&used[i]), clear_word(&full[i]);
+  const int most = a.columns * a.page;
+  for (int s = tid; s < n; s += TB_NT) {
+    const int parent = a.parent ? a.parent[s] : s, want = a.want ? min(max(a.want[s], 0), most) : 0;
+    const bool goes_on = parent >= 0 && parent < n;
+    const int length = goes_on ? min(max(a.length[parent], 0), most) : 0;
+    const int whole = length / a.page, kept = whole + (whole * a.page < length);
+    q.parent[s] = goes_on ? parent : -1;
+    q.length[s] = length;
+    q.full[s] = whole;
+    q.kept[s] = kept;
+    q.want[s] = max(kept, (want + a.page - 1) / a.page);
+    q.gap[s] = a.columns;
+    if (whole < kept) {
+      const int p = a.table[parent * a.table_ld + whole];
+      if (is_page(p)) store_agent(&w.owner[p], kNobody);
     }
+  }
+  if (tid == 0) l.copies = 0;
+  // (the atomics of other waves come behind these stores in the L2)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+
+  // what is kept, by whom
+  for (int64_t i = tid; i < entries; i += TB_NT) {
+    const int s = (int)(i / a.columns), j = (int)(i % a.columns);
+    if (j >= q.kept[s]) continue;
+    const int p = table[q.parent[s] * ld + j];
+    if (!is_page(p)) continue;
+    atomicOr(&used[p >> 5], 1u << (p & 31));
+    if (j < q.full[s])
+      atomicOr(&full[p >> 5], 1u << (p & 31));
+    else
+      atomicMin(&w.owner[p], s + 1);
   }
   __syncthreads();
   // asks of each sequence
   int asked = 0;
-  for (int s0 = 0; s0 < a.sequences; s0 += 1024) {
+  for (int s0 = 0; s0 < n; s0 += TB_NT) {
     const int s = s0 + tid;
     int mine = 0;
-    if (s < a.sequences) {
-      const NextSeq n = next_seq(a, lengths, s);
+    if (s < n) {
       int from = -1;
-      if (n.full < n.kept) {
-        const int p = table[n.parent * ld + n.full];
-        if (p >= 0 && p < a.pages && load_agent(&w.owner[p]) != s + 1) from = p;
+      if (q.full[s] < q.kept[s]) {
+        const int p = table[q.parent[s] * ld + q.full[s]];
+        if (is_page(p) && ((word_of(&full[p >> 5]) >> (p & 31) & 1) || load_agent(&w.owner[p]) != s + 1)) from = p;
       }
-      w.copy_from[s] = from;
-      w.copy_to[s] = -1;
-      mine = (from >= 0) + n.want - n.kept;
+      q.from[s] = from;
+      mine = (from >= 0) + q.want[s] - q.kept[s];
     }
     int total;
-    const int before = block_scan(mine, &total);
-    if (s < a.sequences) w.first_ask[s] = asked + before;
+    const int before = block_scan(mine, l.sums, &total);
+    if (s < n) q.first_ask[s] = asked + before;
     asked += total;
   }
-  // free pages in order
-  int free = 0;
-  for (int p0 = 0; p0 < a.pages; p0 += 1024) {
-    const int p = p0 + tid;
-    const int is = p < a.pages && load_agent(&w.owner[p]) == kNobody;
-    int total;
-    const int before = block_scan(is, &total);
-    if (is) w.spots[free + before] = p;
-    if (p < a.pages) w.to[p] = p;
-    free += total;
-  }
-  __syncthreads();
+  // free pages: a thread's words lie together
+  const int per = (words + TB_NT - 1) / TB_NT, first = min(tid * per, words), end = min(first + per, words);
+  const auto pages_of = [&](int i) { return i * 32 + 32 <= a.pages ? 0xffffffffu : (1u << (a.pages & 31)) - 1; };
+  int free = 0, free_before = 0, mine = 0;
+  for (int i = first; i < end; ++i) mine += __popc(~word_of(&used[i]) & pages_of(i));
+  free_before = block_scan(mine, l.sums, &free);
   const int granted = min(asked, free), in_use = a.pages - free + granted;
-  int moves = 0;
+  const auto behind = [&](int i) {         // the bits of pages from in_use on
+    return i * 32 >= in_use ? 0xffffffffu : i * 32 + 32 <= in_use ? 0u : 0xffffffffu << (in_use & 31);
+  };
+  int moves = 0, moves_before = 0;
   if (a.compact) {
-    for (int p0 = 0; p0 < a.pages; p0 += 1024) {
-      const int p = p0 + tid;
-      const int is = p < a.pages && p >= in_use && load_agent(&w.owner[p]) != kNobody;
-      int total;
-      const int before = block_scan(is, &total);
-      if (is) w.to[p] = w.spots[moves + before];
-      moves += total;
-    }
+    mine = 0;
+    for (int i = first; i < end; ++i) mine += __popc(word_of(&used[i]) & behind(i));
+    moves_before = block_scan(mine, l.sums, &moves);
+  }
+  // the first of them, as many as are given out
+  const int need = moves + granted;
+  int32_t* spots = need <= TB_SPOTS ? l.spots : w.spots;
+  for (int i = first; i < end && free_before < need; ++i)
+    for (uint32_t bits = ~word_of(&used[i]) & pages_of(i); bits && free_before < need; bits &= bits - 1)
+      spots[free_before++] = i * 32 + __ffs(bits) - 1;
+  __syncthreads();
+  if (moves) {
+    for (int i = first; i < end; ++i)
+      for (uint32_t bits = word_of(&used[i]) & behind(i); bits; bits &= bits - 1) {
+        const int p = i * 32 + __ffs(bits) - 1, to = spots[moves_before];
+        w.to[p] = to;
+        *(int2*)&w.pairs[2 * moves_before++] = int2{p, to};
+      }
     __syncthreads();
   }
   // tables
-  int copies = 0;
-  for (int s = wave; s < a.sequences; s += 16) {
-    const NextSeq n = next_seq(a, lengths, s);
-    const int from = w.copy_from[s], ask0 = w.first_ask[s];
-    int32_t* row = a.new_table + s * a.new_ld;
-    int gap = a.columns;
-    for (int j0 = 0; j0 < a.columns; j0 += 64) {
-      const int j = j0 + lane;
-      int p = -1;
-      if (j < n.kept && !(j == n.full && from >= 0)) {
-        p = table[n.parent * ld + j];
-        p = p >= 0 && p < a.pages ? w.to[p] : -1;
-      } else if (j < n.want) {
-        const int ask = ask0 + (j < n.kept ? 0 : (from >= 0) + j - n.kept);
-        p = ask < granted ? w.spots[moves + ask] : -1;
-        if (j < n.kept) {
-          w.copy_to[s] = p;
-          copies += p >= 0;
-        }
-      }
-      if (j < a.columns) row[j] = p;
-      const uint64_t holes = __ballot(p < 0);
-      if (gap == a.columns && holes) gap = min(a.columns, j0 + __ffsll((unsigned long long)holes) - 1);
+  for (int64_t i = tid; i < entries; i += TB_NT) {
+    const int s = (int)(i / a.columns), j = (int)(i % a.columns), kept = q.kept[s], from = q.from[s];
+    const bool copied = from >= 0 && j == q.full[s];
+    int p = -1;
+    if (j < kept && !copied) {
+      p = table[q.parent[s] * ld + j];
+      p = !is_page(p) ? -1 : moves && p >= in_use ? w.to[p] : p;
+    } else if (j < q.want[s]) {
+      const int ask = q.first_ask[s] + (copied ? 0 : (from >= 0) + j - kept);
+      p = ask < granted ? spots[moves + ask] : -1;
+      if (copied && p >= 0) *(int2*)&w.pairs[2 * (moves + atomicAdd(&l.copies, 1))] = int2{from, p};
     }
-    if (lane == 0) {
-      a.new_length[s] = n.length;
-      if (a.room) a.room[s] = gap * a.page;
+    a.new_table[s * a.new_ld + j] = p;
+    if (p < 0) atomicMin(&q.gap[s], j);
+  }
+  __syncthreads();
+  for (int s = tid; s < n; s += TB_NT) {
+    a.new_length[s] = q.length[s];
+    if (a.room) {
+      if constexpr (IN) a.room[s] = q.gap[s] * a.page; else a.room[s] = load_agent(&q.gap[s]) * a.page;
     }
   }
-  int total;
-  block_scan(copies, &total);
   if (tid == 0) {
-    w.counts[0] = moves;
-    if (a.info) a.info[0] = in_use, a.info[1] = asked - granted, a.info[2] = total, a.info[3] = moves;
+    w.counts[0] = moves + l.copies;
+    if (a.info) a.info[0] = in_use, a.info[1] = asked - granted, a.info[2] = l.copies, a.info[3] = moves;
   }
 }
 
-// One block per sequence's copy, then per page that may move.
-__global__ __launch_bounds__(256) void k_copy_pages(TablesLaunch a) {
-  const TablesWork w = tables_work(a.ws, a.sequences, a.columns, a.pages);
-  int src, dst;
-  if (blockIdx.x < (uint32_t)a.sequences) {
-    src = w.copy_from[blockIdx.x], dst = w.copy_to[blockIdx.x];
-    if (dst < 0) return;
-  } else {
-    src = blockIdx.x - a.sequences;
-    dst = w.to[src];
-    if (dst == src) return;
+template <typename V>
+__device__ __forceinline__ void copy_bytes(const char* from, char* to, int64_t begin, int64_t end) {
+  constexpr int N = TB_CHUNK / (256 * sizeof(V));
+  if (N <= 4 && end - begin == TB_CHUNK) {
+    V v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = ((const V*)(from + begin))[i * 256 + threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < N; ++i) ((V*)(to + begin))[i * 256 + threadIdx.x] = v[i];
+    return;
   }
-  const uint32_t* c = (const uint32_t*)((const char*)a.codes + src * a.code_stride);
-  uint32_t* d = (uint32_t*)((char*)a.codes + dst * a.code_stride);
-  for (int64_t i = threadIdx.x; i < a.code_bytes / 4; i += 256) d[i] = c[i];
-  c = (const uint32_t*)((const char*)a.scales + src * a.scale_stride);
-  d = (uint32_t*)((char*)a.scales + dst * a.scale_stride);
-  for (int64_t i = threadIdx.x; i < a.scale_bytes / 4; i += 256) d[i] = c[i];
+  for (int64_t i = begin + threadIdx.x * sizeof(V); i < end; i += 256 * sizeof(V)) *(V*)(to + i) = *(const V*)(from + i);
+}
+// Chunks of pages, over all that are to be copied.  None of them is copied from and to.
+template <typename V>
+__global__ __launch_bounds__(256) void k_copy_pages(TablesLaunch a, int chunks) {
+  const TablesWork w = tables_work(a.ws, a.sequences, a.columns, a.pages);
+  const int64_t units = (int64_t)w.counts[0] * chunks;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const int2 pair = *(const int2*)&w.pairs[2 * (u / chunks)];
+    const int64_t begin = u % chunks * TB_CHUNK;
+    copy_bytes<V>((const char*)a.codes + pair.x * a.code_stride, (char*)a.codes + pair.y * a.code_stride, begin,
+                  min(begin + TB_CHUNK, a.code_bytes));
+    if (begin == 0)
+      copy_bytes<uint32_t>((const char*)a.scales + pair.x * a.scale_stride, (char*)a.scales + pair.y * a.scale_stride, 0, a.scale_bytes);
+  }
 }
 
 }  // namespace
@@ -357,12 +413,26 @@ void write_pages(const PageWriteLaunch& a, bool bf16, hipStream_t s) {
 }
 
 int64_t tables_ws_words(int sequences, int columns, int pages) {
-  return 3 * (int64_t)pages + 4 * (int64_t)sequences + 17 + (int64_t)sequences * columns;
+  return 16 + 5 * (int64_t)pages + 2 * (int64_t)((pages + 31) / 32) + 10 * (int64_t)sequences + (int64_t)sequences * columns;
 }
 
-void next_tables(const TablesLaunch& a, hipStream_t s) {
-  k_next_tables<<<1, 1024, 0, s>>>(a, (const int32_t*)a.new_table == a.table);
-  if (a.codes || a.scales) k_copy_pages<<<dim3((unsigned)(a.sequences + (a.compact ? a.pages : 0))), 256, 0, s>>>(a);
+hipError_t next_tables(const TablesLaunch& a, hipStream_t s) {
+  const bool in_place = (const int32_t*)a.new_table == a.table, in = a.pages <= 32 * TB_WORDS && a.sequences <= TB_SEQS;
+  const auto kernel = in ? k_next_tables<true> : k_next_tables<false>;
+  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(TablesLds));
+  if (e != hipSuccess) return e;
+  kernel<<<1, TB_NT, sizeof(TablesLds), s>>>(a, in_place);
+  if (!a.codes && !a.scales) return hipSuccess;
+  const int chunks = (int)std::max<int64_t>(1, (a.code_bytes + TB_CHUNK - 1) / TB_CHUNK);
+  const int64_t most = ((int64_t)a.sequences + (a.compact ? a.pages : 0)) * chunks;
+  if (most == 0) return hipSuccess;
+  const unsigned blocks = (unsigned)std::min<int64_t>(most, 2048);
+  const bool wide = !(((uintptr_t)a.codes | (uint64_t)a.code_stride | (uint64_t)a.code_bytes) & 15);
+  if (wide)
+    k_copy_pages<uint4><<<dim3(blocks), 256, 0, s>>>(a, chunks);
+  else
+    k_copy_pages<uint32_t><<<dim3(blocks), 256, 0, s>>>(a, chunks);
+  return hipSuccess;
 }
 
 }  // namespace asr

@@ -453,8 +453,7 @@ asr_status asr_next_tables(const asr_page_tables* t, void* ws, size_t ws_bytes, 
     st = check_ws(ws, ws_bytes, need);
     if (st != ASR_OK) return st;
     s.ws = (int32_t*)ws + kCounters;
-    next_tables(s, (hipStream_t)stream);
-    return launched(hipSuccess);
+    return launched(next_tables(s, (hipStream_t)stream));
   });
 }
 
