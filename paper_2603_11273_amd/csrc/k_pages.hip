@@ -45,6 +45,12 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t c, float by) {
   return code4(x);
 }
 
+// Four values that are finite and, over the scale, at most 448.
+__device__ __forceinline__ uint32_t code4_plain(const float* x, float inv) {
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, lo, true);
+}
+
 // Bytes [lo, hi) of the 16 at a dword-aligned place.
 __device__ __forceinline__ void store_some(uint8_t* p, const uint32_t* w, int lo, int hi) {
   if (lo <= 0 && hi >= 16) {
@@ -56,12 +62,66 @@ __device__ __forceinline__ void store_some(uint8_t* p, const uint32_t* w, int lo
     if (i >= lo && i < hi) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
 }
 
+// Four values from an address that is a multiple of four.
+__device__ __forceinline__ void load4(const float* p, float* x) {
+  const float4 v = *(const float4*)p;
+  x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+}
+__device__ __forceinline__ void load4(const bf16_t* p, float* x) {
+  const uint2 v = *(const uint2*)p;
+  x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
+  x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
+}
+
+// What a block of positions gets: tokens start + i to positions length + i, i < count.
+struct NewTokens {
+  int start, count;
+  int64_t length, stop;                    // positions from length to stop
+};
+__device__ __forceinline__ NewTokens new_tokens(const PageWriteLaunch& a, int seq) {
+  const int length = a.length[seq];
+  int start = a.token_start ? a.token_start[seq] : seq, end = a.token_start ? a.token_start[seq + 1] : seq + 1;
+  start = max(start, 0);
+  end = min(min(end, a.tokens), start > INT32_MAX - a.max_new ? INT32_MAX : start + a.max_new);
+  return {start, length < 0 ? 0 : end - start, length, min((int64_t)length + (end - start), (int64_t)a.c.columns * a.c.page)};
+}
+// Codes and scale of a head's block of positions in a page; keys or values.
+struct BlockPlace {
+  uint8_t* codes;
+  float* scale;
+};
+__device__ __forceinline__ BlockPlace block_place(const Pages& c, int page, int64_t p0, int head, int which) {
+  const int per = c.page / kPageBlock;
+  const int64_t at = ((int64_t)which * c.kv_heads + head) * per + (p0 % c.page) / kPageBlock;
+  return {c.codes + page * c.page_stride + at * (kPageBlock * kHeadDim), c.scales + page * c.scale_stride + at};
+}
+// A block's scale with new values up to `top` behind `old` positions: the factor that
+// earlier codes take where it grew.
+struct NewScale {
+  int e;
+  bool grew;
+  float by;
+};
+__device__ __forceinline__ NewScale new_scale(uint32_t top, int old, const float* scale) {
+  NewScale n = {need_exp(top), false, 1.f};
+  if (old > 0) {
+    const float s = *scale;
+    n.e = max(n.e, held_exp(s));
+    n.grew = s != exp_scale(n.e);
+    n.by = (s > 0.f ? s : exp_scale(kLeastScale)) / exp_scale(n.e);
+  }
+  return n;
+}
+
 // One block of 256 threads per (sequence, touched block of positions, head, keys or
-// values); thread = (position, 16 dims).
+// values).  Keys: thread = (position, 16 dims); values, which lie [dim][position]: thread =
+// 4 positions x 4 dims, turned in registers and LDS into (dim, 16 positions).  Bound
+// by memory: 36000 bf16 tokens of 20 heads (276 MB) @AUDIO@.
+constexpr int PW_PITCH = 68;               // bytes of a dim in LDS: writes of a wave go to 64 banks
 template <typename T>
 __global__ __launch_bounds__(256) void k_write_pages(PageWriteLaunch a, int touched) {
-  __shared__ uint32_t tops[4];
-  __shared__ __attribute__((aligned(16))) uint8_t turn[64 * 80];
+  __shared__ uint32_t tops[2][4];
+  __shared__ __attribute__((aligned(16))) uint8_t turn[64 * PW_PITCH];
   const int tid = threadIdx.x;
   uint32_t u = blockIdx.x;
   const int which = u & 1;
@@ -69,88 +129,128 @@ __global__ __launch_bounds__(256) void k_write_pages(PageWriteLaunch a, int touc
   const int head = (int)(u % a.c.kv_heads);
   u /= a.c.kv_heads;
   const int nth = (int)(u % touched), seq = (int)(u / touched);
-  const int length = a.length[seq];
-  int start = a.token_start ? a.token_start[seq] : seq, end = a.token_start ? a.token_start[seq + 1] : seq + 1;
-  start = max(start, 0);
-  end = min(min(end, a.tokens), start > INT32_MAX - a.max_new ? INT32_MAX : start + a.max_new);
-  if (length < 0 || end <= start) return;
-  const int64_t block = (int64_t)length / kPageBlock + nth, p0 = block * kPageBlock;
-  const int64_t stop = min((int64_t)length + (end - start), (int64_t)a.c.columns * a.c.page);
-  if (p0 >= stop) return;
-  const int old = (int)max((int64_t)length - p0, (int64_t)0), last = (int)min(stop - p0, (int64_t)kPageBlock);
+  const NewTokens t = new_tokens(a, seq);
+  if (t.count <= 0) return;
+  const int64_t p0 = (t.length / kPageBlock + nth) * kPageBlock;
+  if (p0 >= t.stop) return;
+  const int old = (int)max(t.length - p0, (int64_t)0), last = (int)min(t.stop - p0, (int64_t)kPageBlock);
   const int page = a.c.table[(int64_t)seq * a.c.table_ld + p0 / a.c.page];
   if (page < 0 || page >= a.c.pages) return;
-  const int per = a.c.page / kPageBlock;
-  const int64_t at = ((int64_t)which * a.c.kv_heads + head) * per + (p0 % a.c.page) / kPageBlock;
-  uint8_t* codes = a.c.codes + page * a.c.page_stride + at * (kPageBlock * kHeadDim);
-  float* scale = a.c.scales + page * a.c.scale_stride + at;
+  const BlockPlace b = block_place(a.c, page, p0, head, which);
 
-  const int pos = tid >> 2, d0 = (tid & 3) * 16;
-  const bool fresh = pos >= old && pos < last;
-  float x[16];
+  float x[4][4];
   uint32_t top = 0;
-  if (fresh) {
-    const T* src = (const T*)(which ? a.v : a.k) + (start + (p0 + pos - length)) * a.ld + head * kHeadDim + d0;
+  const int pos = which ? tid >> 4 << 2 : tid >> 2, d0 = which ? (tid & 15) * 4 : (tid & 3) * 16;
+  const T* src = (const T*)(which ? a.v : a.k) + (t.start + (p0 - t.length) + pos) * a.ld + head * kHeadDim + d0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      x[i] = St<T>::ld(src, i);
-      top = max(top, magnitude(x[i]));
+  for (int i = 0; i < 4; ++i) {
+    const int at = which ? pos + i : pos;
+    if (at >= old && at < last) {
+      load4(which ? src + i * a.ld : src + 4 * i, x[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(x[i][j]) & 0x7fffffffu);
   }
   top = wave_max_u32(top);
-  if ((tid & 63) == 0) tops[tid >> 6] = top;
+  if ((tid & 63) == 0) tops[0][tid >> 6] = top;
   __syncthreads();
-  top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-  int e = need_exp(top);
-  float by = 1.f;
-  bool grew = false;
-  if (old > 0) {
-    const float s = *scale;
-    e = max(e, held_exp(s));
-    grew = s != exp_scale(e);
-    by = (s > 0.f ? s : exp_scale(kLeastScale)) / exp_scale(e);
-  }
-  const float inv = exp_scale(254 - e);
-  uint32_t w[4] = {0, 0, 0, 0};
-  if (fresh) {
+  top = max(max(tops[0][0], tops[0][1]), max(tops[0][2], tops[0][3]));
+  const bool finite = top < 0x7f800000u;
+  if (!finite) {                           // of those that are
+    top = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float y[4] = {x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv};
+    for (int i = 0; i < 16; ++i) top = max(top, magnitude(x[i >> 2][i & 3]));
+    top = wave_max_u32(top);
+    if ((tid & 63) == 0) tops[1][tid >> 6] = top;
+    __syncthreads();
+    top = max(max(tops[1][0], tops[1][1]), max(tops[1][2], tops[1][3]));
+  }
+  const NewScale n = new_scale(top, old, b.scale);
+  const float inv = exp_scale(254 - n.e);
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (finite) {
+      w[i] = code4_plain(x[i], inv);
+    } else {
+      const float y[4] = {x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv};
       w[i] = code4(y);
     }
   }
   if (which == 0) {
-    uint8_t* p = codes + pos * kHeadDim + d0;
-    if (fresh) {
+    uint8_t* p = b.codes + pos * kHeadDim + d0;
+    if (pos >= old && pos < last) {
       *(uint4*)p = uint4{w[0], w[1], w[2], w[3]};
-    } else if (grew && pos < old) {
+    } else if (n.grew && pos < old) {
       const uint4 c = *(const uint4*)p;
-      *(uint4*)p = uint4{rescale4(c.x, by), rescale4(c.y, by), rescale4(c.z, by), rescale4(c.w, by)};
+      *(uint4*)p = uint4{rescale4(c.x, n.by), rescale4(c.y, n.by), rescale4(c.z, n.by), rescale4(c.w, n.by)};
     }
   } else {
-    // values lie [dim][position]: thread = (dim, 16 positions)
-    if (fresh)
-      for (int i = 0; i < 16; ++i) turn[(d0 + i) * 80 + pos] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    // w[position] of 4 dims to 4 positions of a dim
+    const uint32_t ab = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), cd = __builtin_amdgcn_perm(w[3], w[2], 0x05010400);
+    const uint32_t AB = __builtin_amdgcn_perm(w[1], w[0], 0x07030602), CD = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+    const uint32_t v[4] = {__builtin_amdgcn_perm(cd, ab, 0x05040100), __builtin_amdgcn_perm(cd, ab, 0x07060302),
+                           __builtin_amdgcn_perm(CD, AB, 0x05040100), __builtin_amdgcn_perm(CD, AB, 0x07060302)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *(uint32_t*)(turn + (d0 + i) * PW_PITCH + pos) = v[i];
     __syncthreads();
-    const int dim = tid >> 2, t0 = (tid & 3) * 16;
-    uint8_t* p = codes + dim * kPageBlock + t0;
-    const int from = grew ? 0 : old;
-    if (t0 + 16 <= from || t0 >= last) goto done;
-    {
+    const int dim = tid >> 2, t0 = (tid & 3) * 16, from = n.grew ? 0 : old;
+    uint8_t* p = b.codes + dim * kPageBlock + t0;
+    if (t0 + 16 > from && t0 < last) {
       uint32_t c[4];
-      for (int i = 0; i < 4; ++i) c[i] = *(const uint32_t*)(turn + dim * 80 + t0 + 4 * i);
-      if (grew && t0 < old) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = *(const uint32_t*)(turn + dim * PW_PITCH + t0 + 4 * i);
+      if (n.grew && t0 < old) {
         const uint4 o = *(const uint4*)p;
-        const uint32_t r[4] = {rescale4(o.x, by), rescale4(o.y, by), rescale4(o.z, by), rescale4(o.w, by)};
+        const uint32_t r[4] = {rescale4(o.x, n.by), rescale4(o.y, n.by), rescale4(o.z, n.by), rescale4(o.w, n.by)};
+#pragma unroll
         for (int i = 0; i < 16; ++i)
           if (t0 + i < old) c[i >> 2] = (c[i >> 2] & ~(0xffu << (8 * (i & 3)))) | (r[i >> 2] & (0xffu << (8 * (i & 3))));
       }
       store_some(p, c, from - t0, last - t0);
     }
   }
-done:
-  __syncthreads();
-  if (tid == 0) *scale = exp_scale(e);
+  __syncthreads();                         // (every thread has read the scale)
+  if (tid == 0) *b.scale = exp_scale(n.e);
+}
+
+// A token a sequence: one wave per (sequence, head, keys or values), lane = dim, so that
+// all loads of a step are under way at once (128 sequences, 20 heads: @STEP@).
+template <typename T>
+__global__ __launch_bounds__(256) void k_write_step(PageWriteLaunch a) {
+  const int lane = threadIdx.x & 63;
+  uint32_t u = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int which = u & 1;
+  u >>= 1;
+  const int head = (int)(u % a.c.kv_heads), seq = (int)(u / a.c.kv_heads);
+  if (seq >= a.c.sequences) return;
+  const NewTokens t = new_tokens(a, seq);
+  if (t.count <= 0 || t.length >= t.stop) return;
+  const float x = St<T>::ld((const T*)(which ? a.v : a.k) + t.start * a.ld + head * kHeadDim, lane);
+  const int page = a.c.table[(int64_t)seq * a.c.table_ld + t.length / a.c.page];
+  if (page < 0 || page >= a.c.pages) return;
+  const int old = (int)(t.length % kPageBlock);
+  const BlockPlace b = block_place(a.c, page, t.length - old, head, which);
+  const NewScale n = new_scale(wave_max_u32(magnitude(x)), old, b.scale);
+  const uint32_t code = code2(x * exp_scale(254 - n.e), 0.f) & 0xffu;
+  if (n.grew) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // 16 dims of a position, or 16 positions of a dim
+      const int row = i * 16 + (lane >> 2), col = (lane & 3) * 16;
+      uint8_t* p = b.codes + row * 64 + col;
+      if ((which ? col : row) >= old) continue;
+      const uint4 c = *(const uint4*)p;
+      uint32_t r[4] = {rescale4(c.x, n.by), rescale4(c.y, n.by), rescale4(c.z, n.by), rescale4(c.w, n.by)};
+      if (which) store_some(p, r, 0, old - col); else *(uint4*)p = uint4{r[0], r[1], r[2], r[3]};
+    }
+  }
+  b.codes[which ? lane * kPageBlock + old : old * kHeadDim + lane] = (uint8_t)code;
+  // (the wave has read the scale: the factors above come from it)
+  if (lane == 0) *b.scale = exp_scale(n.e);
 }
 
 // ---------------------------------------------------------------------------
@@ -164,7 +264,9 @@ done:
 // the workspace, which only the sequences' last pages touch.
 constexpr int32_t kNobody = 0x7fffffff;
 constexpr int TB_NT = 1024, TB_WORDS = 8192, TB_SPOTS = 4096, TB_SEQS = 1024, TB_ENTRIES = 8192;
-constexpr int TB_CHUNK = 16384;            // bytes of a page that a block copies at a time
+// Bytes of a page that a block copies at a time, 16 a thread (16384 in four loads each,
+// which leave fewer blocks: 120 beams' last pages, 13 MB read and written, 16 us instead of 4).
+constexpr int TB_CHUNK = 4096;
 
 struct SeqArrays {             // of each sequence
   int32_t *parent, *length;    // it goes on from (or -1), positions it keeps
@@ -375,15 +477,6 @@ __global__ __launch_bounds__(TB_NT) void k_next_tables(TablesLaunch a, bool in_p
 
 template <typename V>
 __device__ __forceinline__ void copy_bytes(const char* from, char* to, int64_t begin, int64_t end) {
-  constexpr int N = TB_CHUNK / (256 * sizeof(V));
-  if (N <= 4 && end - begin == TB_CHUNK) {
-    V v[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = ((const V*)(from + begin))[i * 256 + threadIdx.x];
-#pragma unroll
-    for (int i = 0; i < N; ++i) ((V*)(to + begin))[i * 256 + threadIdx.x] = v[i];
-    return;
-  }
   for (int64_t i = begin + threadIdx.x * sizeof(V); i < end; i += 256 * sizeof(V)) *(V*)(to + i) = *(const V*)(from + i);
 }
 // Chunks of pages, over all that are to be copied.  None of them is copied from and to.
@@ -404,6 +497,14 @@ __global__ __launch_bounds__(256) void k_copy_pages(TablesLaunch a, int chunks) 
 }  // namespace
 
 void write_pages(const PageWriteLaunch& a, bool bf16, hipStream_t s) {
+  if (a.max_new == 1) {
+    const unsigned blocks = (unsigned)(((int64_t)a.c.sequences * a.c.kv_heads * 2 + 3) / 4);
+    if (bf16)
+      k_write_step<bf16_t><<<dim3(blocks), 256, 0, s>>>(a);
+    else
+      k_write_step<float><<<dim3(blocks), 256, 0, s>>>(a);
+    return;
+  }
   const int touched = (int)(((int64_t)a.max_new + 2 * kPageBlock - 2) / kPageBlock);
   const unsigned blocks = (unsigned)((int64_t)a.c.sequences * touched * a.c.kv_heads * 2);
   if (bf16)
@@ -426,7 +527,7 @@ hipError_t next_tables(const TablesLaunch& a, hipStream_t s) {
   const int chunks = (int)std::max<int64_t>(1, (a.code_bytes + TB_CHUNK - 1) / TB_CHUNK);
   const int64_t most = ((int64_t)a.sequences + (a.compact ? a.pages : 0)) * chunks;
   if (most == 0) return hipSuccess;
-  const unsigned blocks = (unsigned)std::min<int64_t>(most, 2048);
+  const unsigned blocks = (unsigned)std::min<int64_t>(most, 8192);
   const bool wide = !(((uintptr_t)a.codes | (uint64_t)a.code_stride | (uint64_t)a.code_bytes) & 15);
   if (wide)
     k_copy_pages<uint4><<<dim3(blocks), 256, 0, s>>>(a, chunks);
