@@ -62,15 +62,21 @@ __device__ __forceinline__ void store_some(uint8_t* p, const uint32_t* w, int lo
     if (i >= lo && i < hi) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
 }
 
-// Four values from an address that is a multiple of four.
-__device__ __forceinline__ void load4(const float* p, float* x) {
-  const float4 v = *(const float4*)p;
-  x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+// 16 values; the address is a multiple of 16 bytes.
+__device__ __forceinline__ void load16(const float* p, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float4 v = ((const float4*)p)[i];
+    x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
+  }
 }
-__device__ __forceinline__ void load4(const bf16_t* p, float* x) {
-  const uint2 v = *(const uint2*)p;
-  x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
-  x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
+__device__ __forceinline__ void load16(const bf16_t* p, float* x) {
+  const uint4 v[2] = {((const uint4*)p)[0], ((const uint4*)p)[1]};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t u = ((const uint32_t*)v)[i];
+    x[2 * i] = __uint_as_float(u << 16), x[2 * i + 1] = __uint_as_float(u & 0xffff0000u);
+  }
 }
 
 // What a block of positions gets: tokens start + i to positions length + i, i < count.
@@ -114,10 +120,12 @@ __device__ __forceinline__ NewScale new_scale(uint32_t top, int old, const float
 }
 
 // One block of 256 threads per (sequence, touched block of positions, head, keys or
-// values).  Keys: thread = (position, 16 dims); values, which lie [dim][position]: thread =
-// 4 positions x 4 dims, turned in registers and LDS into (dim, 16 positions).  Bound
-// by memory: 36000 bf16 tokens of 20 heads (276 MB) @AUDIO@.
-constexpr int PW_PITCH = 68;               // bytes of a dim in LDS: writes of a wave go to 64 banks
+// values); thread = (position, 16 dims).  Values lie [dim][position] and are turned in LDS.
+// Bound by memory: 36000 bf16 tokens of 20 heads, 276 MB, in 58 us (4.75 TB/s).  A thread
+// of 4 positions x 4 dims turns its codes in registers, but its loads of 8 bytes cost more
+// than that saves (71 us).  What is not finite is looked for once a block: without any,
+// codes need neither bounds nor a test.
+constexpr int PW_PITCH = 68;               // bytes of a dim in LDS: the four groups of dims write to banks of their own
 template <typename T>
 __global__ __launch_bounds__(256) void k_write_pages(PageWriteLaunch a, int touched) {
   __shared__ uint32_t tops[2][4];
@@ -138,21 +146,16 @@ __global__ __launch_bounds__(256) void k_write_pages(PageWriteLaunch a, int touc
   if (page < 0 || page >= a.c.pages) return;
   const BlockPlace b = block_place(a.c, page, p0, head, which);
 
-  float x[4][4];
+  float x[16];
   uint32_t top = 0;
-  const int pos = which ? tid >> 4 << 2 : tid >> 2, d0 = which ? (tid & 15) * 4 : (tid & 3) * 16;
+  const int pos = tid >> 2, d0 = (tid & 3) * 16;
   const T* src = (const T*)(which ? a.v : a.k) + (t.start + (p0 - t.length) + pos) * a.ld + head * kHeadDim + d0;
+  const bool fresh = pos >= old && pos < last;
+  if (fresh) load16(src, x);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int at = which ? pos + i : pos;
-    if (at >= old && at < last) {
-      load4(which ? src + i * a.ld : src + 4 * i, x[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[i][j] = 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) top = max(top, __float_as_uint(x[i][j]) & 0x7fffffffu);
+  for (int i = 0; i < 16; ++i) {
+    if (!fresh) x[i] = 0.f;
+    top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
   }
   top = wave_max_u32(top);
   if ((tid & 63) == 0) tops[0][tid >> 6] = top;
@@ -162,7 +165,7 @@ __global__ __launch_bounds__(256) void k_write_pages(PageWriteLaunch a, int touc
   if (!finite) {                           // of those that are
     top = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, magnitude(x[i >> 2][i & 3]));
+    for (int i = 0; i < 16; ++i) top = max(top, magnitude(x[i]));
     top = wave_max_u32(top);
     if ((tid & 63) == 0) tops[1][tid >> 6] = top;
     __syncthreads();
@@ -174,28 +177,23 @@ __global__ __launch_bounds__(256) void k_write_pages(PageWriteLaunch a, int touc
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (finite) {
-      w[i] = code4_plain(x[i], inv);
+      w[i] = code4_plain(x + 4 * i, inv);
     } else {
-      const float y[4] = {x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv};
+      const float y[4] = {x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv};
       w[i] = code4(y);
     }
   }
   if (which == 0) {
     uint8_t* p = b.codes + pos * kHeadDim + d0;
-    if (pos >= old && pos < last) {
+    if (fresh) {
       *(uint4*)p = uint4{w[0], w[1], w[2], w[3]};
     } else if (n.grew && pos < old) {
       const uint4 c = *(const uint4*)p;
       *(uint4*)p = uint4{rescale4(c.x, n.by), rescale4(c.y, n.by), rescale4(c.z, n.by), rescale4(c.w, n.by)};
     }
   } else {
-    // w[position] of 4 dims to 4 positions of a dim
-    const uint32_t ab = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), cd = __builtin_amdgcn_perm(w[3], w[2], 0x05010400);
-    const uint32_t AB = __builtin_amdgcn_perm(w[1], w[0], 0x07030602), CD = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
-    const uint32_t v[4] = {__builtin_amdgcn_perm(cd, ab, 0x05040100), __builtin_amdgcn_perm(cd, ab, 0x07060302),
-                           __builtin_amdgcn_perm(CD, AB, 0x05040100), __builtin_amdgcn_perm(CD, AB, 0x07060302)};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *(uint32_t*)(turn + (d0 + i) * PW_PITCH + pos) = v[i];
+    for (int i = 0; i < 16; ++i) turn[(d0 + i) * PW_PITCH + pos] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
     __syncthreads();
     const int dim = tid >> 2, t0 = (tid & 3) * 16, from = n.grew ? 0 : old;
     uint8_t* p = b.codes + dim * kPageBlock + t0;
@@ -217,8 +215,9 @@ __global__ __launch_bounds__(256) void k_write_pages(PageWriteLaunch a, int touc
   if (tid == 0) *b.scale = exp_scale(n.e);
 }
 
-// A token a sequence: one wave per (sequence, head, keys or values), lane = dim, so that
-// all loads of a step are under way at once (128 sequences, 20 heads: @STEP@).
+// A token a sequence: one wave per (sequence, head, keys or values), lane = dim: 16
+// times fewer waves than the blocks above, so that all of them run at once (128
+// sequences of 20 heads: 14.3 -> 8.9 us).
 template <typename T>
 __global__ __launch_bounds__(256) void k_write_step(PageWriteLaunch a) {
   const int lane = threadIdx.x & 63;
