@@ -271,6 +271,8 @@ struct PagedLaunch {
   const int32_t *row_start, *first, *length;
   int32_t n_head, rows, max_rows, max_keys, part, parts;
   float* rec;
+  int64_t blocks;
+  uint32_t* counters;          // one per sequence and cache head (queries of one tile), or NULL: a second kernel joins
 };
 void attend_pages(const PagedLaunch& a, bool bf16, hipStream_t s);
 // 16-column query tiles that a block holds, of `cols` queries of a sequence and cache head

@@ -5,7 +5,8 @@
 // to 64 of the sequence's queries; its four waves take the part's blocks of 64 keys
 // in turn, each with a running maximum, sum and weighted values of its own, joined
 // through LDS at the end; the parts of a row are joined from (max, sum, values)
-// records by a second kernel, or not at all where there is one part.
+// records by the last of its blocks or a second kernel, or not at all where there is one
+// part.
 //
 // Codes go from memory to the matrix instructions without LDS.  With lane = 16 g + m,
 // four score tiles S^T = K Q^T of 16 keys are loaded so that they leave lane (m, g) with
@@ -134,6 +135,53 @@ __device__ __forceinline__ void keep_keys(uint4* v, int key, int lo, int hi) {
 }
 // 0x80 in every byte that is a NaN code.
 __device__ __forceinline__ uint32_t nan_codes(uint32_t c) { return ((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+// out of a row and head from its parts' records, a wave's work, lane = dim: a chain of
+// loads, so all it needs is loaded at once, PA_JOIN records at a time; which of them hold
+// anything they say themselves.  HERE: records of the same launch.
+constexpr int PA_JOIN = 16;
+template <typename T, bool HERE>
+struct Join {
+  const float* val;
+  const float2* ml;
+  int parts, lane;
+  float v[PA_JOIN];
+  float2 rec;
+  __device__ __forceinline__ Join(const PagedLaunch& c, int row, int h)
+      : val(c.rec + ((int64_t)row * c.n_head + h) * c.parts * kHeadDim + (threadIdx.x & 63)), ml(record(c, row, h, 0)),
+        parts(c.parts), lane(threadIdx.x & 63) {
+    load(0);
+  }
+  __device__ __forceinline__ void load(int p0) {
+    rec = float2{-INFINITY, 0.f};
+    if (lane < PA_JOIN && p0 + lane < parts)
+      rec = HERE ? __builtin_bit_cast(float2, load_agent((const uint64_t*)&ml[p0 + lane])) : ml[p0 + lane];
+#pragma unroll
+    for (int p = 0; p < PA_JOIN; ++p) {
+      const float* x = val + (int64_t)(p0 + p) * kHeadDim;
+      v[p] = p0 + p >= parts ? 0.f : HERE ? load_agent(x) : *x;
+    }
+  }
+  __device__ __forceinline__ void store(const PagedLaunch& c, int row, int h) {
+    float M = -INFINITY, L = 0.f, acc = 0.f;
+    for (int p0 = 0; p0 < parts; p0 += PA_JOIN) {
+      if (p0 > 0) load(p0);
+      const bool there = !(rec.y == 0.f);
+      const uint64_t some = __ballot(there);
+      if (!some) continue;
+      const float top = fmaxf(M, wave_max_lanes(there ? rec.x : -INFINITY));
+      const float keep = M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
+      const float fac = !there ? 0.f : rec.x == top ? 1.f : __builtin_amdgcn_exp2f(rec.x - top);
+      M = top;
+      L = L * keep + wave_sum_lanes(there ? fac * rec.y : 0.f);
+      acc *= keep;
+#pragma unroll
+      for (int j = 0; j < PA_JOIN; ++j)
+        if (some >> j & 1) acc += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fac), j)) * v[j];
+    }
+    St<T>::st((T*)c.out, row * c.out_ld + h * kHeadDim + lane, L == 0.f ? 0.f : acc / L);
+  }
+};
 
 template <typename T, int QT>
 __global__ __launch_bounds__(PA_NW * 64) __attribute__((amdgpu_waves_per_eu(QT == 1 ? 3 : 2)))
@@ -391,32 +439,36 @@ void k_attend_pages(PagedArgs a) {
       St<T>::st4((T*)a.c.out, r * a.c.out_ld + h * kHeadDim + d4,
                  L == 0.f ? float4{0.f, 0.f, 0.f, 0.f} : float4{x.x / L, x.y / L, x.z / L, x.w / L});
     } else {
-      if (L != 0.f) *(float4*)(a.c.rec + (((int64_t)r * a.c.n_head + h) * a.c.parts + part) * kHeadDim + d4) = x;
-      if (d4 == 0) *record(a.c, r, h, part) = float2{M, L};
+      float* v = a.c.rec + (((int64_t)r * a.c.n_head + h) * a.c.parts + part) * kHeadDim + d4;
+      float2* ml = record(a.c, r, h, part);
+      if (QT == 1 && a.c.counters) {
+        if (L != 0.f) {
+          store_agent((uint64_t*)v, __builtin_bit_cast(uint64_t, float2{x.x, x.y}));
+          store_agent((uint64_t*)v + 1, __builtin_bit_cast(uint64_t, float2{x.z, x.w}));
+        }
+        if (d4 == 0) store_agent((uint64_t*)ml, __builtin_bit_cast(uint64_t, float2{M, L}));
+      } else {
+        if (L != 0.f) *(float4*)v = x;
+        if (d4 == 0) *ml = float2{M, L};
+      }
+    }
+  }
+  if (QT == 1 && a.c.counters && arrive_last(a.c.counters + ((int64_t)seq * a.c.c.kv_heads + head) * a.tiles + ctile, a.c.parts)) {
+    const int cols = min(count * a.per - col0, 16 * QT);
+    for (int col = wave; col < cols; col += PA_NW) {
+      const int j = (col0 + col) / a.per, r = start + j, h = head * a.per + col0 + col - j * a.per;
+      Join<T, true>(a.c, r, h).store(a.c, r, h);
     }
   }
 }
 
-// out of a row and head from its parts' records; one wave each, lane = dim.  The
-// kernel is a chain of loads, so all it needs is loaded at once, PA_JOIN records at a
-// time; which of them hold anything they say themselves.
-constexpr int PA_JOIN = 16;
 template <typename T>
 __global__ __launch_bounds__(256) void k_join_pages(PagedArgs a) {
   const uint32_t w = blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (w >= (uint32_t)a.c.rows * a.c.n_head) return;
-  const int row = (int)(w / a.c.n_head), h = (int)(w % a.c.n_head), parts = a.c.parts;
-  const float* val = a.c.rec + (int64_t)w * parts * kHeadDim + lane;
-  const float2* ml = record(a.c, row, h, 0);
-  float v[PA_JOIN];
-  float2 rec;
-  auto load = [&](int p0) {
-    rec = lane < PA_JOIN && p0 + lane < parts ? ml[p0 + lane] : float2{-INFINITY, 0.f};
-#pragma unroll
-    for (int p = 0; p < PA_JOIN; ++p) v[p] = p0 + p < parts ? val[(int64_t)(p0 + p) * kHeadDim] : 0.f;
-  };
-  load(0);
+  const int row = (int)(w / a.c.n_head), h = (int)(w % a.c.n_head);
+  Join<T, false> join(a.c, row, h);
   if (a.c.row_start) {
     // the row's sequence is the last one that starts at or before it
     int start = -1, end = 0;
@@ -431,23 +483,7 @@ __global__ __launch_bounds__(256) void k_join_pages(PagedArgs a) {
   } else if (row >= a.c.c.sequences) {
     return;
   }
-  float M = -INFINITY, L = 0.f, acc = 0.f;
-  for (int p0 = 0; p0 < parts; p0 += PA_JOIN) {
-    if (p0 > 0) load(p0);
-    const bool there = !(rec.y == 0.f);
-    const uint64_t some = __ballot(there);
-    if (!some) continue;
-    const float top = fmaxf(M, wave_max_lanes(there ? rec.x : -INFINITY));
-    const float keep = M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
-    const float fac = !there ? 0.f : rec.x == top ? 1.f : __builtin_amdgcn_exp2f(rec.x - top);
-    M = top;
-    L = L * keep + wave_sum_lanes(there ? fac * rec.y : 0.f);
-    acc *= keep;
-#pragma unroll
-    for (int j = 0; j < PA_JOIN; ++j)
-      if (some >> j & 1) acc += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(fac), j)) * v[j];
-  }
-  St<T>::st((T*)a.c.out, row * a.c.out_ld + h * kHeadDim + lane, L == 0.f ? 0.f : acc / L);
+  join.store(a.c, row, h);
 }
 
 template <typename T, int QT>
@@ -467,7 +503,7 @@ void attend(const PagedLaunch& c, hipStream_t s) {
   a.units = (uint32_t)((int64_t)c.c.sequences * c.parts * c.c.kv_heads);
   const int64_t blocks = ((int64_t)a.units + 7) / 8 * 8 * a.tiles;        // (below 2^24: the caller)
   qt == 1 ? launch<T, 1>(a, blocks, s) : launch<T, 2>(a, blocks, s);
-  if (c.parts != 1) k_join_pages<T><<<dim3((unsigned)(((int64_t)c.rows * c.n_head + 3) / 4)), 256, 0, s>>>(a);
+  if (c.parts != 1 && !c.counters) k_join_pages<T><<<dim3((unsigned)(((int64_t)c.rows * c.n_head + 3) / 4)), 256, 0, s>>>(a);
 }
 
 }  // namespace

@@ -262,6 +262,7 @@ asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* byte
   s->rows = a->rows;
   s->max_rows = a->row_start ? a->max_rows : 1;
   s->max_keys = (int32_t)most;
+  s->blocks = (int64_t)units * s->parts;
   *bytes = s->parts > 1 ? kCounters * 4 + (size_t)a->rows * a->n_head * s->parts * (kHeadDim + 2) * 4 : 0;
   return ASR_OK;
 }
@@ -421,6 +422,12 @@ asr_status asr_attend_pages(const asr_paged_attention* a, void* ws, size_t ws_by
     st = check_ws(ws, ws_bytes, need);
     if (st != ASR_OK) return st;
     s.rec = need ? (float*)ws + kCounters : nullptr;
+    // With up to a block a CU and two queries a wave, the last block of a row's parts joins
+    // them; above that a second kernel does (us, last block / kernel: a row on 1500 keys,
+    // 6 heads 7.8 / 9.7, 4 rows of 32 heads on 4000 10 / 12; 2 x 3 rows on 8000, 12
+    // queries a cache head 13.6 / 12.2, 4 rows on 60000 27 / 23).
+    const int64_t queries = (int64_t)s.max_rows * (s.n_head / s.c.kv_heads);
+    s.counters = need && s.blocks <= cu_count() && queries <= 8 ? (uint32_t*)ws : nullptr;
     attend_pages(s, a->dtype == ASR_BF16, (hipStream_t)stream);
     return launched(hipSuccess);
   });
