@@ -297,58 +297,62 @@ __device__ SM_INLINE Cut cut_list(const List& e, Cut in, bool by_count, uint64_t
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < SM_NW; ++i) hi = fmaxf(hi, s.tops[i]), lo = fminf(lo, s.lows[i]);
-  // bins of one width over their range: most often the cut's holds a few tokens
-  const float range = hi - lo, by = range > 1e-30f && range < 1e30f ? (SM_FINE - 1) / range : 0.f;
-  auto bin = [&](float x) SM_INLINE { return min((int)((hi - x) * by), SM_FINE - 1); };
-  for (int i = lane; i < e.n; i += 64) {
-    const float x = e.logit[i];
-    if (in.keeps(x, e.token[i])) atomicAdd((unsigned long long*)&s.fine[bin(x)], by_count ? 1ull : (unsigned long long)w.whole(x));
-  }
-  find_bin<SM_FINE>(s.fine, s, [&](uint64_t) SM_INLINE { return goal; });
-  const int found = s.found;
-  uint64_t rest = goal - s.found_before;
-  for (int i = lane; i < e.n; i += 64) {
-    const float x = e.logit[i];
-    if (in.keeps(x, e.token[i]) && bin(x) == found) {
-      const uint32_t at = atomicAdd(&s.members, 1u);
-      if (at < SM_MEMBERS) s.member_logit[at] = x, s.member_token[at] = e.token[i];
-    }
-  }
-  __syncthreads();
-  const int m = s.members;
-  if (m <= SM_MEMBERS) {                   // (every wave for itself)
-    const float x = lane < m ? s.member_logit[lane] : -INFINITY;
-    const int token = lane < m ? s.member_token[lane] : INT32_MAX;
-    const uint64_t y = lane >= m ? 0 : by_count ? 1 : w.whole(x);
-    uint64_t before = 0;
-    for (int j = 0; j < m; ++j) {
-      const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), j));
-      const int t = __builtin_amdgcn_readlane(token, j);
-      before += o > x || (o == x && t < token) ? lane_value(y, j) : 0;
-    }
-    const int at = __ffsll((unsigned long long)__ballot(before < rest && rest <= before + y)) - 1;
-    return {__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at)), __builtin_amdgcn_readlane(token, at)};
-  }
-  // many in one bin (equal ones, as a rule): by the digits of their logits
-  uint32_t prefix = 0;
-#pragma unroll 1
-  for (int level = 0; level < 3; ++level) {
-    const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
-    __syncthreads();
-    clear<sizeof(s.fine)>(s.fine);
-    __syncthreads();
+  uint64_t rest = goal;
+  float l = hi;                            // (often all have one logit)
+  if (hi != lo) {
+    // bins of one width over their range: most often the cut's holds a few tokens
+    const float range = hi - lo, by = range > 1e-30f && range < 1e30f ? (SM_FINE - 1) / range : 0.f;
+    auto bin = [&](float x) SM_INLINE { return min((int)((hi - x) * by), SM_FINE - 1); };
     for (int i = lane; i < e.n; i += 64) {
       const float x = e.logit[i];
-      const uint32_t k = falling(x);
-      if (in.keeps(x, e.token[i]) && bin(x) == found && (level == 0 || !((k ^ prefix) >> (shift + bits))))
-        atomicAdd((unsigned long long*)&s.fine[k >> shift & ((1 << bits) - 1)], by_count ? 1ull : (unsigned long long)w.whole(x));
+      if (in.keeps(x, e.token[i])) atomicAdd((unsigned long long*)&s.fine[bin(x)], by_count ? 1ull : (unsigned long long)w.whole(x));
     }
-    find_bin<SM_FINE>(s.fine, s, [&](uint64_t) SM_INLINE { return rest; });
-    prefix |= s.found << shift;
+    find_bin<SM_FINE>(s.fine, s, [&](uint64_t) SM_INLINE { return goal; });
+    const int found = s.found;
     rest -= s.found_before;
+    for (int i = lane; i < e.n; i += 64) {
+      const float x = e.logit[i];
+      if (in.keeps(x, e.token[i]) && bin(x) == found) {
+        const uint32_t at = atomicAdd(&s.members, 1u);
+        if (at < SM_MEMBERS) s.member_logit[at] = x, s.member_token[at] = e.token[i];
+      }
+    }
+    __syncthreads();
+    const int m = s.members;
+    if (m <= SM_MEMBERS) {                   // (every wave for itself)
+      const float x = lane < m ? s.member_logit[lane] : -INFINITY;
+      const int token = lane < m ? s.member_token[lane] : INT32_MAX;
+      const uint64_t y = lane >= m ? 0 : by_count ? 1 : w.whole(x);
+      uint64_t before = 0;
+      for (int j = 0; j < m; ++j) {
+        const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), j));
+        const int t = __builtin_amdgcn_readlane(token, j);
+        before += o > x || (o == x && t < token) ? lane_value(y, j) : 0;
+      }
+      const int at = __ffsll((unsigned long long)__ballot(before < rest && rest <= before + y)) - 1;
+      return {__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at)), __builtin_amdgcn_readlane(token, at)};
+    }
+    // many in one bin: by the digits of their logits
+    uint32_t prefix = 0;
+  #pragma unroll 1
+    for (int level = 0; level < 3; ++level) {
+      const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
+      __syncthreads();
+      clear<sizeof(s.fine)>(s.fine);
+      __syncthreads();
+      for (int i = lane; i < e.n; i += 64) {
+        const float x = e.logit[i];
+        const uint32_t k = falling(x);
+        if (in.keeps(x, e.token[i]) && bin(x) == found && (level == 0 || !((k ^ prefix) >> (shift + bits))))
+          atomicAdd((unsigned long long*)&s.fine[k >> shift & ((1 << bits) - 1)], by_count ? 1ull : (unsigned long long)w.whole(x));
+      }
+      find_bin<SM_FINE>(s.fine, s, [&](uint64_t) SM_INLINE { return rest; });
+      prefix |= s.found << shift;
+      rest -= s.found_before;
+    }
+    l = of_falling(prefix);
   }
   // the first of those at the cut's logit
-  const float l = of_falling(prefix);
   const uint64_t each = by_count ? 1 : max(w.whole(l), (uint64_t)1), ties = (rest + each - 1) / each;
   const int per = (e.n + 63) / 64, begin = min(lane * per, e.n), end = min(begin + per, e.n);
   uint64_t n = 0, t;
@@ -426,8 +430,11 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     r.each([&](int base, const float* x) SM_INLINE {
 #pragma unroll
       for (int i = E - 1; i >= 0; --i) {
-        if (logprob_out) all += w.whole(x[i]);
         if (x[i] == top) at = min(at, base + i);
+      }
+      if (logprob_out) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) all += w.whole(x[i]);
       }
     });
     if (at < INT32_MAX) atomicMin(&s.first, at);
@@ -551,23 +558,26 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       for (int i = 0; i < E; ++i) {
         is[i] = __ballot(depth(top, x[i]) - lo < width);
         any |= is[i];
-        if (sum_all) sum += w.whole(x[i]);
+      }
+      if (sum_all) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) sum += w.whole(x[i]);
       }
       if (any) {
-        bool in[E];
         uint32_t at = n;
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-          in[i] = (is[i] >> lane & 1) && cut.keeps(x[i], base + i);
-          is[i] = __ballot(in[i]);
-          at = __builtin_amdgcn_mbcnt_hi((uint32_t)(is[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)is[i], at));
-          n += __popcll(is[i]);
-        }
+        for (int i = 0; i < E; ++i)
+          if (is[i]) {
+            is[i] &= __ballot(cut.keeps(x[i], base + i));
+            at = __builtin_amdgcn_mbcnt_hi((uint32_t)(is[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)is[i], at));
+            n += __popcll(is[i]);
+          }
 #pragma unroll
         for (int i = 0; i < E; ++i)
-          if (in[i]) {
-            if (at < (uint32_t)room) logit[at] = x[i], token[at] = base + i;
-            ++at;
+          if (is[i]) {
+            const bool in = is[i] >> lane & 1;
+            if (in && at < (uint32_t)room) logit[at] = x[i], token[at] = base + i;
+            at += in;
           }
       }
     });
@@ -686,15 +696,16 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     const uint32_t lo = bin_begin(from), width = bin_end(to) - lo;
     uint64_t sum = 0;
     r.each([&](int base, const float* x) SM_INLINE {
+      bool in[E], some = sum_all;
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const uint32_t at = depth(top, x[i]);
-        const bool in = at - lo < width && cut.keeps(x[i], base + i);
-        if (!sum_all && !__any(in)) continue;
-        const uint64_t y = w.whole(x[i]);
-        if (sum_all) sum += y;
-        if (in && y) atomicAdd((unsigned long long*)&s.bins[bin_of(at)], (unsigned long long)y);
-      }
+      for (int i = 0; i < E; ++i) some |= in[i] = depth(top, x[i]) - lo < width && cut.keeps(x[i], base + i);
+      if (!__any(some)) return;
+      uint64_t y[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) sum += y[i] = w.whole(x[i]);
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (in[i] && y[i]) atomicAdd((unsigned long long*)&s.bins[bin_of(depth(top, x[i]))], (unsigned long long)y[i]);
     });
     if (sum_all) all = block_add(sum, s), have_all = true;
   };
@@ -729,14 +740,16 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   __syncthreads();
   r.each(
       [&](int base, const float* x) SM_INLINE {
+        bool in[E], some = sum_all;
+#pragma unroll
+        for (int i = 0; i < E; ++i) some |= in[i] = cut.keeps(x[i], base + i);
+        if (!__any(some)) return;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          const bool in = cut.keeps(x[i], base + i);
-          if (!sum_all && !__any(in)) continue;
           const uint64_t y = w.whole(x[i]);
-          n += in;
+          n += in[i];
           sum += y;
-          part += in ? y : 0;
+          part += in[i] ? y : 0;
         }
       },
       [&](int seg) SM_INLINE {
