@@ -20,6 +20,8 @@
 // Weights are whole numbers, so sums do not depend on an order: 2^(i / 512) from a table
 // times a polynomial, in 64 bits.  The kernel is bound by its instructions: a weight
 // takes about 24 of them, a bin 7, against half a cycle a token for its bytes.
+#include <algorithm>
+
 #include "asr_device.h"
 
 namespace asr {
@@ -78,9 +80,9 @@ struct RowOf {
     }
   }
   __device__ __forceinline__ int base(int step) const { return first + (step * 64 + (int)(threadIdx.x & 63)) * E; }
-  // f(first token, x) over the wave's part; after(segment) behind each SM_U steps
+  // f(first token, 16 bytes) over the wave's part; after(segment) behind each SM_U steps
   template <class F, class G>
-  __device__ SM_INLINE void each(F&& f, G&& after) const {
+  __device__ SM_INLINE void raw(F&& f, G&& after) const {
 #pragma unroll 1
     for (int i = 0; i < steps; i += SM_U) {
       uint4 u[SM_U];
@@ -88,13 +90,20 @@ struct RowOf {
       for (int j = 0; j < SM_U; ++j) u[j] = fetch(base(i + j));
 #pragma unroll
       for (int j = 0; j < SM_U; ++j)
-        if (i + j < steps) {
-          float x[E];
-          floats(u[j], x);
-          f(base(i + j), x);
-        }
+        if (i + j < steps) f(base(i + j), u[j]);
       after((int)(threadIdx.x >> 6) * ((steps + SM_U - 1) / SM_U) + i / SM_U);
     }
+  }
+  // f(first token, x)
+  template <class F, class G>
+  __device__ SM_INLINE void each(F&& f, G&& after) const {
+    raw(
+        [&](int base, const uint4& u) SM_INLINE {
+          float x[E];
+          floats(u, x);
+          f(base, x);
+        },
+        after);
   }
   template <class F>
   __device__ SM_INLINE void each(F&& f) const {
@@ -178,6 +187,35 @@ struct Lds {
 };
 static_assert(kRulesMaxVocab <= SM_NT * SM_U * 64 * 4, "a segment a thread");
 
+// bf16 logits by their values: SV_N values from the row's largest down (17344 or more of them
+// negative ones where that is below 4: to -384), the last for all behind.
+constexpr int SV_N = 33 * SM_NT, SV_IDS = 2048;
+struct ValuesLds {
+  double tab[SM_TAB];
+  uint32_t hist[SV_N];                     // tokens of a value, then the place of its weight
+  union {
+    uint64_t weight[SV_IDS];
+    struct {
+      uint64_t mass[SV_N / 64];
+      uint32_t n[SV_N / 64];
+    } part;                                // of 64 values
+  };
+  uint64_t seg[SM_NT / 2];
+  uint32_t ties[SM_NT / 2];                // at the cut's value before a segment
+  uint64_t sums[2][SM_NW];
+  uint64_t found_before, found_other;
+  uint32_t found, ids;
+};
+static_assert(sizeof(ValuesLds) <= 163840, "the LDS of a CU");
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+// Of two bf16, numbers that rise as they fall, the zeros' equal; and back.
+__device__ __forceinline__ i16x2 falling2(uint32_t u) {
+  const i16x2 x = __builtin_bit_cast(i16x2, u), negative = x >> 15;
+  return (x ^ ~negative) + (negative | (int16_t)-32768);
+}
+__device__ __forceinline__ uint32_t falling16(uint32_t b) { return b & 0x8000u ? b - 1 : 0x7fffu - b; }
+__device__ __forceinline__ float of_falling16(uint32_t k) { return __uint_as_float((k & 0x8000u ? k + 1 : 0x7fffu - k) << 16); }
+
 // Inclusive sum over the lanes before (data-parallel moves: rows of 16, then their ends).
 __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
 #define SM_STEP(ctrl, rows)                                                                          \
@@ -200,7 +238,8 @@ __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
 }
 // Exclusive sums over the threads of two values; their sums over all in *va and *vb.
-__device__ __forceinline__ void block_scan2(uint64_t a, uint64_t b, Lds& s, uint64_t* before_a, uint64_t* va, uint64_t* before_b,
+template <class S>
+__device__ __forceinline__ void block_scan2(uint64_t a, uint64_t b, S& s, uint64_t* before_a, uint64_t* va, uint64_t* before_b,
                                             uint64_t* vb) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t x = wave_scan(a), y = wave_scan(b);
@@ -221,7 +260,8 @@ __device__ __forceinline__ void block_scan2(uint64_t a, uint64_t b, Lds& s, uint
   *va = ta;
   *vb = tb;
 }
-__device__ __forceinline__ uint64_t block_scan(uint64_t v, Lds& s, uint64_t* total) {
+template <class S>
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, S& s, uint64_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t x = wave_scan(v);
   __syncthreads();
@@ -469,6 +509,197 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     least = {of_falling(in), INT32_MAX};
   }
   auto tighter = [&](Cut x) SM_INLINE { return least.l > x.l ? least : x; };
+
+  // ---- bf16: all that the cut takes is how many tokens have each value
+  if constexpr (E == 8) {
+    ValuesLds& v = *(ValuesLds*)sample_lds;
+    const uint32_t first_key = falling16(__float_as_uint(top) >> 16);
+    const i16x2 from = {(int16_t)first_key, (int16_t)first_key};
+    const uint32_t none = falling16(0xff80u) - first_key;           // -inf
+    // (false: tokens behind the values that are counted matter)
+    auto by_values = [&]() SM_INLINE {
+      __syncthreads();
+      for (int i = tid; i < SV_N / 4; i += SM_NT) ((uint4*)v.hist)[i] = uint4{0, 0, 0, 0};
+      if (tid == 0) v.ids = 0;
+      __syncthreads();
+      auto at2 = [&](uint32_t u) SM_INLINE { return __builtin_bit_cast(uint32_t, falling2(u) - from); };
+      r.raw(
+          [&](int, const uint4& u) SM_INLINE {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t k = at2(((const uint32_t*)&u)[i]);
+              atomicAdd(&v.hist[min(k & 0xffffu, (uint32_t)SV_N - 1)], 1u);
+              atomicAdd(&v.hist[min(k >> 16, (uint32_t)SV_N - 1)], 1u);
+            }
+          },
+          [](int) SM_INLINE {});
+      __syncthreads();
+      auto count_of = [&](uint32_t b) SM_INLINE { return b == SV_N - 1 || b == none ? 0u : v.hist[b]; };
+      auto weight_of = [&](uint32_t b) SM_INLINE { return w.whole(of_falling16(first_key + b)); };
+#pragma unroll 1
+      for (int i = 0; i < SV_N / SM_NT; ++i) {
+        const uint32_t b = i * SM_NT + tid, c = count_of(b);
+        uint64_t n = 0, mass = 0;
+        if (__any(c != 0)) n = wave_scan(c), mass = wave_scan(c * weight_of(b));
+        if (lane == 63) v.part.n[i * SM_NW + wave] = (uint32_t)n, v.part.mass[i * SM_NW + wave] = mass;
+      }
+      __syncthreads();
+      const bool has_part = tid < SV_N / 64;
+      const uint64_t n = has_part ? v.part.n[tid] : 0, mass = has_part ? v.part.mass[tid] : 0;
+      uint64_t n_before, n_all, mass_before, mass_all;
+      block_scan2(n, mass, v, &n_before, &n_all, &mass_before, &mass_all);
+      if (v.hist[SV_N - 1] && (w.place(of_falling16(first_key + SV_N - 1)) >= w.least || (k_on && n_all < (uint64_t)top_k))) return false;
+      all = mass_all;
+      uint32_t end = 0, ties = 0;          // kept: values before `end`, and of that one the first `ties` tokens
+      uint64_t each = 0, kept_mass = mass_all;
+      auto locate = [&](bool by_count, uint64_t goal) SM_INLINE {
+        const uint64_t own = by_count ? n : mass, before = by_count ? n_before : mass_before;
+        if (before < goal && goal <= before + own) v.found = tid, v.found_before = before, v.found_other = mass_before;
+        __syncthreads();
+        const uint32_t b = v.found * 64 + lane, c = count_of(b);
+        const uint64_t y = weight_of(b), z = by_count ? c : c * y, upto = v.found_before + wave_scan(z);
+        const uint64_t weights = v.found_other + wave_scan(c * y) - c * y;
+        const int at = __ffsll((unsigned long long)__ballot(upto - z < goal && goal <= upto)) - 1;
+        const uint64_t rest = goal - lane_value(upto - z, at);
+        const uint32_t there = __builtin_amdgcn_readlane(c, at);
+        each = lane_value(y, at);
+        end = __builtin_amdgcn_readlane(b, at);
+        ties = (uint32_t)(by_count ? rest : (rest + each - 1) / each);
+        kept_mass = lane_value(weights, at) + ties * each;
+        if (ties == there) ++end, ties = 0;
+        __syncthreads();
+      };
+      const bool k_cuts = k_on && n_all >= (uint64_t)top_k;
+      if (k_cuts) locate(true, top_k);
+      if (p_on) locate(false, p_goal(kept_mass));
+      if (!k_cuts && !p_on) end = min(none, (uint32_t)SV_N - 1);   // all
+      if (least.l > -INFINITY) {
+        const uint32_t u = __float_as_uint(least.l), behind = falling16((u >> 31 ? u : u + 0xffffu) >> 16) - first_key + 1;
+        if (behind <= end) end = behind, ties = 0;
+      }
+      // the kept values' weights
+      uint64_t kept_n = 0;
+      kept_mass = 0;
+      for (uint32_t b = tid; b < end; b += SM_NT) {
+        const uint32_t c = count_of(b);
+        if (!c) continue;
+        const uint64_t y = weight_of(b);
+        const uint32_t id = atomicAdd(&v.ids, 1u);
+        if (id < SV_IDS) v.weight[id] = y;
+        v.hist[b] = id;
+        kept_n += c;
+        kept_mass += c * y;
+      }
+      uint64_t t0, t1, kept_all, mass_kept;
+      block_scan2(kept_n, kept_mass, v, &t0, &kept_all, &t1, &mass_kept);
+      mass_kept += ties * each;
+      if (tid == 0 && a.kept) a.kept[row] = (int32_t)kept_all + ties;
+      // segments' sums
+      const bool table = v.ids <= SV_IDS;
+      uint64_t part = 0;
+      uint32_t equal = 0;
+      r.raw(
+          [&](int, const uint4& u) SM_INLINE {
+            uint32_t k[E];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t both = at2(((const uint32_t*)&u)[i]);
+              k[2 * i] = both & 0xffffu, k[2 * i + 1] = both >> 16;
+            }
+            uint32_t least_k = k[0];
+#pragma unroll
+            for (int i = 1; i < E; ++i) least_k = min(least_k, k[i]);
+            if (ties) {
+#pragma unroll
+              for (int i = 0; i < E; ++i) equal += k[i] == end;
+            }
+            if (!__any(least_k < end)) return;
+            if (table) {
+#pragma unroll
+              for (int i = 0; i < E; ++i) k[i] = k[i] < end ? v.hist[k[i]] : ~0u;
+#pragma unroll
+              for (int i = 0; i < E; ++i) {
+                const uint64_t y = v.weight[min(k[i], (uint32_t)SV_IDS - 1)];
+                part += k[i] != ~0u ? y : 0;
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < E; ++i) part += k[i] < end ? weight_of(k[i]) : 0;
+            }
+          },
+          [&](int seg) SM_INLINE {
+            if (__any(part != 0)) part = lane_value(wave_scan(part), 63);
+            uint32_t e = 0;
+            if (ties && __any(equal)) e = (uint32_t)lane_value(wave_scan(equal), 63);
+            if (lane == 0) v.seg[seg] = part, v.ties[seg] = e;
+            part = 0, equal = 0;
+          });
+      __syncthreads();
+      const int segments = r.segments();
+      const uint64_t own_ties = tid < segments ? v.ties[tid] : 0;
+      const uint64_t ties_before = block_scan(own_ties, v, &t0);
+      uint64_t own = tid < segments ? v.seg[tid] : 0;
+      if (ties_before < ties) own += min(ties - ties_before, own_ties) * each;
+      const uint64_t upto = block_scan(own, v, &t0) + own;
+      if (tid < segments) v.seg[tid] = upto, v.ties[tid] = (uint32_t)ties_before;
+      __syncthreads();
+      for (int d = wave; d < a.draws; d += SM_NW) {
+        const uint64_t goal = goal_of(d, mass_kept);
+        int lo = 0, hi = segments - 1;                             // the first segment whose sum is above goal
+        while (lo < hi) {
+          const int mid = (lo + hi) / 2;
+          if (v.seg[mid] > goal) hi = mid; else lo = mid + 1;
+        }
+        uint64_t c = lo ? v.seg[lo - 1] : 0, tied = v.ties[lo];
+        const int steps = r.segment_steps(lo);
+        uint4 u[SM_U];
+#pragma unroll
+        for (int j = 0; j < SM_U; ++j) u[j] = r.fetch(j < steps ? r.segment_base(lo, j) : a.vocab);
+#pragma unroll
+        for (int j = 0; j < SM_U; ++j) {
+          if (j >= steps) break;
+          float x[E];
+          uint64_t z[E], of_lane = 0, equal_lane = 0;
+          uint32_t k[E];
+          const int base = r.segment_base(lo, j);
+          r.floats(u[j], x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t both = at2(((const uint32_t*)&u[j])[i]);
+            k[2 * i] = both & 0xffffu, k[2 * i + 1] = both >> 16;
+          }
+#pragma unroll
+          for (int i = 0; i < E; ++i) equal_lane += k[i] == end;
+          const uint64_t scanned_ties = wave_scan(equal_lane);
+          uint64_t nth = tied + scanned_ties - equal_lane;
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            const bool in = k[i] < end || (k[i] == end && nth < ties);
+            nth += k[i] == end;
+            of_lane += z[i] = in ? w.whole(x[i]) : 0;
+          }
+          const uint64_t scanned = wave_scan(of_lane);
+          uint64_t at = c + scanned - of_lane;
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            if (at <= goal && goal < at + z[i]) answer(d, base + i, x[i]);
+            at += z[i];
+          }
+          c += lane_value(scanned, 63);
+          tied += lane_value(scanned_ties, 63);
+        }
+      }
+      return true;
+    };
+    if (r.steps * 64 * E > SM_LIST && (k_on || p_on)) {
+      if (by_values()) return;
+      __syncthreads();
+      all = 0;
+      clear<sizeof(s.bins)>(s.bins);
+      clear<sizeof(s.counts)>(s.counts);
+      __syncthreads();
+    }
+  }
 
   // ---- a bin that the cut is not behind: `last`; tokens before it
   int last = -1;
@@ -774,11 +1005,16 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     }
     uint64_t c = lo ? s.seg[lo - 1] : 0;
     const int steps = r.segment_steps(lo);
-    for (int j = 0; j < steps; ++j) {
+    uint4 u[SM_U];
+#pragma unroll
+    for (int j = 0; j < SM_U; ++j) u[j] = r.fetch(j < steps ? r.segment_base(lo, j) : a.vocab);
+#pragma unroll
+    for (int j = 0; j < SM_U; ++j) {
+      if (j >= steps) break;
       float x[E];
       uint64_t z[E], of_lane = 0;
       const int base = r.segment_base(lo, j);
-      r.floats(r.fetch(base), x);
+      r.floats(u[j], x);
 #pragma unroll
       for (int i = 0; i < E; ++i) of_lane += z[i] = cut.keeps(x[i], base + i) ? w.whole(x[i]) : 0;
       const uint64_t scanned = wave_scan(of_lane);
@@ -794,10 +1030,12 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
 }
 
 template <typename T>
+constexpr int kLds = sizeof(T) == 2 ? (int)std::max(sizeof(Lds), sizeof(ValuesLds)) : (int)sizeof(Lds);
+template <typename T>
 hipError_t launch(const SampleLaunch& a, int unit, hipStream_t s) {
-  const hipError_t e = hipFuncSetAttribute((const void*)k_sample<T>, hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(Lds));
+  const hipError_t e = hipFuncSetAttribute((const void*)k_sample<T>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds<T>);
   if (e != hipSuccess) return e;
-  k_sample<T><<<dim3((unsigned)a.rows), SM_NT, sizeof(Lds), s>>>(a, unit);
+  k_sample<T><<<dim3((unsigned)a.rows), SM_NT, kLds<T>, s>>>(a, unit);
   return hipSuccess;
 }
 

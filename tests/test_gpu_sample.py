@@ -126,6 +126,48 @@ def test_zeros_of_either_sign_tie():
     assert check(x, [[0.1], [0.9]], top_k=[1, 2]).reshape(-1).tolist() == [5, 9]
 
 
+@pytest.mark.parametrize("V", [9001, 60007])
+def test_bf16_values(V):
+    """Rows of bf16 logits that are counted by value, and those whose values lie too far apart for that."""
+    rng = np.random.default_rng(V)
+    rows = 9
+    x = (rng.standard_normal((rows, V)) * 3 - 4).astype(np.float32)
+    x[1, 100:] = -1e30                                   # masked by a large number
+    x[2, 100:] = -np.inf
+    x[3] = rng.integers(0, 3, V)                         # three values
+    x[4] *= 2.0 ** rng.integers(-30, 6, V)               # thousands of values, tiny ones among them
+    x[5] = x[5] * 100 + 3000                             # a large maximum: values down to it are out of reach
+    x[6] = -np.abs(x[6]) * 1000
+    x[7, ::2], x[7, 1::4] = 0.0, -0.0
+    x[8] = 1e38 * np.sign(x[8])
+    x = torch.from_numpy(x).to(BF16)
+    u = rng.random((rows, 3)).astype(np.float32)
+    k = [50, 99, 100, V // 2, 3000, 5000, 17, V // 3, V // 2 + 7]
+    check(x, u, top_k=k)
+    check(x, u, top_k=[101] * rows, top_p=[0.9] * rows)
+    check(x, u, top_p=[0.9, 0.5, 0.99, 0.7, 0.6, 0.8, 0.3, 0.95, 0.9], temperature=[1, 2, 0.5, 1, 0.2, 30, 500, 1, 1])
+    check(x, u, top_k=k, top_p=[0.97] * rows, min_p=[0.01, 0, 0.5, 0.1, 0.02, 1e-6, 0, 0.3, 0], temperature=[0.7] * rows)
+    check(x, u, top_k=[V - 1] * rows, temperature=[float("inf"), 1e30, 1, 1e6, 1, 1e38, 1, 1e-3, 1])
+
+
+def test_f32_rows_that_the_lists_cannot_hold():
+    """Cuts among many tokens: wide distributions, many equal logits, logits in rising and falling order."""
+    rng = np.random.default_rng(37)
+    V, rows = 60007, 6
+    x = (rng.standard_normal((rows, V)) * 0.5).astype(np.float32)
+    x[1] = np.round(x[1] * 8) / 8
+    x[2], x[3] = np.sort(x[2]), np.sort(x[3])[::-1]
+    x[4] = 0.0
+    x[5] = np.where(rng.random(V) < 0.7, 1.0, x[5])
+    x = torch.from_numpy(x)
+    u = rng.random((rows, 3)).astype(np.float32)
+    check(x, u, top_k=[20000, 30000, 9000, 50000, 777, 44000])
+    check(x, u, top_p=[0.91, 0.5, 0.99, 0.3, 0.7003, 0.95])
+    # (all weights of row 4 are 1, which a min-p of 1 keeps: no distance, and nothing rounded)
+    check(x, u, least=-1, top_k=[20000, 30000, 9000, 50000, 30001, 44000], top_p=[0.9, 0.6, 0.95, 0.4, 0.7003, 0.97], min_p=[0.3, 0.01, 0, 0.2, 1, 0])
+    check(x, u, least=-1, min_p=[0.5, 0.6, 0.2, 0.1, 1.0, 0.9])
+
+
 def test_parameter_sets():
     x, u, rng = inputs(19, 7, 1500, BF16, draws=2)
     check(x, u, temperature=[0.5, 1.5, 0.0], top_k=[3, 0, 50], set=[2, 0, 0, -1, 1, 3, 2147483647], sets=3)
