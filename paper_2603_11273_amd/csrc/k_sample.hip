@@ -80,24 +80,38 @@ struct RowOf {
     }
   }
   __device__ __forceinline__ int base(int step) const { return first + (step * 64 + (int)(threadIdx.x & 63)) * E; }
-  // f(first token, 16 bytes) over the wave's part; after(segment) behind each SM_U steps
-  template <class F, class G>
+  // f(first token, 16 bytes) over the wave's part; after(segment) behind each SM_U steps.
+  // U loads at once; 1: one ahead, in the least code, where f is long.
+  template <int U, class F, class G>
   __device__ SM_INLINE void raw(F&& f, G&& after) const {
+    const int seg = (int)(threadIdx.x >> 6) * ((steps + SM_U - 1) / SM_U);
+    if constexpr (U == 1) {
+      uint4 next = fetch(base(0));
 #pragma unroll 1
-    for (int i = 0; i < steps; i += SM_U) {
-      uint4 u[SM_U];
+      for (int i = 0; i < steps; ++i) {
+        const uint4 u = next;
+        next = fetch(base(i + 1));
+        f(base(i), u);
+        if (i % SM_U == SM_U - 1 || i == steps - 1) after(seg + i / SM_U);
+      }
+    } else {
+      static_assert(U == SM_U, "");
+#pragma unroll 1
+      for (int i = 0; i < steps; i += SM_U) {
+        uint4 u[SM_U];
 #pragma unroll
-      for (int j = 0; j < SM_U; ++j) u[j] = fetch(base(i + j));
+        for (int j = 0; j < SM_U; ++j) u[j] = fetch(base(i + j));
 #pragma unroll
-      for (int j = 0; j < SM_U; ++j)
-        if (i + j < steps) f(base(i + j), u[j]);
-      after((int)(threadIdx.x >> 6) * ((steps + SM_U - 1) / SM_U) + i / SM_U);
+        for (int j = 0; j < SM_U; ++j)
+          if (i + j < steps) f(base(i + j), u[j]);
+        after(seg + i / SM_U);
+      }
     }
   }
   // f(first token, x)
-  template <class F, class G>
+  template <int U, class F, class G>
   __device__ SM_INLINE void each(F&& f, G&& after) const {
-    raw(
+    raw<U>(
         [&](int base, const uint4& u) SM_INLINE {
           float x[E];
           floats(u, x);
@@ -105,9 +119,9 @@ struct RowOf {
         },
         after);
   }
-  template <class F>
+  template <int U, class F>
   __device__ SM_INLINE void each(F&& f) const {
-    each(f, [](int) SM_INLINE {});
+    each<U>(f, [](int) SM_INLINE {});
   }
   __device__ __forceinline__ int segments() const { return SM_NW * ((steps + SM_U - 1) / SM_U); }
   // the first token of a segment's step for this lane; steps of the segment
@@ -192,9 +206,9 @@ static_assert(kRulesMaxVocab <= SM_NT * SM_U * 64 * 4, "a segment a thread");
 constexpr int SV_N = 33 * SM_NT, SV_IDS = 2048;
 struct ValuesLds {
   double tab[SM_TAB];
-  uint32_t hist[SV_N];                     // tokens of a value, then the place of its weight
+  uint32_t hist[SV_N];                     // tokens of a value, then where its weight is, in bytes
   union {
-    uint64_t weight[SV_IDS];
+    uint64_t weight[SV_IDS + 1];           // the last: 0
     struct {
       uint64_t mass[SV_N / 64];
       uint32_t n[SV_N / 64];
@@ -237,45 +251,24 @@ __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 |
          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
 }
-// Exclusive sums over the threads of two values; their sums over all in *va and *vb.
+// Exclusive sums over the threads; the sum over all in *total.  (Code that runs once is
+// bound by its fetch, some 0.1 us for 64 bytes: the waves' sums are joined by a scan too.)
+template <class S>
+__device__ __forceinline__ uint64_t block_scan(uint64_t v, S& s, uint64_t* total, int which = 0) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t x = wave_scan(v);
+  if (which == 0) __syncthreads();
+  if (lane == 63) s.sums[which][wave] = x;
+  __syncthreads();
+  const uint64_t upto = wave_scan(s.sums[which][lane & (SM_NW - 1)]);       // (lanes 0 to 15: of the waves)
+  *total = lane_value(upto, SM_NW - 1);
+  return (wave ? lane_value(upto, wave - 1) : 0) + x - v;
+}
 template <class S>
 __device__ __forceinline__ void block_scan2(uint64_t a, uint64_t b, S& s, uint64_t* before_a, uint64_t* va, uint64_t* before_b,
                                             uint64_t* vb) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t x = wave_scan(a), y = wave_scan(b);
-  __syncthreads();
-  if (lane == 63) s.sums[0][wave] = x, s.sums[1][wave] = y;
-  __syncthreads();
-  uint64_t pa = 0, pb = 0, ta = 0, tb = 0;
-#pragma unroll
-  for (int i = 0; i < SM_NW; ++i) {
-    const uint64_t u = s.sums[0][i], v = s.sums[1][i];
-    pa += i < wave ? u : 0;
-    pb += i < wave ? v : 0;
-    ta += u;
-    tb += v;
-  }
-  *before_a = pa + x - a;
-  *before_b = pb + y - b;
-  *va = ta;
-  *vb = tb;
-}
-template <class S>
-__device__ __forceinline__ uint64_t block_scan(uint64_t v, S& s, uint64_t* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t x = wave_scan(v);
-  __syncthreads();
-  if (lane == 63) s.sums[0][wave] = x;
-  __syncthreads();
-  uint64_t before = 0, all = 0;
-#pragma unroll
-  for (int i = 0; i < SM_NW; ++i) {
-    const uint64_t y = s.sums[0][i];
-    before += i < wave ? y : 0;
-    all += y;
-  }
-  *total = all;
-  return before + x - v;
+  *before_a = block_scan(a, s, va);
+  *before_b = block_scan(b, s, vb, 1);
 }
 __device__ __forceinline__ uint64_t block_add(uint64_t v, Lds& s) {
   uint64_t all;
@@ -429,7 +422,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   clear<sizeof(s.counts)>(s.counts);
   float mine = -INFINITY;
   bool nan = false;
-  r.each([&](int, const float* x) SM_INLINE {
+  r.template each<SM_U>([&](int, const float* x) SM_INLINE {
 #pragma unroll
     for (int i = 0; i < E; i += 2) {
       mine = fmaxf(mine, fmaxf(x[i], x[i + 1]));
@@ -467,7 +460,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
 
   if (greedy) {
     int at = INT32_MAX;
-    r.each([&](int base, const float* x) SM_INLINE {
+    r.template each<1>([&](int base, const float* x) SM_INLINE {
 #pragma unroll
       for (int i = E - 1; i >= 0; --i) {
         if (x[i] == top) at = min(at, base + i);
@@ -523,7 +516,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       if (tid == 0) v.ids = 0;
       __syncthreads();
       auto at2 = [&](uint32_t u) SM_INLINE { return __builtin_bit_cast(uint32_t, falling2(u) - from); };
-      r.raw(
+      r.template raw<SM_U>(
           [&](int, const uint4& u) SM_INLINE {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -536,9 +529,11 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       __syncthreads();
       auto count_of = [&](uint32_t b) SM_INLINE { return b == SV_N - 1 || b == none ? 0u : v.hist[b]; };
       auto weight_of = [&](uint32_t b) SM_INLINE { return w.whole(of_falling16(first_key + b)); };
+      uint32_t next = count_of(tid);
 #pragma unroll 1
       for (int i = 0; i < SV_N / SM_NT; ++i) {
-        const uint32_t b = i * SM_NT + tid, c = count_of(b);
+        const uint32_t b = i * SM_NT + tid, c = next;
+        next = count_of(min(b + SM_NT, (uint32_t)SV_N - 1));
         uint64_t n = 0, mass = 0;
         if (__any(c != 0)) n = wave_scan(c), mass = wave_scan(c * weight_of(b));
         if (lane == 63) v.part.n[i * SM_NW + wave] = (uint32_t)n, v.part.mass[i * SM_NW + wave] = mass;
@@ -570,26 +565,32 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
         __syncthreads();
       };
       const bool k_cuts = k_on && n_all >= (uint64_t)top_k;
-      if (k_cuts) locate(true, top_k);
-      if (p_on) locate(false, p_goal(kept_mass));
+#pragma unroll 1
+      for (int by = 0; by < 2; ++by)
+        if (by == 0 ? k_cuts : p_on) locate(by == 0, by == 0 ? (uint64_t)top_k : p_goal(kept_mass));
       if (!k_cuts && !p_on) end = min(none, (uint32_t)SV_N - 1);   // all
       if (least.l > -INFINITY) {
         const uint32_t u = __float_as_uint(least.l), behind = falling16((u >> 31 ? u : u + 0xffffu) >> 16) - first_key + 1;
         if (behind <= end) end = behind, ties = 0;
       }
-      // the kept values' weights
+      // the kept values' weights, and for every value the place of its weight: the others' is 0
       uint64_t kept_n = 0;
       kept_mass = 0;
-      for (uint32_t b = tid; b < end; b += SM_NT) {
-        const uint32_t c = count_of(b);
-        if (!c) continue;
-        const uint64_t y = weight_of(b);
-        const uint32_t id = atomicAdd(&v.ids, 1u);
-        if (id < SV_IDS) v.weight[id] = y;
-        v.hist[b] = id;
-        kept_n += c;
-        kept_mass += c * y;
+      for (uint32_t b = tid; b < SV_N; b += SM_NT) {
+        uint32_t place = SV_IDS;
+        if (b < end) {
+          const uint32_t c = count_of(b);
+          if (c) {
+            const uint64_t y = weight_of(b);
+            place = atomicAdd(&v.ids, 1u);
+            if (place < SV_IDS) v.weight[place] = y;
+            kept_n += c;
+            kept_mass += c * y;
+          }
+        }
+        v.hist[b] = place * 8;
       }
+      if (tid == 0) v.weight[SV_IDS] = 0;
       uint64_t t0, t1, kept_all, mass_kept;
       block_scan2(kept_n, kept_mass, v, &t0, &kept_all, &t1, &mass_kept);
       mass_kept += ties * each;
@@ -598,7 +599,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       const bool table = v.ids <= SV_IDS;
       uint64_t part = 0;
       uint32_t equal = 0;
-      r.raw(
+      r.template raw<1>(
           [&](int, const uint4& u) SM_INLINE {
             uint32_t k[E];
 #pragma unroll
@@ -606,25 +607,22 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
               const uint32_t both = at2(((const uint32_t*)&u)[i]);
               k[2 * i] = both & 0xffffu, k[2 * i + 1] = both >> 16;
             }
-            uint32_t least_k = k[0];
-#pragma unroll
-            for (int i = 1; i < E; ++i) least_k = min(least_k, k[i]);
             if (ties) {
 #pragma unroll
               for (int i = 0; i < E; ++i) equal += k[i] == end;
             }
-            if (!__any(least_k < end)) return;
             if (table) {
 #pragma unroll
-              for (int i = 0; i < E; ++i) k[i] = k[i] < end ? v.hist[k[i]] : ~0u;
+              for (int i = 0; i < E; ++i) k[i] = v.hist[min(k[i], (uint32_t)SV_N - 1)];
 #pragma unroll
-              for (int i = 0; i < E; ++i) {
-                const uint64_t y = v.weight[min(k[i], (uint32_t)SV_IDS - 1)];
-                part += k[i] != ~0u ? y : 0;
-              }
+              for (int i = 0; i < E; ++i) part += *(const uint64_t*)((const char*)v.weight + k[i]);
             } else {
+#pragma unroll 1
+              for (int i = 0; i < E; ++i) {
+                part += k[0] < end ? weight_of(k[0]) : 0;
 #pragma unroll
-              for (int i = 0; i < E; ++i) part += k[i] < end ? weight_of(k[i]) : 0;
+                for (int j = 0; j < E - 1; ++j) k[j] = k[j + 1];
+              }
             }
           },
           [&](int seg) SM_INLINE {
@@ -652,20 +650,19 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
         }
         uint64_t c = lo ? v.seg[lo - 1] : 0, tied = v.ties[lo];
         const int steps = r.segment_steps(lo);
-        uint4 u[SM_U];
-#pragma unroll
-        for (int j = 0; j < SM_U; ++j) u[j] = r.fetch(j < steps ? r.segment_base(lo, j) : a.vocab);
-#pragma unroll
-        for (int j = 0; j < SM_U; ++j) {
-          if (j >= steps) break;
+        uint4 next = r.fetch(r.segment_base(lo, 0));
+#pragma unroll 1
+        for (int j = 0; j < steps; ++j) {
+          const uint4 u = next;
+          next = r.fetch(r.segment_base(lo, j + 1));
           float x[E];
           uint64_t z[E], of_lane = 0, equal_lane = 0;
           uint32_t k[E];
           const int base = r.segment_base(lo, j);
-          r.floats(u[j], x);
+          r.floats(u, x);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t both = at2(((const uint32_t*)&u[j])[i]);
+            const uint32_t both = at2(((const uint32_t*)&u)[i]);
             k[2 * i] = both & 0xffffu, k[2 * i + 1] = both >> 16;
           }
 #pragma unroll
@@ -706,7 +703,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   uint64_t before = 0;
   bool counted = false, have_all = false;
   auto count_bins = [&]() SM_INLINE {                // the bin of top-k's cut; false where there are no more tokens than that
-    r.each([&](int, const float* x) SM_INLINE {
+    r.template each<SM_U>([&](int, const float* x) SM_INLINE {
 #pragma unroll
       for (int i = 0; i < E; ++i)
         if (x[i] > -INFINITY) atomicAdd(&s.counts[bin_of(depth(top, x[i]))], 1u);
@@ -743,7 +740,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       if (n) atomicAdd((unsigned long long*)&s.bins[bin_of(depth(top, x))], (unsigned long long)((kOne + n) * times));
     };
     if (mine > -INFINITY) note(mine, 1);
-    r.each([&](int, const float* x) SM_INLINE {
+    r.template each<1>([&](int, const float* x) SM_INLINE {
       if (x[0] != mine && x[0] > -INFINITY) note(x[0], E);
     });
     __syncthreads();
@@ -783,7 +780,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     int n = 0;
     uint64_t sum = 0;
     __syncthreads();
-    r.each([&](int base, const float* x) SM_INLINE {
+    r.template each<1>([&](int base, const float* x) SM_INLINE {
       uint64_t is[E], any = 0;
 #pragma unroll
       for (int i = 0; i < E; ++i) {
@@ -823,14 +820,18 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   if (last >= 0 && few && list_bins(0, last, s.list.logit[wave], s.list.token[wave], SM_LIST, logprob_out || (p_on && !k_on))) {
     const int per = (e.n + 63) / 64, begin = min(lane * per, e.n), end = min(begin + per, e.n);
     bool fine = true;
-    if (k_on && listed_all > (uint64_t)top_k) cut = cut_list(e, cut, true, top_k, w, s);
-    if (p_on) {
-      uint64_t mass = 0;
-      for (int i = begin; i < end; ++i) mass += cut.keeps(e.logit[i], e.token[i]) ? w.whole(e.logit[i]) : 0;
-      mass = block_add(mass, s);
-      const uint64_t goal = p_goal(k_on ? mass : all);
-      fine = goal <= mass;                 // the guess was far enough
-      if (fine) cut = cut_list(e, cut, false, goal, w, s);
+#pragma unroll 1
+    for (int by = k_on && listed_all > (uint64_t)top_k ? 0 : 1; by < (p_on ? 2 : 1); ++by) {
+      uint64_t goal = top_k;
+      if (by == 1) {
+        uint64_t mass = 0;
+        for (int i = begin; i < end; ++i) mass += cut.keeps(e.logit[i], e.token[i]) ? w.whole(e.logit[i]) : 0;
+        mass = block_add(mass, s);
+        goal = p_goal(k_on ? mass : all);
+        fine = goal <= mass;               // the guess was far enough
+        if (!fine) break;
+      }
+      cut = cut_list(e, cut, by == 0, goal, w, s);
     }
     if (fine) {
       cut = tighter(cut);
@@ -855,9 +856,6 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   }
 
   // ---- many tokens: each cut's bin, then its list
-  auto narrow = [&](bool sum_all) SM_INLINE {
-    return list_bins(last, last, s.narrow.logit[wave], s.narrow.token[wave], SM_NARROW, sum_all);
-  };
   // (a bin too full for the lists: digits over the row)
   auto cut_row = [&](bool by_count, uint64_t rest) SM_INLINE {
     const Cut in = cut;
@@ -869,7 +867,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       __syncthreads();
       clear<sizeof(s.fine)>(s.fine);
       __syncthreads();
-      r.each([&](int base, const float* x) SM_INLINE {
+      r.template each<1>([&](int base, const float* x) SM_INLINE {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           const uint32_t k = falling(x[i]);
@@ -886,7 +884,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     // the last of the kept ones at the cut's logit: its segment, then its step
     __syncthreads();
     uint64_t n = 0, t;
-    r.each(
+    r.template each<1>(
         [&](int base, const float* x) SM_INLINE {
 #pragma unroll
           for (int i = 0; i < E; ++i) n += __popcll(__ballot(x[i] == l && in.keeps(l, base + i)));
@@ -926,7 +924,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   auto weigh = [&](int from, int to, bool sum_all) SM_INLINE {
     const uint32_t lo = bin_begin(from), width = bin_end(to) - lo;
     uint64_t sum = 0;
-    r.each([&](int base, const float* x) SM_INLINE {
+    r.template each<1>([&](int base, const float* x) SM_INLINE {
       bool in[E], some = sum_all;
 #pragma unroll
       for (int i = 0; i < E; ++i) some |= in[i] = depth(top, x[i]) - lo < width && cut.keeps(x[i], base + i);
@@ -950,26 +948,25 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     }
     __syncthreads();
   }
-  if (k_on) {
-    const int bin = last;
-    const bool fits = narrow(false);
-    cut = fits ? cut_list(e, cut, true, top_k - before, w, s) : cut_row(true, top_k - before);
-    if (p_on) weigh(0, bin, logprob_out && !have_all);
-  } else if (p_on) {
-    weigh(0, SM_BINS - 1, !have_all);
-  }
-  if (p_on) {
-    uint64_t goal = 0;
-    find_bin<SM_BINS>(s.bins, s, [&](uint64_t mass) SM_INLINE { return goal = p_goal(mass); });
-    last = s.found, before = s.found_before;
-    const bool fits = narrow(false);
-    cut = fits ? cut_list(e, cut, false, goal - before, w, s) : cut_row(false, goal - before);
+  const int k_bin = k_on ? last : SM_BINS - 1;
+#pragma unroll 1
+  for (int by = 0; by < 2; ++by) {
+    uint64_t goal = top_k;
+    if (!(by == 0 ? k_on : p_on)) continue;
+    if (by == 1) {
+      weigh(0, k_bin, !have_all && (logprob_out || !k_on));
+      find_bin<SM_BINS>(s.bins, s, [&](uint64_t mass) SM_INLINE { return goal = p_goal(mass); });
+      last = s.found, before = s.found_before;
+    }
+    goal -= before;
+    const bool fits = list_bins(last, last, s.narrow.logit[wave], s.narrow.token[wave], SM_NARROW, false);
+    cut = fits ? cut_list(e, cut, by == 0, goal, w, s) : cut_row(by == 0, goal);
   }
   cut = tighter(cut);
   uint64_t sum = 0, n = 0, part = 0;
   const bool sum_all = logprob_out && !have_all;
   __syncthreads();
-  r.each(
+  r.template each<1>(
       [&](int base, const float* x) SM_INLINE {
         bool in[E], some = sum_all;
 #pragma unroll
@@ -1005,16 +1002,15 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     }
     uint64_t c = lo ? s.seg[lo - 1] : 0;
     const int steps = r.segment_steps(lo);
-    uint4 u[SM_U];
-#pragma unroll
-    for (int j = 0; j < SM_U; ++j) u[j] = r.fetch(j < steps ? r.segment_base(lo, j) : a.vocab);
-#pragma unroll
-    for (int j = 0; j < SM_U; ++j) {
-      if (j >= steps) break;
+    uint4 next = r.fetch(r.segment_base(lo, 0));
+#pragma unroll 1
+    for (int j = 0; j < steps; ++j) {
+      const uint4 u = next;
+      next = r.fetch(r.segment_base(lo, j + 1));
       float x[E];
       uint64_t z[E], of_lane = 0;
       const int base = r.segment_base(lo, j);
-      r.floats(u[j], x);
+      r.floats(u, x);
 #pragma unroll
       for (int i = 0; i < E; ++i) of_lane += z[i] = cut.keeps(x[i], base + i) ? w.whole(x[i]) : 0;
       const uint64_t scanned = wave_scan(of_lane);
