@@ -415,6 +415,8 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   int32_t top_k = has && a.top_k ? a.top_k[set] : 0;
   const float top_p = has && a.top_p ? a.top_p[set] : 1.f, min_p = has && a.min_p ? a.min_p[set] : 0.f;
 
+  const float uniform = lane < a.draws ? a.u[(int64_t)row * a.draws + lane] : 0.f;
+
   // the largest logit
   if (tid < SM_TAB) s.tab[tid] = ldexp(exp2((double)tid / SM_TAB), unit);
   if (tid == 0) s.bad = 0, s.first = INT32_MAX;
@@ -454,7 +456,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     if (logprob_out) logprob_out[d] = (float)(w.place(l) / kScale - log(ldexp((double)all, -unit)));
   };
   auto goal_of = [&](int d, uint64_t mass) SM_INLINE {
-    const float u = a.u[(int64_t)row * a.draws + d];
+    const float u = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(uniform), d));
     return min((uint64_t)((u > 0.f ? fmin((double)u, 1.0 - 0x1p-24) : 0.0) * (double)mass), mass - 1);
   };
 
@@ -529,14 +531,23 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       __syncthreads();
       auto count_of = [&](uint32_t b) SM_INLINE { return b == SV_N - 1 || b == none ? 0u : v.hist[b]; };
       auto weight_of = [&](uint32_t b) SM_INLINE { return w.whole(of_falling16(first_key + b)); };
-      uint32_t next = count_of(tid);
+      // (three at a time, as most hold nothing)
+      constexpr int W = 3;
+      static_assert(SV_N % (W * SM_NT) == 0, "");
 #pragma unroll 1
-      for (int i = 0; i < SV_N / SM_NT; ++i) {
-        const uint32_t b = i * SM_NT + tid, c = next;
-        next = count_of(min(b + SM_NT, (uint32_t)SV_N - 1));
-        uint64_t n = 0, mass = 0;
-        if (__any(c != 0)) n = wave_scan(c), mass = wave_scan(c * weight_of(b));
-        if (lane == 63) v.part.n[i * SM_NW + wave] = (uint32_t)n, v.part.mass[i * SM_NW + wave] = mass;
+      for (int i = 0; i < SV_N / SM_NT; i += W) {
+        uint32_t c[W], any = 0;
+#pragma unroll
+        for (int j = 0; j < W; ++j) any |= c[j] = count_of((i + j) * SM_NT + tid);
+        const bool some = __any(any != 0);
+#pragma unroll 1
+        for (int j = i; j < i + W; ++j) {
+          uint64_t n = 0, mass = 0;
+          if (some) n = wave_scan(c[0]), mass = wave_scan(c[0] * weight_of(j * SM_NT + tid));
+          if (lane == 63) v.part.n[j * SM_NW + wave] = (uint32_t)n, v.part.mass[j * SM_NW + wave] = mass;
+#pragma unroll
+          for (int m = 0; m < W - 1; ++m) c[m] = c[m + 1];
+        }
       }
       __syncthreads();
       const bool has_part = tid < SV_N / 64;
@@ -576,20 +587,22 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       // the kept values' weights, and for every value the place of its weight: the others' is 0
       uint64_t kept_n = 0;
       kept_mass = 0;
-      for (uint32_t b = tid; b < SV_N; b += SM_NT) {
+      const int kept_steps = ((int)end + SM_NT - 1) / SM_NT;
+#pragma unroll 1
+      for (int i = 0; i < kept_steps; ++i) {
+        const uint32_t b = i * SM_NT + tid, c = b < end ? count_of(b) : 0;
         uint32_t place = SV_IDS;
-        if (b < end) {
-          const uint32_t c = count_of(b);
-          if (c) {
-            const uint64_t y = weight_of(b);
-            place = atomicAdd(&v.ids, 1u);
-            if (place < SV_IDS) v.weight[place] = y;
-            kept_n += c;
-            kept_mass += c * y;
-          }
+        if (c) {
+          const uint64_t y = weight_of(b);
+          place = atomicAdd(&v.ids, 1u);
+          if (place < SV_IDS) v.weight[place] = y;
+          kept_n += c;
+          kept_mass += c * y;
         }
         v.hist[b] = place * 8;
       }
+      for (int i = kept_steps * (SM_NT / 4) + tid; i < SV_N / 4; i += SM_NT)
+        ((uint4*)v.hist)[i] = uint4{SV_IDS * 8, SV_IDS * 8, SV_IDS * 8, SV_IDS * 8};
       if (tid == 0) v.weight[SV_IDS] = 0;
       uint64_t t0, t1, kept_all, mass_kept;
       block_scan2(kept_n, kept_mass, v, &t0, &kept_all, &t1, &mass_kept);
@@ -599,7 +612,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       const bool table = v.ids <= SV_IDS;
       uint64_t part = 0;
       uint32_t equal = 0;
-      r.template raw<1>(
+      r.template raw<SM_U>(
           [&](int, const uint4& u) SM_INLINE {
             uint32_t k[E];
 #pragma unroll
@@ -648,18 +661,20 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
           const int mid = (lo + hi) / 2;
           if (v.seg[mid] > goal) hi = mid; else lo = mid + 1;
         }
-        uint64_t c = lo ? v.seg[lo - 1] : 0, tied = v.ties[lo];
+        uint64_t c = lo ? v.seg[lo - 1] : 0;
+        uint32_t tied = v.ties[lo];
         const int steps = r.segment_steps(lo);
-        uint4 next = r.fetch(r.segment_base(lo, 0));
+        uint4 ahead[SM_U];
+#pragma unroll
+        for (int j = 0; j < SM_U; ++j) ahead[j] = r.fetch(j < steps ? r.segment_base(lo, j) : a.vocab);
 #pragma unroll 1
         for (int j = 0; j < steps; ++j) {
-          const uint4 u = next;
-          next = r.fetch(r.segment_base(lo, j + 1));
-          float x[E];
-          uint64_t z[E], of_lane = 0, equal_lane = 0;
-          uint32_t k[E];
+          const uint4 u = ahead[0];
+#pragma unroll
+          for (int m = 0; m < SM_U - 1; ++m) ahead[m] = ahead[m + 1];
+          uint64_t z[E], of_lane = 0;
+          uint32_t k[E], equal_lane = 0;
           const int base = r.segment_base(lo, j);
-          r.floats(u, x);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t both = at2(((const uint32_t*)&u)[i]);
@@ -667,23 +682,26 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
           }
 #pragma unroll
           for (int i = 0; i < E; ++i) equal_lane += k[i] == end;
-          const uint64_t scanned_ties = wave_scan(equal_lane);
-          uint64_t nth = tied + scanned_ties - equal_lane;
+          const uint32_t scanned_ties = (uint32_t)wave_scan(equal_lane);
+          uint32_t nth = tied + scanned_ties - equal_lane;
+          tied += __builtin_amdgcn_readlane(scanned_ties, 63);
 #pragma unroll
           for (int i = 0; i < E; ++i) {
-            const bool in = k[i] < end || (k[i] == end && nth < ties);
-            nth += k[i] == end;
-            of_lane += z[i] = in ? w.whole(x[i]) : 0;
+            z[i] = table ? *(const uint64_t*)((const char*)v.weight + v.hist[min(k[i], (uint32_t)SV_N - 1)]) : k[i] < end ? weight_of(k[i]) : 0;
+            if (k[i] == end && nth++ < ties) z[i] = each;
+            of_lane += z[i];
           }
           const uint64_t scanned = wave_scan(of_lane);
           uint64_t at = c + scanned - of_lane;
+          int chosen = -1;
+          uint32_t chosen_key = 0;
 #pragma unroll
           for (int i = 0; i < E; ++i) {
-            if (at <= goal && goal < at + z[i]) answer(d, base + i, x[i]);
+            if (at <= goal && goal < at + z[i]) chosen = i, chosen_key = k[i];
             at += z[i];
           }
           c += lane_value(scanned, 63);
-          tied += lane_value(scanned_ties, 63);
+          if (chosen >= 0) answer(d, base + chosen, of_falling16(first_key + chosen_key));
         }
       }
       return true;
@@ -1002,11 +1020,14 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     }
     uint64_t c = lo ? s.seg[lo - 1] : 0;
     const int steps = r.segment_steps(lo);
-    uint4 next = r.fetch(r.segment_base(lo, 0));
+    uint4 ahead[SM_U];
+#pragma unroll
+    for (int j = 0; j < SM_U; ++j) ahead[j] = r.fetch(j < steps ? r.segment_base(lo, j) : a.vocab);
 #pragma unroll 1
     for (int j = 0; j < steps; ++j) {
-      const uint4 u = next;
-      next = r.fetch(r.segment_base(lo, j + 1));
+      const uint4 u = ahead[0];
+#pragma unroll
+      for (int m = 0; m < SM_U - 1; ++m) ahead[m] = ahead[m + 1];
       float x[E];
       uint64_t z[E], of_lane = 0;
       const int base = r.segment_base(lo, j);
