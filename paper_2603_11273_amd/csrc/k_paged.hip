@@ -194,7 +194,7 @@ void k_attend_pages(PagedArgs a) {
   if (u >= a.units) return;
   const int head = (int)(u % a.c.c.kv_heads);
   u /= a.c.c.kv_heads;
-  const int part = (int)(u % a.c.parts), seq = (int)(u / a.c.parts);
+  const int seq = (int)(u % a.c.c.sequences), part = (int)(u / a.c.c.sequences);
   int start, count;
   rows_of(a.c, seq, &start, &count);
   if (col0 >= count * a.per) return;

@@ -219,6 +219,30 @@ asr_status check_pages(const asr_pages& c, Pages* p) {
 // of each of its wave's blocks.
 constexpr int kPartStep = 4 * kPageBlock, kMostPart = 64 * kPartStep;
 
+// Keys per part, `keys` at most for each of `units` (a sequence's queries and a cache
+// head).  With P parts of n keys the call takes the turns of equal units, of n and what a
+// part costs besides (`fixed` keys' worth) each; units of all lengths up to `keys` take
+// their average share, the last parts, which end alone, and the parts' costs; a second
+// kernel joins more than one part.  Whether lengths differ is not known here, so P is
+// least for the sum of both.  Measured (us, bf16, by parts of 2048 / 4096 / 8192 keys):
+// 64 x 8 units of 515 to 8191 keys 60 / 61 / 67, all of 8191 92 / 86 / 84; 16 x 8 of 65536
+// 171 / 168 / 166; 24 x 8 of 6000 39 / 35 / 35; the rule's: @RULE@.
+int paged_part(int64_t units, int64_t keys, bool ragged, int fixed) {
+  const int64_t cus = cu_count(), least = std::max<int64_t>(1, (keys + kMostPart - 1) / kMostPart);
+  const int64_t most = std::max(least, std::min<int64_t>((keys + kPartStep - 1) / kPartStep, 8 * cus / units));
+  int64_t best = kPartStep;
+  double best_cost = HUGE_VAL;
+  for (int64_t p = least; p <= most; ++p) {
+    const int64_t n = std::max<int64_t>(1, ((keys + p - 1) / p + kPartStep - 1) / kPartStep) * kPartStep;
+    const int64_t blocks = units * ((keys + n - 1) / n);
+    double cost = (double)((blocks + cus - 1) / cus) * (double)(n + fixed) + (blocks > units ? 600 : 0);
+    if (ragged)
+      cost += (double)units * keys / (2.0 * cus) + 0.75 * n + fixed * std::max(1.0, blocks / (2.0 * cus)) + (blocks > units ? 600 : 0);
+    if (cost < best_cost) best = n, best_cost = cost;
+  }
+  return (int)best;
+}
+
 asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* bytes) {
   if (!a) return fail(ASR_EINVAL, "NULL argument");
   if (a->dtype != ASR_F32 && a->dtype != ASR_BF16) return fail(ASR_EINVAL, "dtype");
@@ -240,11 +264,7 @@ asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* byte
   if (a->part_keys) {
     s->part = a->part_keys;
   } else {
-    const int fixed = (int)(200 + 10 * std::min<int64_t>(cols, 64)) * 2;
-    const bool ragged = a->cache.sequences > 1;
-    s->part = part_keys(std::max<int64_t>(units, 1), most, ragged, fixed, kPartStep);
-    if (ragged) s->part = part_keys_ragged(units, most, s->part, fixed, 20, kPartStep);
-    s->part = std::min(s->part, kMostPart);
+    s->part = paged_part(std::max<int64_t>(units, 1), most, a->cache.sequences > 1, 400 + 20 * (int)std::min<int64_t>(cols, 64));
   }
   s->parts = std::max(parts_of((int)most, s->part), 1);
   const double blocks = ((double)units * s->parts + 8.0 * tiles);
