@@ -667,8 +667,8 @@ asr_status asr_write_pages(const asr_page_write* w, void* stream);
  * or the table ends there; a row without any key gives zeros.  What a row does not
  * see does not touch it, NaN codes included; what it sees makes it NaN as the
  * formula does.  Sums are float32; a row's bits depend neither on the other rows nor
- * on its place (with part_keys given; 0 lets the library split by the size of the
- * call).
+ * on its place (with part_keys given; 0 lets the library split the work by the call's
+ * size and, under windows, by what the rows see).
  *   q: float32 [rows][n_head * 64], rows q_ld apart; out of type dtype, rows
  * out_ld apart (both 16-byte aligned, q_ld and out_ld multiples of 4). */
 typedef struct {

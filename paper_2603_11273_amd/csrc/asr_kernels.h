@@ -272,6 +272,7 @@ struct PagedLaunch {
   int32_t n_head, rows, max_rows, max_keys, part, parts;
   float* rec;
   int64_t blocks;
+  bool even;                   // parts are of what a tile's queries see, not of positions
   uint32_t* counters;          // one per sequence and cache head (queries of one tile), or NULL: a second kernel joins
 };
 void attend_pages(const PagedLaunch& a, bool bf16, hipStream_t s);

@@ -200,8 +200,25 @@ void k_attend_pages(PagedArgs a) {
   if (col0 >= count * a.per) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int m = lane & 15, g = lane >> 4;
-  const int k0 = part * a.c.part;
-  const int bound = (int)min((int64_t)k0 + a.c.part, (int64_t)a.c.max_keys);
+  int k0 = part * a.c.part;
+  int bound = (int)min((int64_t)k0 + a.c.part, (int64_t)a.c.max_keys);
+  if (a.c.even) {
+    // equal parts of what the tile's queries see
+    int lo = INT32_MAX, hi = 0;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const int j = (col0 + 16 * t + m) / a.per;
+      if (j >= count) continue;
+      const int f = max(a.c.first[start + j], 0), e = min(a.c.length[start + j], a.c.max_keys);
+      if (f < e) lo = min(lo, f), hi = max(hi, e);
+    }
+    lo = (int)~wave_max_u32(~(uint32_t)lo) & -kPageBlock;
+    hi = (int)wave_max_u32((uint32_t)hi);
+    const int n = max(((hi - lo + a.c.parts - 1) / a.c.parts + kPageBlock - 1) / kPageBlock, PA_NW) * kPageBlock;
+    k0 = hi > lo ? (int)min((int64_t)lo + (int64_t)part * n, (int64_t)hi & -kPageBlock) : 0;
+    bound = hi > lo ? (int)min((int64_t)lo + (int64_t)(part + 1) * n, (int64_t)hi) : 0;
+    if (hi > lo && (int64_t)lo + (int64_t)part * n >= hi) bound = k0;       // (nothing left for it)
+  }
 
   // the wave's blocks of keys: lane i knows the i-th's page
   const int per = a.c.c.page / kPageBlock;

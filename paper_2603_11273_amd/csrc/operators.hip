@@ -226,7 +226,7 @@ constexpr int kPartStep = 4 * kPageBlock, kMostPart = 64 * kPartStep;
 // kernel joins more than one part.  Whether lengths differ is not known here, so P is
 // least for the sum of both.  Measured (us, bf16, by parts of 2048 / 4096 / 8192 keys):
 // 64 x 8 units of 515 to 8191 keys 60 / 61 / 67, all of 8191 92 / 86 / 84; 16 x 8 of 65536
-// 171 / 168 / 166; 24 x 8 of 6000 39 / 35 / 35; the rule's: @RULE@.
+// 171 / 168 / 166; 24 x 8 of 6000 39 / 35 / 35; the rule's: 61, 86, 168, 35.
 int paged_part(int64_t units, int64_t keys, bool ragged, int fixed) {
   const int64_t cus = cu_count(), least = std::max<int64_t>(1, (keys + kMostPart - 1) / kMostPart);
   const int64_t most = std::max(least, std::min<int64_t>((keys + kPartStep - 1) / kPartStep, 8 * cus / units));
@@ -283,6 +283,9 @@ asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* byte
   s->max_rows = a->row_start ? a->max_rows : 1;
   s->max_keys = (int32_t)most;
   s->blocks = (int64_t)units * s->parts;
+  // (windows: positions would leave most parts nothing; 7 chunks of up to 33 rows on up to
+  // 4001 keys, windows of 1000: 19.8 -> 15.9 us)
+  s->even = a->first && !a->part_keys && s->parts > 1;
   *bytes = s->parts > 1 ? kCounters * 4 + (size_t)a->rows * a->n_head * s->parts * (kHeadDim + 2) * 4 : 0;
   return ASR_OK;
 }
