@@ -329,7 +329,7 @@ class _Operator:
         """A tensor's checks (contiguous; with ld, rows that are); its address."""
         if t is None:
             return None
-        if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        if t.dtype != dtype or t.shape != shape or t.device != device:
             raise TypeError(f"{name} must be {dtype} of shape {tuple(shape)} on {device}")
         if not (t.is_contiguous() or (ld and t.stride(-1) == 1)):
             raise TypeError(f"{name} must be contiguous")
@@ -348,7 +348,9 @@ class _Operator:
             self._ws.record_stream(torch.cuda.current_stream(self._dev) if stream is None else stream)
             self._streams.add(st)
         if torch.cuda.current_device() == self._dev.index:
-            _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st))
+            e = self._run(self._ref, self._ws_ptr, self._ws_bytes, st)
+            if e:
+                _check(e)
             return
         with torch.cuda.device(self._dev):
             _check(self._run(self._ref, self._ws_ptr, self._ws_bytes, st))

@@ -140,8 +140,8 @@ struct Weights {
   double top, c;           // 512 log2(e) / T
   double least;            // of what weighs less than an eighth of a unit
   __device__ __forceinline__ double place(float l) const { return ((double)l - top) * c; }
-  __device__ __forceinline__ uint64_t whole(float l) const {
-    const double y = fmax(place(l), least);                // (0 times -inf, too)
+  __device__ __forceinline__ double weight(float l) const {
+    const double y = fmax(place(l), least);          // (0 times -inf, too)
     constexpr double kMagic = 6755399441055744.0;          // 1.5 * 2^52: the nearest whole number is in the low bits
     const double t = y + kMagic;
     const int k = __double2loint(t);
@@ -149,9 +149,12 @@ struct Weights {
     constexpr double a1 = 6.93147180559945286e-01 / 512, a2 = a1 * a1 / 2, a3 = a1 * a1 * a1 / 6;   // (the next term: 9e-15)
     const double e = tab[k & (SM_TAB - 1)];
     const double v = fma(fma(fma(a3, r, a2), r, a1), r * e, e);
-    // times 2^(k / 512), in the exponent; 2^52 leaves the whole number in the low bits
-    const double z = __hiloint2double(__double2hiint(v) + (int)((uint32_t)(k & ~(SM_TAB - 1)) << 11), __double2loint(v));
-    return (uint64_t)__double_as_longlong(z + 4503599627370496.0) & 0xfffffffffffffull;
+    // times 2^(k / 512), in the exponent
+    return __hiloint2double(__double2hiint(v) + (int)((uint32_t)(k & ~(SM_TAB - 1)) << 11), __double2loint(v));
+  }
+  // 2^52 leaves the whole number in the low bits
+  __device__ __forceinline__ uint64_t whole(float l) const {
+    return (uint64_t)__double_as_longlong(weight(l) + 4503599627370496.0) & 0xfffffffffffffull;
   }
 };
 
@@ -462,6 +465,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
 
   if (greedy) {
     int at = INT32_MAX;
+    double whole_row = 0.0;
     r.template each<1>([&](int base, const float* x) SM_INLINE {
 #pragma unroll
       for (int i = E - 1; i >= 0; --i) {
@@ -469,11 +473,11 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       }
       if (logprob_out) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) all += w.whole(x[i]);
+        for (int i = 0; i < E; ++i) whole_row += w.weight(x[i]);
       }
     });
     if (at < INT32_MAX) atomicMin(&s.first, at);
-    all = block_add(all, s);
+    all = block_add((uint64_t)whole_row, s);
     if (tid < a.draws) answer(tid, s.first, top);
     if (tid == 0 && a.kept) a.kept[row] = 1;
     return;
@@ -796,7 +800,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   auto list_bins = [&](int from, int to, float* logit, int32_t* token, int room, bool sum_all) SM_INLINE {
     const uint32_t lo = bin_begin(from), width = bin_end(to) - lo;
     int n = 0;
-    uint64_t sum = 0;
+    double sum = 0.0;                      // (a lane's, in the order of its tokens: always the same)
     __syncthreads();
     r.template each<1>([&](int base, const float* x) SM_INLINE {
       uint64_t is[E], any = 0;
@@ -807,7 +811,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       }
       if (sum_all) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) sum += w.whole(x[i]);
+        for (int i = 0; i < E; ++i) sum += w.weight(x[i]);
       }
       if (any) {
         uint32_t at = n;
@@ -829,7 +833,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     });
     e = {logit, token, n};
     uint64_t t0, sum_of, over;
-    block_scan2(sum, lane == 0 ? (n > room ? 1ull << 32 : 0) + (uint64_t)n : 0, s, &t0, &sum_of, &t0, &over);
+    block_scan2((uint64_t)sum, lane == 0 ? (n > room ? 1ull << 32 : 0) + (uint64_t)n : 0, s, &t0, &sum_of, &t0, &over);
     if (sum_all) all = sum_of, have_all = true;
     listed_all = over & 0xffffffffu;
     return over >> 32 == 0;
