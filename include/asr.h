@@ -744,10 +744,11 @@ asr_status asr_next_tables(const asr_page_tables* t, void* ws, size_t ws_bytes, 
  * the first is always kept.  A temperature that is not above 0 keeps only the first, and
  * T counts as 1.  Draw d of the row is the first kept token v, by number, at which the kept
  * weights up to v sum to more than u[r][d] times their whole sum (u below 0 or NaN counts
- * as 0, 1 and above as the float32 below 1).  Sums are of weights (formed to 2^-44 of
- * themselves) rounded to multiples of 2^-50, or of 2^(n - 62) where the vocabulary is above
- * 2^12 and 2^n the power of two not below it, in whole numbers, so neither the work's
- * split nor its order can change a token.
+ * as 0, 1 and above as the float32 below 1).  Weights are formed to 2^-44 of themselves and
+ * rounded to multiples of 2^-50, or of 2^(n - 62) where the vocabulary is above 2^12 and 2^n
+ * the power of two not below it; sums of kept ones are whole numbers of these, those of a whole
+ * row may be doubles instead (2^-47 of the sum), always added in the same order.  So neither
+ * the other rows nor the work's split can change a token.
  *   token [rows][draws]; logprob [rows][draws] or NULL: (l - M) / T - log sum over all v of
  * w_v, in float32; kept [rows] or NULL: tokens kept.  A row whose logits hold a NaN or
  * +inf, or only -inf, gives token -1, kept 0 and logprob NaN (only -inf: -inf).

@@ -218,6 +218,8 @@ void k_attend_pages(PagedArgs a) {
     k0 = hi > lo ? (int)min((int64_t)lo + (int64_t)part * n, (int64_t)hi & -kPageBlock) : 0;
     bound = hi > lo ? (int)min((int64_t)lo + (int64_t)(part + 1) * n, (int64_t)hi) : 0;
     if (hi > lo && (int64_t)lo + (int64_t)part * n >= hi) bound = k0;       // (nothing left for it)
+    k0 = __builtin_amdgcn_readfirstlane(k0);
+    bound = __builtin_amdgcn_readfirstlane(bound);
   }
 
   // the wave's blocks of keys: lane i knows the i-th's page

@@ -445,12 +445,12 @@ asr_status asr_attend_pages(const asr_paged_attention* a, void* ws, size_t ws_by
     st = check_ws(ws, ws_bytes, need);
     if (st != ASR_OK) return st;
     s.rec = need ? (float*)ws + kCounters : nullptr;
-    // With up to a block a CU and two queries a wave, the last block of a row's parts joins
-    // them; above that a second kernel does (us, last block / kernel: a row on 1500 keys,
-    // 6 heads 7.8 / 9.7, 4 rows of 32 heads on 4000 10 / 12; 2 x 3 rows on 8000, 12
-    // queries a cache head 13.6 / 12.2, 4 rows on 60000 27 / 23).
+    // With up to three blocks a CU and two queries a wave, the last block of a row's parts
+    // joins them; above that a second kernel does (us, last block / kernel: a row on 1500
+    // keys, 6 heads 7.8 / 9.7, 4 rows of 32 heads on 4000 10 / 12, 24 rows on 6000 36 / 37;
+    // 64 on 8191 100 / 95; 2 x 3 rows on 8000, 12 queries a cache head 13.6 / 12.2).
     const int64_t queries = (int64_t)s.max_rows * (s.n_head / s.c.kv_heads);
-    s.counters = need && s.blocks <= cu_count() && queries <= 8 ? (uint32_t*)ws : nullptr;
+    s.counters = need && s.blocks <= 3 * cu_count() && queries <= 8 ? (uint32_t*)ws : nullptr;
     attend_pages(s, a->dtype == ASR_BF16, (hipStream_t)stream);
     return launched(hipSuccess);
   });
