@@ -168,6 +168,16 @@ def test_f32_rows_that_the_lists_cannot_hold():
     check(x, u, least=-1, min_p=[0.5, 0.6, 0.2, 0.1, 1.0, 0.9])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_one_token_holds_nearly_all(dtype):
+    """What the other tokens weigh is far below a unit: the log-probability is 0 as it stands."""
+    x, u, _ = inputs(41, 3, 70001, dtype, 1.0)
+    x[:, 777] = 90.0
+    for kw in ({}, dict(top_p=[0.5] * 3), dict(top_k=[5] * 3), dict(top_k=[5000] * 3, top_p=[0.9] * 3), dict(min_p=[0.1] * 3),
+               dict(temperature=[0.0] * 3)):
+        assert (check(x, u, **kw) == 777).all()
+
+
 def test_parameter_sets():
     x, u, rng = inputs(19, 7, 1500, BF16, draws=2)
     check(x, u, temperature=[0.5, 1.5, 0.0], top_k=[3, 0, 50], set=[2, 0, 0, -1, 1, 3, 2147483647], sets=3)
