@@ -447,6 +447,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < SM_NW; ++i) top = fmaxf(top, s.tops[i]);
+  top += 0.f;                              // (not -0, from which 0 would be -0 away)
   if (nan || top == INFINITY) s.bad = 1;
   __syncthreads();
   int32_t* token_out = a.token + (int64_t)row * a.draws;
@@ -804,7 +805,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   }
 
   // The tokens of bins `from` to `to` that `cut` keeps into the waves' lists of `room`; whether
-  // they fit.  f(token, bin's depth) besides.
+  // they fit.
   List e;
   uint64_t listed_all;
   auto list_bins = [&](int from, int to, float* logit, int32_t* token, int room, bool sum_all) SM_INLINE {

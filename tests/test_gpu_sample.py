@@ -126,6 +126,22 @@ def test_zeros_of_either_sign_tie():
     assert check(x, [[0.1], [0.9]], top_k=[1, 2]).reshape(-1).tolist() == [5, 9]
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [700, 40003])
+def test_zeros_of_either_sign_are_the_largest(V, dtype):
+    """Rows whose largest logits are zeros: of one sign, or of both in several parts of the row."""
+    rng = np.random.default_rng(V)
+    x = -np.abs(rng.standard_normal((5, V)).astype(np.float32)) - 0.5
+    x[0, ::7], x[1, ::7] = -0.0, 0.0
+    x[2, : V // 2 : 5], x[2, V // 2 :: 5] = -0.0, 0.0
+    x[3, : V // 2 : 5], x[3, V // 2 :: 5] = 0.0, -0.0
+    x[4, ::3] = np.where(rng.random(len(x[4, ::3])) < 0.5, 0.0, -0.0)
+    x, u = torch.from_numpy(x).to(dtype), rng.random((5, 3)).astype(np.float32)
+    for kw in ({}, dict(top_k=[7] * 5), dict(top_k=[V // 3] * 5), dict(top_p=[0.3] * 5), dict(top_k=[V // 2] * 5, top_p=[0.8] * 5),
+               dict(min_p=[0.4] * 5), dict(temperature=[0.0] * 5), dict(top_k=[900] * 5)):
+        check(x, u, least=-1, **kw)
+
+
 @pytest.mark.parametrize("V", [9001, 60007])
 def test_bf16_values(V):
     """Rows of bf16 logits that are counted by value, and those whose values lie too far apart for that."""
