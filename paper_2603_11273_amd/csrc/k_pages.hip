@@ -82,23 +82,24 @@ __device__ __forceinline__ void load16(const bf16_t* p, float* x) {
 // What a block of positions gets: tokens start + i to positions length + i, i < count.
 struct NewTokens {
   int start, count;
-  int64_t length, stop;                    // positions from length to stop
+  uint32_t length, stop;                   // positions from length to stop, at most 2^30
 };
 __device__ __forceinline__ NewTokens new_tokens(const PageWriteLaunch& a, int seq) {
   const int length = a.length[seq];
   int start = a.token_start ? a.token_start[seq] : seq, end = a.token_start ? a.token_start[seq + 1] : seq + 1;
   start = max(start, 0);
   end = min(min(end, a.tokens), start > INT32_MAX - a.max_new ? INT32_MAX : start + a.max_new);
-  return {start, length < 0 ? 0 : end - start, length, min((int64_t)length + (end - start), (int64_t)a.c.columns * a.c.page)};
+  const uint32_t most = a.c.columns * a.c.page;
+  return {start, length < 0 ? 0 : end - start, (uint32_t)length, min((uint32_t)length + (uint32_t)max(end - start, 0), most)};
 }
 // Codes and scale of a head's block of positions in a page; keys or values.
 struct BlockPlace {
   uint8_t* codes;
   float* scale;
 };
-__device__ __forceinline__ BlockPlace block_place(const Pages& c, int page, int64_t p0, int head, int which) {
+__device__ __forceinline__ BlockPlace block_place(const Pages& c, int page, uint32_t p0, int head, int which) {
   const int per = c.page / kPageBlock;
-  const int64_t at = ((int64_t)which * c.kv_heads + head) * per + (p0 % c.page) / kPageBlock;
+  const int64_t at = (int64_t)(which * c.kv_heads + head) * per + p0 % (uint32_t)c.page / kPageBlock;
   return {c.codes + page * c.page_stride + at * (kPageBlock * kHeadDim), c.scales + page * c.scale_stride + at};
 }
 // A block's scale with new values up to `top` behind `old` positions: the factor that
@@ -139,17 +140,17 @@ __global__ __launch_bounds__(256) void k_write_pages(PageWriteLaunch a, int touc
   const int nth = (int)(u % touched), seq = (int)(u / touched);
   const NewTokens t = new_tokens(a, seq);
   if (t.count <= 0) return;
-  const int64_t p0 = (t.length / kPageBlock + nth) * kPageBlock;
-  if (p0 >= t.stop) return;
-  const int old = (int)max(t.length - p0, (int64_t)0), last = (int)min(t.stop - p0, (int64_t)kPageBlock);
-  const int page = a.c.table[(int64_t)seq * a.c.table_ld + p0 / a.c.page];
+  const uint32_t p0 = (t.length / kPageBlock + nth) * kPageBlock;
+  if (t.length >= t.stop || p0 >= t.stop) return;
+  const int old = max((int)(t.length - p0), 0), last = (int)min(t.stop - p0, (uint32_t)kPageBlock);
+  const int page = a.c.table[(int64_t)seq * a.c.table_ld + p0 / (uint32_t)a.c.page];
   if (page < 0 || page >= a.c.pages) return;
   const BlockPlace b = block_place(a.c, page, p0, head, which);
 
   float x[16];
   uint32_t top = 0;
   const int pos = tid >> 2, d0 = (tid & 3) * 16;
-  const T* src = (const T*)(which ? a.v : a.k) + (t.start + (p0 - t.length) + pos) * a.ld + head * kHeadDim + d0;
+  const T* src = (const T*)(which ? a.v : a.k) + (t.start + ((int64_t)p0 - t.length) + pos) * a.ld + head * kHeadDim + d0;
   const bool fresh = pos >= old && pos < last;
   if (fresh) load16(src, x);
 #pragma unroll
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(256) void k_write_step(PageWriteLaunch a) {
   const NewTokens t = new_tokens(a, seq);
   if (t.count <= 0 || t.length >= t.stop) return;
   const float x = St<T>::ld((const T*)(which ? a.v : a.k) + t.start * a.ld + head * kHeadDim, lane);
-  const int page = a.c.table[(int64_t)seq * a.c.table_ld + t.length / a.c.page];
+  const int page = a.c.table[(int64_t)seq * a.c.table_ld + t.length / (uint32_t)a.c.page];
   if (page < 0 || page >= a.c.pages) return;
   const int old = (int)(t.length % kPageBlock);
   const BlockPlace b = block_place(a.c, page, t.length - old, head, which);
@@ -349,13 +350,13 @@ __global__ __launch_bounds__(TB_NT) void k_next_tables(TablesLaunch a, bool in_p
   const auto is_page = [&](int p) { return p >= 0 && p < a.pages; };
 
   // the old table, where its entries are read twice from near or would be overwritten
-  const int64_t entries = (int64_t)n * a.columns;
+  const int entries = n * a.columns;       // (at most 2^26)
   const bool near = entries <= TB_ENTRIES;
   const int32_t* table = a.table;
   int64_t ld = a.table_ld;
   if (near || in_place) {
     int32_t* copy = near ? l.table : w.old_table;
-    for (int64_t i = tid; i < entries; i += TB_NT) copy[i] = a.table[i / a.columns * a.table_ld + i % a.columns];
+    for (int i = tid; i < entries; i += TB_NT) copy[i] = a.table[i / a.columns * a.table_ld + i % a.columns];
     table = copy, ld = a.columns;
   }
   for (int i = tid; i < words; i += TB_NT) clear_word(&used[i]), clear_word(&full[i]);
@@ -382,8 +383,8 @@ __global__ __launch_bounds__(TB_NT) void k_next_tables(TablesLaunch a, bool in_p
   __syncthreads();
 
   // what is kept, by whom
-  for (int64_t i = tid; i < entries; i += TB_NT) {
-    const int s = (int)(i / a.columns), j = (int)(i % a.columns);
+  for (int i = tid; i < entries; i += TB_NT) {
+    const int s = i / a.columns, j = i - s * a.columns;
     if (j >= q.kept[s]) continue;
     const int p = table[q.parent[s] * ld + j];
     if (!is_page(p)) continue;
@@ -446,8 +447,8 @@ __global__ __launch_bounds__(TB_NT) void k_next_tables(TablesLaunch a, bool in_p
     __syncthreads();
   }
   // tables
-  for (int64_t i = tid; i < entries; i += TB_NT) {
-    const int s = (int)(i / a.columns), j = (int)(i % a.columns), kept = q.kept[s], from = q.from[s];
+  for (int i = tid; i < entries; i += TB_NT) {
+    const int s = i / a.columns, j = i - s * a.columns, kept = q.kept[s], from = q.from[s];
     const bool copied = from >= 0 && j == q.full[s];
     int p = -1;
     if (j < kept && !copied) {
@@ -480,12 +481,12 @@ __device__ __forceinline__ void copy_bytes(const char* from, char* to, int64_t b
 }
 // Chunks of pages, over all that are to be copied.  None of them is copied from and to.
 template <typename V>
-__global__ __launch_bounds__(256) void k_copy_pages(TablesLaunch a, int chunks) {
+__global__ __launch_bounds__(256) void k_copy_pages(TablesLaunch a, uint32_t chunks) {
   const TablesWork w = tables_work(a.ws, a.sequences, a.columns, a.pages);
-  const int64_t units = (int64_t)w.counts[0] * chunks;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+  const uint32_t units = (uint32_t)w.counts[0] * chunks;      // (of memory that is there, so below 2^32)
+  for (uint32_t u = blockIdx.x; u < units; u += gridDim.x) {
     const int2 pair = *(const int2*)&w.pairs[2 * (u / chunks)];
-    const int64_t begin = u % chunks * TB_CHUNK;
+    const int64_t begin = (int64_t)(u % chunks) * TB_CHUNK;
     copy_bytes<V>((const char*)a.codes + pair.x * a.code_stride, (char*)a.codes + pair.y * a.code_stride, begin,
                   min(begin + TB_CHUNK, a.code_bytes));
     if (begin == 0)
