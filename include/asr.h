@@ -662,7 +662,7 @@ asr_status asr_write_pages(const asr_page_write* w, void* stream);
  * alone), at most max_rows of them, are of sequence s; row starts do not fall, rows
  * of no sequence are left as they were.  One row a sequence is a decode step;
  * several with one length are hypotheses of one clip, with rising ones a prompt or
- * drafts under a causal mask.  Keys are read once for up to 64 queries of a
+ * drafts under a causal mask.  Keys are read once for up to 32 queries of a
  * sequence and cache head.  A negative first counts as 0, a length past max_keys
  * or the table ends there; a row without any key gives zeros.  What a row does not
  * see does not touch it, NaN codes included; what it sees makes it NaN as the

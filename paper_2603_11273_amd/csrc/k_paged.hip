@@ -2,7 +2,7 @@
 //
 // The codes are the traffic: 128 bytes a key and head for 4 * 64 operations a
 // query.  A block takes a part of the keys of one (sequence, cache head) and up
-// to 64 of the sequence's queries; its four waves take the part's blocks of 64 keys
+// to 32 of the sequence's queries; its four waves take the part's blocks of 64 keys
 // in turn, each with a running maximum, sum and weighted values of its own, joined
 // through LDS at the end; the parts of a row are joined from (max, sum, values)
 // records by the last of its blocks or a second kernel, or not at all where there is one
