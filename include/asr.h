@@ -614,7 +614,7 @@ asr_status asr_logit_rules(const asr_rules* r, void* ws, size_t ws_bytes, void* 
  * page_stride a multiple of 16; page a multiple of 64, at most 4096.
  *   Position i of sequence s is position i % page of page table[s][i / page].  An
  * entry outside [0, pages) is no page: its positions cannot be written and are
- * not there to attend to. */
+ * not there to attend to.  No scale that a row sees is infinite. */
 typedef struct {
   int32_t kv_heads, page, pages;
   uint8_t* codes;

@@ -317,7 +317,7 @@ void k_attend_pages(PagedArgs a) {
   while (at >= 0) {
     const int key0 = k0 + (wave + PA_NW * at) * kPageBlock, key = key0 + 16 * g;
     const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), at));
-    const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), at));
+    float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), at));
     const bool mixed = key0 < all_lo || key0 + kPageBlock > all_hi;   // some column does not see some key
     advance();
     float s[QT][16];
@@ -343,6 +343,16 @@ void k_attend_pages(PagedArgs a) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) bad |= nan_codes(v[t].x) | nan_codes(v[t].y) | nan_codes(v[t].z) | nan_codes(v[t].w);
       nans = __any(bad != 0);
+      // (and so is a scale's, which 0 times it would spread)
+      if (!(fabsf(vs) < INFINITY)) {
+        vs = 1.f;
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+          if (max(first[t], key0) < min(end[t], key0 + kPageBlock)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[t][i] = f32x4{NAN, NAN, NAN, NAN};
+          }
+      }
     }
     if (nans) {
 #pragma unroll

@@ -376,6 +376,27 @@ def test_nan_touches_the_rows_that_see_it(dtype):
     case.check(case.run(dtype, part_keys=256))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_scales_that_are_not_finite_touch_the_rows_that_see_them(bad, dtype):
+    """The scale of a block that only the last rows see, of keys or of values."""
+    for m in (0, 1):
+        case = Attend(45, [9, 3], [135, 70], mask="causal", heads=4, kv=2)
+        case.pool.scales[case.table[0, 2], m, 1, 0] = bad          # positions 128 to 134: rows 2 to 8 of 0 to 8
+        case.pool.poke()
+        for part_keys in (0, 256):
+            got = host(case.run(dtype, part_keys=part_keys).double())
+            with np.errstate(all="ignore"):
+                ref = attention(case.pool.codes, case.pool.scales, case.table, case.start, case.first, case.length, case.q, 4, 0.125,
+                                dtype == BF16)
+            for r, (want, tol) in enumerate(ref):
+                sees = np.zeros(256, bool)
+                sees[128:] = r < 9 and case.length[r] > 128        # query heads 2 and 3 are on cache head 1
+                assert np.isfinite(want[~sees]).all() and (np.abs(got[r] - want)[~sees] <= tol[~sees]).all(), r
+                if np.isnan(bad):                                  # (what an infinite one gives is not said)
+                    assert np.isnan(got[r][sees]).all() and np.isnan(want[sees]).all(), r
+
+
 def test_queries_that_are_not_finite():
     case = Attend(43, [3, 1], [100, 70])
     case.q[0, 3], case.q[1, 70], case.q[2, 130] = np.nan, np.inf, -np.inf
