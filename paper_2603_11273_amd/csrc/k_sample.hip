@@ -195,7 +195,10 @@ struct Lds {
   };
   union {
     uint32_t counts[SM_BINS];
-    uint64_t fine[SM_FINE];
+    struct {
+      uint64_t fine[SM_FINE];
+      uint32_t fine_n[SM_FINE];
+    };
     uint64_t seg[SM_NT];
   };
   struct {
@@ -204,7 +207,7 @@ struct Lds {
   } narrow;
   uint64_t sums[2][SM_NW];
   uint64_t found_before, found_in, found_other;
-  uint32_t found, members;
+  uint32_t found, members, members2;
   float tops[SM_NW], lows[SM_NW];
   float member_logit[SM_MEMBERS];
   int32_t member_token[SM_MEMBERS];
@@ -808,10 +811,12 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   // they fit.
   List e;
   uint64_t listed_all;
+  float listed_low;
   auto list_bins = [&](int from, int to, float* logit, int32_t* token, int room, bool sum_all) SM_INLINE {
     const uint32_t lo = bin_begin(from), width = bin_end(to) - lo;
     int n = 0;
     double sum = 0.0;                      // (a lane's, in the order of its tokens: always the same)
+    float low = INFINITY;
     __syncthreads();
     r.template each<1>([&](int base, const float* x) SM_INLINE {
       uint64_t is[E], any = 0;
@@ -837,34 +842,96 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
         for (int i = 0; i < E; ++i)
           if (is[i]) {
             const bool in = is[i] >> lane & 1;
+            low = in ? fminf(low, x[i]) : low;
             if (in && at < (uint32_t)room) logit[at] = x[i], token[at] = base + i;
             at += in;
           }
       }
     });
     e = {logit, token, n};
+    low = -wave_max_lanes(-low);
+    if (lane == 0) s.lows[wave] = low;
+    if (tid == 0) s.members = s.members2 = 0;
+    clear<sizeof(s.fine)>(s.fine);
+    ((uint2*)s.fine_n)[tid] = uint2{0, 0};
     uint64_t t0, sum_of, over;
     block_scan2((uint64_t)sum, lane == 0 ? (n > room ? 1ull << 32 : 0) + (uint64_t)n : 0, s, &t0, &sum_of, &t0, &over);
     if (sum_all) all = sum_of, have_all = true;
     listed_all = over & 0xffffffffu;
+    listed_low = -wave_max_lanes(-s.lows[lane & (SM_NW - 1)]);
     return over >> 32 == 0;
   };
 
   if (last >= 0 && few && list_bins(0, last, s.list.logit[wave], s.list.token[wave], SM_LIST, logprob_out || (p_on && !k_on))) {
     const int per = (e.n + 63) / 64, begin = min(lane * per, e.n), end = min(begin + per, e.n);
     bool fine = true;
-#pragma unroll 1
-    for (int by = k_on && listed_all > (uint64_t)top_k ? 0 : 1; by < (p_on ? 2 : 1); ++by) {
-      uint64_t goal = top_k;
-      if (by == 1) {
-        uint64_t mass = 0;
-        for (int i = begin; i < end; ++i) mass += cut.keeps(e.logit[i], e.token[i]) ? w.whole(e.logit[i]) : 0;
-        mass = block_add(mass, s);
-        goal = p_goal(k_on ? mass : all);
-        fine = goal <= mass;               // the guess was far enough
-        if (!fine) break;
+    const bool k_cuts = k_on && listed_all > (uint64_t)top_k;
+    if (k_cuts || p_on) {
+      // both cuts from the same bins, of one width: most often a cut's holds a few tokens
+      const float range = top - listed_low, scale = range > 1e-30f && range < 1e30f ? (SM_FINE - 1) / range : 0.f;
+      auto bin = [&](float x) SM_INLINE { return min((int)((top - x) * scale), SM_FINE - 1); };
+      for (int i = lane; i < e.n; i += 64) {
+        const int b = bin(e.logit[i]);
+        atomicAdd((unsigned long long*)&s.fine[b], (unsigned long long)w.whole(e.logit[i]));
+        atomicAdd(&s.fine_n[b], 1u);
       }
-      cut = cut_list(e, cut, by == 0, goal, w, s);
+      __syncthreads();
+      const ulonglong2 y = ((const ulonglong2*)s.fine)[tid];
+      const uint2 c = ((const uint2*)s.fine_n)[tid];
+      uint64_t y_before, mass, c_before, t0;
+      block_scan2(y.x + y.y, c.x + c.y, s, &y_before, &mass, &c_before, &t0);
+#pragma unroll 1
+      for (int by = k_cuts ? 0 : 1; by < (p_on ? 2 : 1); ++by) {
+        uint64_t goal = top_k;
+        if (by == 1) {
+          goal = p_goal(k_on ? mass : all);
+          fine = goal <= mass;             // the guess was far enough
+          if (!fine) break;
+        }
+        const uint64_t before = by ? y_before : c_before, one = by ? y.x : c.x, two = by ? y.y : c.y;
+        if (before < goal && goal <= before + one + two) {
+          const bool second = before + one < goal;
+          s.found = 2 * tid + second, s.found_before = second ? before + one : before, s.found_other = second ? y_before + y.x : y_before;
+        }
+        __syncthreads();
+        const int found = s.found;
+        const uint64_t rest = goal - s.found_before, lighter = s.found_other;
+        uint32_t* members = by ? &s.members2 : &s.members;
+        for (int i = lane; i < e.n; i += 64) {
+          const float x = e.logit[i];
+          if (bin(x) == found && cut.keeps(x, e.token[i])) {
+            const uint32_t at = atomicAdd(members, 1u);
+            if (at < SM_MEMBERS) s.member_logit[at] = x, s.member_token[at] = e.token[i];
+          }
+        }
+        __syncthreads();
+        const int m = *members;
+        if (m > SM_MEMBERS) {
+          cut = cut_list(e, cut, by == 0, goal, w, s);
+          if (by == 0 && p_on) {
+            mass = 0;
+            for (int i = begin; i < end; ++i) mass += cut.keeps(e.logit[i], e.token[i]) ? w.whole(e.logit[i]) : 0;
+            mass = block_add(mass, s);
+          }
+          continue;
+        }
+        // (every wave for itself)
+        const float x = lane < m ? s.member_logit[lane] : -INFINITY;
+        const int token = lane < m ? s.member_token[lane] : INT32_MAX;
+        const uint64_t own = lane < m ? w.whole(x) : 0;
+        uint64_t heavier = 0, rank = 0;
+        for (int j = 0; j < m; ++j) {
+          const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), j));
+          const int t = __builtin_amdgcn_readlane(token, j);
+          const bool first = o > x || (o == x && t < token);
+          heavier += first ? lane_value(own, j) : 0;
+          rank += first;
+        }
+        const bool last_kept = lane < m && (by ? heavier < rest && rest <= heavier + own : rank + 1 == rest);
+        const int at = __ffsll((unsigned long long)__ballot(last_kept)) - 1;
+        cut = {__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), at)), __builtin_amdgcn_readlane(token, at)};
+        if (by == 0) mass = lighter + lane_value(heavier + own, at);
+      }
     }
     if (fine) {
       cut = tighter(cut);
