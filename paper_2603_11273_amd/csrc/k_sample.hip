@@ -25,9 +25,10 @@
 // times a polynomial, in 64 bits.  Bound by instructions (a weight takes 22, 13 of them on
 // doubles: some 0.2 ns a token of a row) and by the fetch of code that runs once, some 0.1 us
 // for 64 bytes, hence loops where they cost nothing.  A row of 51865 under top-p
-// takes 24 to 31 us by what it keeps (max 4, guess 5, list and weights 15, cut 4), 128 rows
-// under all filters 35, 256 bf16 rows of 131071 with 5 draws 75 (max 12, counts 14, their
-// weights and cuts 18, segments 17, draws 7); sorting each row took 302, 1453, 3805.
+// takes 24 to 31 us by what it keeps (max 4, guess 5, list and weights 16, cut 4; 62 where the
+// lists cannot hold it), 128 rows under all filters 33, 256 bf16 rows of 131071 with 5 draws 75
+// (max 12, counts 14, their weights and cuts 18, segments 17, draws 7); sorting each row took
+// 302, 1453, 3805.
 #include <algorithm>
 
 #include "asr_device.h"
@@ -145,11 +146,13 @@ struct RowOf {
 // e^{(l - M) / T} in whole units of 2^-unit.
 struct Weights {
   const double* tab;       // 2^(unit + i / 512)
+  int unit;
   double top, c;           // 512 log2(e) / T
   double least;            // place of 2^-60 units: what weighs less counts as that, nothing in every sum
   __device__ __forceinline__ double place(float l) const { return ((double)l - top) * c; }
-  __device__ __forceinline__ double weight(float l) const {
-    const double y = fmax(place(l), least);          // (0 times -inf, too)
+  __device__ __forceinline__ double weight(float l) const { return power(fmax(place(l), least)); }   // (0 times -inf, too)
+  // 2^(unit + y / 512)
+  __device__ __forceinline__ double power(double y) const {
     constexpr double kMagic = 6755399441055744.0;          // 1.5 * 2^52: the nearest whole number is in the low bits
     const double t = y + kMagic;
     const int k = __double2loint(t);
@@ -159,6 +162,14 @@ struct Weights {
     const double v = fma(fma(fma(a3, r, a2), r, a1), r * e, e);
     // times 2^(k / 512), in the exponent
     return __hiloint2double(__double2hiint(v) + (int)((uint32_t)(k & ~(SM_TAB - 1)) << 11), __double2loint(v));
+  }
+  // log2(x), x > 0: the float instruction's, and what its power leaves of x
+  __device__ __forceinline__ double log2_of(double x) const {
+    int exponent;
+    const double f = 2.0 * frexp(x, &exponent);
+    const double near = (double)__builtin_amdgcn_logf((float)f);
+    const double rest = fma(f, ldexp(power(near * -(double)SM_TAB), -unit), -1.0);      // (below 2^-22: the cube is nothing)
+    return exponent - 1 + near + fma(-0.5 * rest, rest, rest) * 1.4426950408889634074;
   }
   // 2^52 leaves the whole number in the low bits
   __device__ __forceinline__ uint64_t whole(float l) const {
@@ -464,11 +475,11 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     return;
   }
   constexpr double kScale = 512.0 * 1.4426950408889634074;
-  const Weights w = {s.tab, (double)top, kScale / (greedy ? 1.0 : (double)temperature), -512.0 * (unit + 60)};
+  const Weights w = {s.tab, unit, (double)top, kScale / (greedy ? 1.0 : (double)temperature), -512.0 * (unit + 60)};
   uint64_t all = 0;                        // of all weights, once `have_all`
   auto answer = [&](int d, int token, float l) SM_INLINE {
     token_out[d] = token;
-    if (logprob_out) logprob_out[d] = (float)(w.place(l) / kScale - log(ldexp((double)all, -unit)));
+    if (logprob_out) logprob_out[d] = (float)((w.place(l) * (1.0 / SM_TAB) - (w.log2_of((double)all) - unit)) * 0.69314718055994530942);
   };
   auto goal_of = [&](int d, uint64_t mass) SM_INLINE {
     const float u = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(uniform), d));
@@ -506,7 +517,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   // min-p as a cut: the least logit whose weight is at least min_p
   Cut least = cut;
   if (min_p > 0.f && min_p <= 1.f) {
-    const double bound = 512.0 * log2((double)min_p);
+    const double bound = SM_TAB * w.log2_of((double)min_p);
     auto passes = [&](uint32_t k) SM_INLINE { return w.place(of_falling(k)) >= bound; };
     const uint32_t first = falling(top), end = falling(-INFINITY);
     const uint32_t near = falling((float)fmax(fmin(w.top + bound / w.c, w.top), -3e38));
