@@ -747,7 +747,7 @@ asr_status asr_next_tables(const asr_page_tables* t, void* ws, size_t ws_bytes, 
  * as 0, 1 and above as the float32 below 1).  Weights are formed to 2^-44 of themselves and
  * rounded to multiples of 2^-50, or of 2^(n - 62) where the vocabulary is above 2^12 and 2^n
  * the power of two not below it; sums of kept ones are whole numbers of these, those of a whole
- * row may be doubles instead (2^-47 of the sum), always added in the same order.  So neither
+ * row may be doubles of weights before rounding (logprob's is), always added in the same order.  So neither
  * the other rows nor the work's split can change a token.
  *   token [rows][draws]; logprob [rows][draws] or NULL: (l - M) / T - log sum over all v of
  * w_v, in float32; kept [rows] or NULL: tokens kept.  A row whose logits hold a NaN or

@@ -172,9 +172,10 @@ struct Weights {
     return exponent - 1 + near + fma(-0.5 * rest, rest, rest) * 1.4426950408889634074;
   }
   // 2^52 leaves the whole number in the low bits
-  __device__ __forceinline__ uint64_t whole(float l) const {
-    return (uint64_t)__double_as_longlong(weight(l) + 4503599627370496.0) & 0xfffffffffffffull;
+  static __device__ __forceinline__ uint64_t rounded(double weight) {
+    return (uint64_t)__double_as_longlong(weight + 4503599627370496.0) & 0xfffffffffffffull;
   }
+  __device__ __forceinline__ uint64_t whole(float l) const { return rounded(weight(l)); }
 };
 
 // Kept: logits above `l`, and of those at it tokens up to `last`.
@@ -272,6 +273,20 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
 #undef SM_STEP
   return v;
 }
+// The same of doubles.
+__device__ __forceinline__ double wave_sum64(double v) {
+#define SM_STEP(ctrl, rows)                                                                          \
+  v += __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), ctrl, rows, 0xf, false),   \
+                        __builtin_amdgcn_update_dpp(0, __double2loint(v), ctrl, rows, 0xf, false))
+  SM_STEP(0x111, 0xf);
+  SM_STEP(0x112, 0xf);
+  SM_STEP(0x114, 0xf);
+  SM_STEP(0x118, 0xf);
+  SM_STEP(0x142, 0xa);
+  SM_STEP(0x143, 0xc);
+#undef SM_STEP
+  return v;
+}
 __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 |
          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
@@ -294,6 +309,16 @@ __device__ __forceinline__ void block_scan2(uint64_t a, uint64_t b, S& s, uint64
                                             uint64_t* vb) {
   *before_a = block_scan(a, s, va);
   *before_b = block_scan(b, s, vb, 1);
+}
+// The sum of a over the threads, always in the same order; *before and *total of b as above.
+template <class S>
+__device__ __forceinline__ double block_sum_scan(double a, uint64_t b, S& s, uint64_t* before, uint64_t* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const double x = wave_sum64(a);
+  __syncthreads();
+  if (lane == 63) s.sums[1][wave] = (uint64_t)__double_as_longlong(x);
+  *before = block_scan(b, s, total);       // (its barriers stand for both)
+  return __longlong_as_double((long long)lane_value((uint64_t)__double_as_longlong(wave_sum64(__longlong_as_double((long long)s.sums[1][lane & (SM_NW - 1)]))), SM_NW - 1));
 }
 __device__ __forceinline__ uint64_t block_add(uint64_t v, Lds& s) {
   uint64_t all;
@@ -476,10 +501,10 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   }
   constexpr double kScale = 512.0 * 1.4426950408889634074;
   const Weights w = {s.tab, unit, (double)top, kScale / (greedy ? 1.0 : (double)temperature), -512.0 * (unit + 60)};
-  uint64_t all = 0;                        // of all weights, once `have_all`
+  double all = 0.0;                        // of all weights, not rounded, once `have_all`
   auto answer = [&](int d, int token, float l) SM_INLINE {
     token_out[d] = token;
-    if (logprob_out) logprob_out[d] = (float)((w.place(l) * (1.0 / SM_TAB) - (w.log2_of((double)all) - unit)) * 0.69314718055994530942);
+    if (logprob_out) logprob_out[d] = (float)((w.place(l) * (1.0 / SM_TAB) - w.log2_of(ldexp(all, -unit))) * 0.69314718055994530942);
   };
   auto goal_of = [&](int d, uint64_t mass) SM_INLINE {
     const float u = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(uniform), d));
@@ -500,7 +525,8 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       }
     });
     if (at < INT32_MAX) atomicMin(&s.first, at);
-    all = block_add((uint64_t)whole_row, s);
+    uint64_t t0, t1;
+    all = block_sum_scan(whole_row, 0, s, &t0, &t1);
     if (tid < a.draws) answer(tid, s.first, top);
     if (tid == 0 && a.kept) a.kept[row] = 1;
     return;
@@ -558,6 +584,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       __syncthreads();
       auto count_of = [&](uint32_t b) SM_INLINE { return b == SV_N - 1 || b == none ? 0u : v.hist[b]; };
       auto weight_of = [&](uint32_t b) SM_INLINE { return w.whole(of_falling16(first_key + b)); };
+      double row_sum = 0.0;
       // (three at a time, as most hold nothing)
       constexpr int W = 3;
       static_assert(SV_N % (W * SM_NT) == 0, "");
@@ -570,7 +597,12 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
 #pragma unroll 1
         for (int j = i; j < i + W; ++j) {
           uint64_t n = 0, mass = 0;
-          if (some) n = wave_scan(c[0]), mass = wave_scan(c[0] * weight_of(j * SM_NT + tid));
+          if (some) {
+            const double y = w.weight(of_falling16(first_key + j * SM_NT + tid));
+            n = wave_scan(c[0]);
+            mass = wave_scan(c[0] * w.rounded(y));
+            row_sum += c[0] ? c[0] * y : 0.0;
+          }
           if (lane == 63) v.part.n[j * SM_NW + wave] = (uint32_t)n, v.part.mass[j * SM_NW + wave] = mass;
 #pragma unroll
           for (int m = 0; m < W - 1; ++m) c[m] = c[m + 1];
@@ -582,7 +614,8 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       uint64_t n_before, n_all, mass_before, mass_all;
       block_scan2(n, mass, v, &n_before, &n_all, &mass_before, &mass_all);
       if (v.hist[SV_N - 1] && (w.place(of_falling16(first_key + SV_N - 1)) >= w.least || (k_on && n_all < (uint64_t)top_k))) return false;
-      all = mass_all;
+      uint64_t t0, t1;
+      all = block_sum_scan(row_sum, 0, v, &t0, &t1);
       uint32_t end = 0, ties = 0;          // kept: values before `end`, and of that one the first `ties` tokens
       uint64_t each = 0, kept_mass = mass_all;
       auto locate = [&](bool by_count, uint64_t goal) SM_INLINE {
@@ -631,7 +664,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       for (int i = kept_steps * (SM_NT / 4) + tid; i < SV_N / 4; i += SM_NT)
         ((uint4*)v.hist)[i] = uint4{SV_IDS * 8, SV_IDS * 8, SV_IDS * 8, SV_IDS * 8};
       if (tid == 0) v.weight[SV_IDS] = 0;
-      uint64_t t0, t1, kept_all, mass_kept;
+      uint64_t kept_all, mass_kept;
       block_scan2(kept_n, kept_mass, v, &t0, &kept_all, &t1, &mass_kept);
       mass_kept += ties * each;
       if (tid == 0 && a.kept) a.kept[row] = (int32_t)kept_all + ties;
@@ -738,7 +771,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     if (r.steps * 64 * E > SM_LIST && (k_on ? top_k > SM_FEW : p_on)) {
       if (by_values()) return;
       __syncthreads();
-      all = 0;
+      all = 0.0;
       clear<sizeof(s.bins)>(s.bins);
       clear<sizeof(s.counts)>(s.counts);
       __syncthreads();
@@ -865,8 +898,8 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     if (tid == 0) s.members = s.members2 = 0;
     clear<sizeof(s.fine)>(s.fine);
     ((uint2*)s.fine_n)[tid] = uint2{0, 0};
-    uint64_t t0, sum_of, over;
-    block_scan2((uint64_t)sum, lane == 0 ? (n > room ? 1ull << 32 : 0) + (uint64_t)n : 0, s, &t0, &sum_of, &t0, &over);
+    uint64_t t0, over;
+    const double sum_of = block_sum_scan(sum, lane == 0 ? (n > room ? 1ull << 32 : 0) + (uint64_t)n : 0, s, &t0, &over);
     if (sum_all) all = sum_of, have_all = true;
     listed_all = over & 0xffffffffu;
     listed_low = -wave_max_lanes(-s.lows[lane & (SM_NW - 1)]);
@@ -895,7 +928,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       for (int by = k_cuts ? 0 : 1; by < (p_on ? 2 : 1); ++by) {
         uint64_t goal = top_k;
         if (by == 1) {
-          goal = p_goal(k_on ? mass : all);
+          goal = p_goal(k_on ? mass : (uint64_t)all);
           fine = goal <= mass;             // the guess was far enough
           if (!fine) break;
         }
@@ -1034,7 +1067,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
   // weights of what `cut` keeps of bins `from` to `to` into the bins; those of all
   auto weigh = [&](int from, int to, bool sum_all) SM_INLINE {
     const uint32_t lo = bin_begin(from), width = bin_end(to) - lo;
-    uint64_t sum = 0;
+    double sum = 0.0;
     r.template each<1>([&](int base, const float* x) SM_INLINE {
       bool in[E], some = sum_all;
 #pragma unroll
@@ -1042,12 +1075,17 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       if (!__any(some)) return;
       uint64_t y[E];
 #pragma unroll
-      for (int i = 0; i < E; ++i) sum += y[i] = w.whole(x[i]);
+      for (int i = 0; i < E; ++i) {
+        const double z = w.weight(x[i]);
+        sum += z;
+        y[i] = w.rounded(z);
+      }
 #pragma unroll
       for (int i = 0; i < E; ++i)
         if (in[i] && y[i]) atomicAdd((unsigned long long*)&s.bins[bin_of(depth(top, x[i]))], (unsigned long long)y[i]);
     });
-    if (sum_all) all = block_add(sum, s), have_all = true;
+    uint64_t t0, t1;
+    if (sum_all) all = block_sum_scan(sum, 0, s, &t0, &t1), have_all = true;
   };
   if (k_on || p_on) {
     __syncthreads();
@@ -1074,7 +1112,8 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     cut = fits ? cut_list(e, cut, by == 0, goal, w, s) : cut_row(by == 0, goal);
   }
   cut = tighter(cut);
-  uint64_t sum = 0, n = 0, part = 0;
+  double sum = 0.0;
+  uint64_t n = 0, part = 0;
   const bool sum_all = logprob_out && !have_all;
   __syncthreads();
   r.template each<1>(
@@ -1085,10 +1124,10 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
         if (!__any(some)) return;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          const uint64_t y = w.whole(x[i]);
+          const double z = w.weight(x[i]);
           n += in[i];
-          sum += y;
-          part += in[i] ? y : 0;
+          sum += z;
+          part += in[i] ? w.rounded(z) : 0;
         }
       },
       [&](int seg) SM_INLINE {
@@ -1096,9 +1135,9 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
         if (lane == 0) s.seg[seg] = part;
         part = 0;
       });
-  uint64_t t0, t1, n_all, mass;
-  block_scan2(sum, n, s, &t0, &t1, &t0, &n_all);
-  if (sum_all) all = t1;
+  uint64_t t0, n_all, mass;
+  const double sum_of = block_sum_scan(sum, n, s, &t0, &n_all);
+  if (sum_all) all = sum_of;
   if (tid == 0 && a.kept) a.kept[row] = (int32_t)n_all;
   const int segments = r.segments();
   const uint64_t own = tid < segments ? s.seg[tid] : 0, upto = block_scan(own, s, &mass) + own;

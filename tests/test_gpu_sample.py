@@ -194,6 +194,16 @@ def test_one_token_holds_nearly_all(dtype):
         assert (check(x, u, **kw) == 777).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_log_probabilities_near_zero(dtype):
+    """A token that is all but certain: its log-probability is minus what tens of thousands of others weigh, each less than a unit."""
+    x, u, _ = inputs(43, 6, 50113, dtype, 1.0)
+    x[:, 31423] = torch.tensor([20.0, 24.0, 26.0, 28.0, 30.0, 34.0])
+    for kw in ({}, dict(top_p=[0.99] * 6), dict(top_k=[5] * 6), dict(top_k=[40000] * 6, top_p=[0.9] * 6), dict(min_p=[0.1] * 6),
+               dict(temperature=[0.0] * 6), dict(top_k=[5000] * 6)):
+        assert (check(x, u, **kw) == 31423).all()
+
+
 def test_parameter_sets():
     x, u, rng = inputs(19, 7, 1500, BF16, draws=2)
     check(x, u, temperature=[0.5, 1.5, 0.0], top_k=[3, 0, 50], set=[2, 0, 0, -1, 1, 3, 2147483647], sets=3)
