@@ -506,7 +506,7 @@ __global__ __launch_bounds__(256) void k_join_pages(PagedArgs a) {
       const int n = __popcll(__ballot(s0 + lane < a.c.c.sequences && x <= row));
       if (n == 0) break;
       start = __builtin_amdgcn_readlane(x, n - 1);
-      end = a.c.row_start[s0 + n];
+      end = n < 64 ? __builtin_amdgcn_readlane(x, n) : a.c.row_start[s0 + 64];
     }
     if (start < 0 || row >= end || row - start >= a.c.max_rows) return;
   } else if (row >= a.c.c.sequences) {
