@@ -108,11 +108,13 @@ __device__ __forceinline__ float lanes16_sum(float v) {
   return __uint_as_float(p32[0]) + __uint_as_float(p32[1]);
 }
 
-// Rows of a sequence: [start, start + count).
+// Rows of a sequence: [start, start + count).  A start behind the rows (a padded list's, up
+// to 2^31 - 1) has none: count stays in [0, max_rows], so that its product with the queries
+// of a row holds in 32 bits.
 __device__ __forceinline__ void rows_of(const PagedLaunch& c, int seq, int* start, int* count) {
   const int s = c.row_start ? c.row_start[seq] : seq, e = c.row_start ? c.row_start[seq + 1] : seq + 1;
   *start = s;
-  *count = s < 0 ? 0 : min(min(e, c.rows) - s, c.max_rows);
+  *count = s < 0 || s >= c.rows ? 0 : min(min(max(e, s), c.rows) - s, c.max_rows);
 }
 
 // (max, sum) of part `part` of a row and head; a sum of 0 says that the part has no
