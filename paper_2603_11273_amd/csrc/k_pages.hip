@@ -89,8 +89,9 @@ __device__ __forceinline__ NewTokens new_tokens(const PageWriteLaunch& a, int se
   int start = a.token_start ? a.token_start[seq] : seq, end = a.token_start ? a.token_start[seq + 1] : seq + 1;
   start = max(start, 0);
   end = min(min(end, a.tokens), start > INT32_MAX - a.max_new ? INT32_MAX : start + a.max_new);
+  end = max(end, start);                   // (an end far below the start: their distance passes 32 bits)
   const uint32_t most = a.c.columns * a.c.page;
-  return {start, length < 0 ? 0 : end - start, (uint32_t)length, min((uint32_t)length + (uint32_t)max(end - start, 0), most)};
+  return {start, length < 0 ? 0 : end - start, (uint32_t)length, min((uint32_t)length + (uint32_t)(end - start), most)};
 }
 // Codes and scale of a head's block of positions in a page; keys or values.
 struct BlockPlace {
