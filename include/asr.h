@@ -678,7 +678,7 @@ typedef struct {
   int32_t rows, max_rows;
   int32_t max_keys;
   int32_t part_keys;         /* keys per part of the work: 0, or a multiple of 256 up to 16384 */
-  float scale;
+  float scale;               /* finite, below 2.3e38 in magnitude */
   const float* q;
   int64_t q_ld;
   void* out;

@@ -255,7 +255,9 @@ asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* byte
   if (!a->row_start && a->rows > a->cache.sequences) return fail(ASR_EINVAL, "more rows than sequences, and no row_start");
   if (a->part_keys != 0 && (a->part_keys < 256 || a->part_keys > 16384 || a->part_keys % 256))
     return fail(ASR_EINVAL, "part_keys must be 0 or a multiple of 256, at most 16384");
-  if (!std::isfinite(a->scale)) return fail(ASR_EINVAL, "scale");
+  // (scores are powers of 2 in the kernel: the scale is taken times log2(e), a float too)
+  const float qmul = a->scale * 1.4426950408889634f;
+  if (!std::isfinite(qmul)) return fail(ASR_EINVAL, "scale must be finite, below 2.3e38 in magnitude");
   const int64_t most = std::min<int64_t>(a->max_keys, (int64_t)a->cache.columns * a->cache.page);
   const int64_t per = a->n_head / a->cache.kv_heads, cols = (a->row_start ? a->max_rows : 1) * per;
   if (cols > INT32_MAX) return fail(ASR_EINVAL, "too many queries in a sequence");
@@ -274,7 +276,7 @@ asr_status plan_paged(const asr_paged_attention* a, PagedLaunch* s, size_t* byte
   s->q_ld = a->q_ld;
   s->out = a->out;
   s->out_ld = a->out_ld;
-  s->qmul = a->scale * 1.4426950408889634f;
+  s->qmul = qmul;
   s->row_start = a->row_start;
   s->first = a->first;
   s->length = a->length;
