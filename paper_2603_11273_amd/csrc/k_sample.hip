@@ -6,7 +6,7 @@
 // A block of 1024 threads takes a row, each wave a sixteenth of it, which comes from L2
 // again at each pass.  After the largest logit M (and each thread's):
 //
-// float32 logits, bf16 ones with a small top-k or up to 8192 tokens:
+// float32 logits, bf16 ones with a small top-k or up to 16384 tokens:
 //   1. a bin that the cut cannot lie behind: bins are the leading bits of M - l (256 to an
 //      octave), filled with counts for top-k (up to 768 wanted tokens: of the threads'
 //      largest alone) or, for top-p, with the float32 weights of the threads' largest and
@@ -17,7 +17,7 @@
 //   Where a wave's list would be longer than 512 tokens, counts or weights of the whole
 //   row are filled into bins for each cut in turn, only the cut's own bin is listed, and
 //   draws go by sums over segments of 4 loads of a wave.
-// bf16 logits with top-k above 768 or top-p: tokens are counted by value, in LDS; counts times
+// more bf16 logits, with top-k above 768 or top-p: tokens are counted by value, in LDS; counts times
 //   weights give the sums and the cuts, one pass over the tokens the segments' sums, each
 //   value's weight looked up.
 //
@@ -41,6 +41,7 @@ constexpr int SM_BINS = 8192, SM_FINE = 2048, SM_TAB = 512;
 constexpr int SM_LIST = 512, SM_NARROW = 256;      // of a wave: all tokens up to a bin, those of one bin
 constexpr int SM_U = 4;                            // loads under way, and in a segment
 constexpr int SM_FEW = 768;                        // wanted tokens that the threads' largest may bound
+constexpr int SM_VALUES = 16384;                   // bf16 tokens above which values are counted
 constexpr int SM_MEMBERS = 64;
 
 #define SM_INLINE __attribute__((always_inline))
@@ -766,9 +767,17 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
       }
       return true;
     };
-    // (128 rows of 51866, us, lists / values: top-k 50 26 / 42, 1000 36 / 42; top-p 0.5 33 /
-    // 43, 0.99 62 / 43; top-k 9000 and top-p 71 / 44)
-    if (r.steps * 64 * E > SM_LIST && (k_on ? top_k > SM_FEW : p_on)) {
+    // Values take the same time whatever is kept, lists as much as there is before the cut.
+    // Lists / values, us, 128 rows of logits with a deviation of 3, of 1.5 and of 0.5:
+    //    12001  top-k 2000  23 / 36, 28 / 36, 33 / 31   top-p 0.5  34 / 33, 22 / 36, 42 / 31   0.9  36 / 33, 40 / 37, 33 / 32
+    //    24000  top-k 2000  27 / 31, 30 / 34, 37 / 30   top-p 0.5  41 / 32, 28 / 35, 41 / 30   0.9  47 / 32, 39 / 35, 41 / 30
+    //    51866  top-k 1000  41 / 43, 40 / 47, 49 / 42   top-p 0.5  31 / 44, 45 / 48, 67 / 43   0.9  40 / 44, 64 / 48, 69 / 43
+    //   131071  top-k 1000  78 / 70, 75 / 73, 89 / 69   top-p 0.5  68 / 70, 139 / 75, 141 / 71 0.9  89 / 71, 135 / 75, 146 / 71
+    // (the last 256 rows), and top-k 50 and 768 of 51866 28 / 43 and 37 / 43.  Over top-k 769 to
+    // half of the tokens, top-p 0.3 to 0.99 and both, lists take 0.62 to 1.02 of the values' time at
+    // 8200 tokens (by deviation), 0.81 to 1.18 at 12001, 0.82 to 1.34 at 16000 (1.01 on the whole),
+    // 0.99 to 1.45 at 51866.
+    if (a.vocab > SM_VALUES && (k_on ? top_k > SM_FEW : p_on)) {
       if (by_values()) return;
       __syncthreads();
       all = 0.0;
