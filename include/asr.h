@@ -666,9 +666,14 @@ asr_status asr_write_pages(const asr_page_write* w, void* stream);
  * sequence and cache head.  A negative first counts as 0, a length past max_keys
  * or the table ends there; a row without any key gives zeros.  What a row does not
  * see does not touch it, NaN codes included; what it sees makes it NaN as the
- * formula does.  Sums are float32; a row's bits depend neither on the other rows nor
- * on its place (with part_keys given; 0 lets the library split the work by the call's
- * size and, under windows, by what the rows see).
+ * formula does.  Sums are float32; queries and softmax weights are multiplied as
+ * sums of two bf16 numbers for a bf16 result (off by 2^-17 and 2^-16 of themselves),
+ * of three, which hold them whole, for a float32 one.  A weight times the value scale
+ * of its block keeps what is above 2^-134: where scales are below 2^-110 (values below
+ * 3e-31) digits are lost.  A row's bits depend neither on the other rows nor on its
+ * place (with part_keys given; 0 lets the library split the work by the call's size
+ * and, under windows, by what the rows see).  Row starts behind the rows say that a
+ * sequence has none.
  *   q: float32 [rows][n_head * 64], rows q_ld apart; out of type dtype, rows
  * out_ld apart (both 16-byte aligned, q_ld and out_ld multiples of 4). */
 typedef struct {

@@ -656,8 +656,8 @@ class Sampler(_Operator):
     [rows]; temperature, top_p, min_p float32 and top_k int32 [sets].  plan(logits, u, token,
     logprob, kept): logits [rows][vocab] of `dtype` (float32 or bfloat16), u float32
     [rows][draws] in [0, 1), token int32 and logprob float32 [rows][draws], kept int32 [rows]
-    (logprob and kept may be None).  One call at a time: calls that may overlap on the GPU need
-    plans with a workspace each (default: one of the plan's own)."""
+    (logprob and kept may be None).  The call has no scratch, so calls of one plan may overlap on
+    the GPU where their outputs lie apart; a workspace that is given is left as it is."""
 
     def __init__(self, rows, vocab, dtype, *, draws=1, sets=None, set=None, temperature=None, top_k=None,
                  top_p=None, min_p=None, device=None, workspace=None):

@@ -25,7 +25,6 @@ constexpr int PA_OLD = 68;               // floats a query's row takes in LDS: 1
 constexpr float kRaise = 8.f;            // the reference follows the maximum from 2^8 on
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint4 load_once(const uint8_t* p) {
   return __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4*)p));
 }
@@ -47,7 +46,9 @@ __device__ __forceinline__ bf16x8 values8(uint32_t a, uint32_t b) {
 
 // Floats as sums of bf16 for the matrix instructions: a pair where the result is
 // bf16 (one bf16 alone would move a score of 20 by 0.04, the pair by 2e-4), three,
-// which is all of them, where it is float32.
+// which is all of them, where it is float32.  A pair is off by up to 2^-17 of the number
+// where its first is rounded (queries), 2^-16 where it is cut (weights): against products in
+// float32 one result of 150 to 200 comes out a bf16 step apart, as far from 64 bits as the other.
 template <typename T>
 constexpr int kTerms = sizeof(T) == 2 ? 2 : 3;
 template <int N>

@@ -228,8 +228,8 @@ struct Lds {
 };
 static_assert(kRulesMaxVocab <= SM_NT * SM_U * 64 * 4, "a segment a thread");
 
-// bf16 logits by their values: SV_N values from the row's largest down (17344 or more of them
-// negative ones where that is below 4: to -384), the last for all behind.
+// bf16 logits by their values: SV_N values from the row's largest down (where that is below 4,
+// 17279 or more of them negative ones: to -256, which is not one of them), the last for all behind.
 constexpr int SV_N = 33 * SM_NT, SV_IDS = 2048;
 struct ValuesLds {
   double tab[SM_TAB];
