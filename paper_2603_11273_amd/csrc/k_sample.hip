@@ -25,10 +25,10 @@
 // times a polynomial, in 64 bits.  Bound by instructions (a weight takes 22, 13 of them on
 // doubles: some 0.2 ns a token of a row) and by the fetch of code that runs once, some 0.1 us
 // for 64 bytes, hence loops where they cost nothing.  A row of 51865 under top-p
-// takes 24 to 31 us by what it keeps (max 4, guess 5, list and weights 16, cut 4; 62 where the
-// lists cannot hold it), 128 rows under all filters 33, 256 bf16 rows of 131071 with 5 draws 75
-// (max 12, counts 14, their weights and cuts 18, segments 17, draws 7); sorting each row took
-// 302, 1453, 3805.
+// takes 24 to 39 us by what it keeps (max 4, guess 5, list and weights 16, cut 4 on the way; 62
+// where the lists cannot hold it), 128 rows under all filters 32, 256 bf16 rows of 131071 with 5
+// draws 75 (max 12, counts 14, their weights and cuts 18, segments 17, draws 7); sorting each row
+// took 302, 1453, 3805.
 #include <algorithm>
 
 #include "asr_device.h"
@@ -774,7 +774,7 @@ __global__ __launch_bounds__(SM_NT) void k_sample(SampleLaunch a, int unit) {
     //    51866  top-k 1000  41 / 43, 40 / 47, 49 / 42   top-p 0.5  31 / 44, 45 / 48, 67 / 43   0.9  40 / 44, 64 / 48, 69 / 43
     //   131071  top-k 1000  78 / 70, 75 / 73, 89 / 69   top-p 0.5  68 / 70, 139 / 75, 141 / 71 0.9  89 / 71, 135 / 75, 146 / 71
     // (the last 256 rows), and top-k 50 and 768 of 51866 28 / 43 and 37 / 43.  Over top-k 769 to
-    // half of the tokens, top-p 0.3 to 0.99 and both, lists take 0.62 to 1.02 of the values' time at
+    // half of the tokens, top-p 0.3 to 0.99 and both, lists take 0.63 to 1.02 of the values' time at
     // 8200 tokens (by deviation), 0.81 to 1.18 at 12001, 0.82 to 1.34 at 16000 (1.01 on the whole),
     // 0.99 to 1.45 at 51866.
     if (a.vocab > SM_VALUES && (k_on ? top_k > SM_FEW : p_on)) {
