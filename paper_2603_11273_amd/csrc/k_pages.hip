@@ -124,9 +124,10 @@ __device__ __forceinline__ NewScale new_scale(uint32_t top, int old, const float
 // One block of 256 threads per (sequence, touched block of positions, head, keys or
 // values); thread = (position, 16 dims).  Values lie [dim][position] and are turned in LDS.
 // Bound by memory: 36000 bf16 tokens of 20 heads, 276 MB, in 58 us where no cache holds them
-// (4.8 TB/s), in 49 where the last level holds some (the same call again).  A thread of 4 positions x 4 dims turns its codes in
-// registers, but its loads of 8 bytes cost more than that saves (71 us a call).  What is not finite is looked for once a block: without any,
-// codes need neither bounds nor a test.
+// (4.8 TB/s), in 49 where the last level holds some (the same call again).  A thread of 4
+// positions x 4 dims turns its codes in registers, but its loads of 8 bytes cost more than
+// that saves (71 us).  What is not finite is looked for once a block: without any, codes
+// need neither bounds nor a test.
 constexpr int PW_PITCH = 68;               // bytes of a dim in LDS: the four groups of dims write to banks of their own
 template <typename T>
 __global__ __launch_bounds__(256) void k_write_pages(PageWriteLaunch a, int touched) {
